@@ -412,6 +412,139 @@ int xsv_selftest_device_table(void);
  */
 int xsv_plan_batch_groups(int n, const int* cache_tokens, const int* frame_tokens, int heads, int multiprocessors);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Many sequences of different lengths from one pool of 4-bit pages (no counterpart in the paper, which streams one
+ * video through a cache of its own; this is what a server of many requests needs next to it).
+ *
+ * A page holds 64 tokens -- one quantisation group -- of every key/value head of one layer, quantised at the paper's
+ * granularities (Eq. 11: keys per channel over the page's 64 tokens, values per token over 64 channels) with fp16
+ * parameters rounded outwards: offset z = the group's minimum rounded down to fp16, scale s = (maximum - z) / 15
+ * rounded up to fp16 (1 where that is 0), code = nearest-even of (x - z) / s, value = code * s + z, off by at most
+ * s / 2.  Inputs are finite; magnitudes beyond 65504 are stored as 65504.  A sequence is a row of a block table (page
+ * indices in order) and a length; sequences take pages from a ring of free pages.  A sequence's last, unfilled page
+ * keeps its keys as they came, 16 bits, in the sequence's tail (per-channel scales need all 64 tokens); its values are
+ * in the page.  A step of a model: xsv_page_plan once, then per layer xsv_qk_norm_rope, xsv_page_append,
+ * xsv_page_attention.
+ *
+ * These entry points keep no state and own no memory: everything is the caller's, lengths and tables stay on the
+ * device, nothing synchronises, and all of them can be captured into a CUDA graph (the first call on a device, which
+ * may load the kernels, belongs before the capture).  They use the current device, which must be that of the
+ * pointers and of `stream`.  All int arrays are device arrays.  Index values read on the device are checked there: a
+ * token, page or sequence that is out of range is skipped, and what depends on it is not written or reads as masked.
+ */
+typedef enum { XSV_NORM_NONE = 0, XSV_NORM_RMS = 1, XSV_NORM_LAYER = 2 } xsv_norm;
+typedef enum {
+    XSV_ROPE_NONE = 0,
+    XSV_ROPE_HALF = 1,    /* channel i with channel i + rotary_dim / 2                                     */
+    XSV_ROPE_PAIRS = 2,   /* channel 2 i with channel 2 i + 1                                              */
+    XSV_ROPE_2D = 3       /* two positions a token: the first half of the head by the first, the second by
+                             the second, each half as XSV_ROPE_HALF                                        */
+} xsv_rope;
+typedef enum { XSV_TOKEN_MAJOR = 0 /* [token][head][d] */, XSV_HEAD_MAJOR = 1 /* [head][token][d], xsv_step's */ } xsv_layout;
+
+/*
+ * Queries and keys of a projection, normalised per head and rotated by position, and the values, laid out for
+ * xsv_step (XSV_HEAD_MAJOR) or for the page operators (XSV_TOKEN_MAJOR), in one pass.
+ *   q, k, v       : device, 16-bit; row of token t at t * stride elements, heads contiguous ([heads][head_dim]).  Any
+ *                   of the three may be NULL together with its output.  Strides are multiples of 8 elements.
+ *   head_dim      : 64 or 128.
+ *   norm          : over a head's channels: x / sqrt(mean x^2 + eps) (RMS) or (x - mean) / sqrt(var + eps) (LAYER),
+ *                   then * weight + bias.  Weights and biases: device, 16-bit (`dtype`), [head_dim], each may be NULL
+ *                   (1, 0); ignored for XSV_NORM_NONE.
+ *   rope          : angle = position * inv_freq, in float64; (lo, hi) -> (lo cos - hi sin, hi cos + lo sin).
+ *                   rotary_dim (a multiple of 8, at most head_dim): channels that are rotated, from the first on; must
+ *                   be head_dim for XSV_ROPE_2D.
+ *   inv_freq      : device, float [rotary_dim / 2]; [head_dim / 4] for XSV_ROPE_2D.
+ *   positions     : device, int [n_tokens]; [n_tokens][2] for XSV_ROPE_2D.  Any int, negative ones too.
+ *   q_out, ...    : contiguous in `layout`; must not alias an input.  Rounded once, from float32.
+ * Pointers 16-byte aligned (inv_freq, positions: 4).  n_tokens may be 0.
+ */
+xsv_status xsv_qk_norm_rope(const void* q, const void* k, const void* v, long long q_stride, long long k_stride,
+                            long long v_stride, int n_tokens, int q_heads, int kv_heads, int head_dim, xsv_dtype dtype,
+                            xsv_norm norm, const void* q_weight, const void* q_bias, const void* k_weight,
+                            const void* k_bias, float eps, xsv_rope rope, int rotary_dim, const float* inv_freq,
+                            const int* positions, xsv_layout layout, void* q_out, void* k_out, void* v_out, void* stream);
+
+#define XSV_PAGE_TOKENS 64
+#define XSV_PAGE_MAX_SEQS 8192           /* sequences (rows of a block table, tails of a pool) */
+#define XSV_PAGE_MAX_PAGES (1 << 25)     /* pages of a pool: slots are 32-bit                 */
+
+/* The pool of one layer.  Bytes of `records`: n_pages * kv_heads * 72 * head_dim (the record's layout is in
+ * csrc/page_layout.cuh); of `k_tail`: max_seqs * 2 * kv_heads * 64 * head_dim * 2 ([sequence][page index % 2][head]
+ * [token][channel], 16-bit).  Neither needs to be cleared. */
+typedef struct {
+    void* records;      /* device, 16-byte aligned */
+    void* k_tail;       /* device, 16-byte aligned */
+    long long n_pages;
+    int max_seqs;
+    int kv_heads;
+    int head_dim;       /* 64 or 128 */
+    xsv_dtype dtype;
+} xsv_page_pool;
+
+/*
+ * One step's bookkeeping, from the sequences' lengths.
+ *   cached_len   : [n_seqs], tokens that each sequence holds.
+ *   new_len      : [n_seqs], tokens that it gets now (0: none); negative: the sequence ends, its pages are given back.
+ *   block_table  : [n_seqs][table_width], entries of new pages are written, all others left as they are (a sequence
+ *                  that ended too: its length says that it holds nothing).
+ *   free_ring    : [n_pages], room for every page that these sequences may hold; the free pages are the ring_state[1]
+ *                  entries from ring_state[0] on, cyclically.
+ *   ring_state   : [2 or more], head and count; ring_state_out: [4], head, count, sequences refused, new tokens.
+ *   cu_new       : [n_seqs + 1], first new token of each sequence.
+ *   total_len    : [n_seqs], length after the step.
+ *   slot_map     : [max_tokens], page * 64 + place of each new token; -1 behind the last one and for a refused sequence.
+ *   token_seq    : [max_tokens], its sequence; -1 behind the last one.   positions: [max_tokens]; 0 behind the last one.
+ * Pages are taken in the order of the sequences, and given back behind the free ones (they are not taken by the same
+ * call).  A sequence is refused (total_len = cached_len, no page, slots -1) if its table row is too short, its
+ * tokens do not fit max_tokens, or too few pages are free for it and those before it.  Outputs must not be inputs;
+ * what is written is not read, so a repeated call does the same.  Sum of new tokens below 2^31.
+ */
+xsv_status xsv_page_plan(const int* cached_len, const int* new_len, int n_seqs, int* block_table, int table_width,
+                         int* free_ring, int n_pages, const int* ring_state, int* ring_state_out, int* cu_new,
+                         int* total_len, int* slot_map, int* token_seq, int* positions, int max_tokens, void* stream);
+
+/*
+ * New keys and values into the pages.  K, V: device, [n_tokens] rows of [kv_heads][head_dim] at k_stride / v_stride
+ * elements (multiples of 8), the tokens of a sequence together and in order, as the plan lists them.  slot_map,
+ * token_seq, cu_new, total_len: the plan's.  Tokens with slot -1 are skipped.  Keys of a page that the call fills are
+ * quantised, those of the last unfilled page kept in the tail.  A call can be repeated as long as no sequence's new
+ * tokens span three pages after starting inside one.  A page must belong to one sequence while it is not full.
+ */
+xsv_status xsv_page_append(const xsv_page_pool* pool, const void* K, const void* V, long long k_stride, long long v_stride,
+                           int n_tokens, const int* slot_map, const int* token_seq, const int* cu_new,
+                           const int* total_len, int n_seqs, void* stream);
+
+/*
+ * What the pages hold, as values: row i of K_out, V_out ([n_rows][kv_heads][head_dim], `dtype`) is the token at
+ * positions[i] of sequence token_seq[i]; zeros where there is none.
+ */
+xsv_status xsv_page_read(const xsv_page_pool* pool, const int* block_table, int table_width, const int* total_len,
+                         int n_seqs, const int* token_seq, const int* positions, int n_rows, void* K_out, void* V_out,
+                         void* stream);
+
+/*
+ * Causal attention of the new tokens over what their sequences hold, themselves included (call it after the append):
+ *   out[t][h] = softmax over positions j of the sequence, j <= position of t (and j > position - window if window > 0),
+ *               of scale * q[t][h] . k[j][h / (q_heads / kv_heads)], times v[j].
+ *   Q            : device, n_tokens rows of [q_heads][head_dim] at q_stride elements (a multiple of 8).
+ *   max_new      : at least the largest number of new tokens of a sequence (a host number; larger costs time only).
+ *   scale        : positive, usually 1 / sqrt(head_dim).
+ *   out          : [n_tokens][q_heads][head_dim], contiguous.  Rows behind cu_new[n_seqs] are left as they were; rows
+ *                  that see no token (of a sequence that the plan refused, for instance) are zero.
+ *   workspace    : device, 16-byte aligned, at least xsv_page_attention_workspace() bytes; needs no clearing, holds
+ *                  nothing between calls, and serves one call at a time (calls that may overlap take one each).
+ * Probabilities and scaled queries are rounded to fp16 before the tensor cores, sums are float32.  Every device-side
+ * wait is bounded; a row whose wait ran out is NaN.
+ */
+xsv_status xsv_page_attention(const xsv_page_pool* pool, const void* Q, long long q_stride, int n_tokens, int q_heads,
+                              const int* block_table, int table_width, const int* cu_new, const int* total_len, int n_seqs,
+                              int max_new, float scale, int window, void* out, void* workspace, size_t workspace_bytes,
+                              void* stream);
+
+/* Bytes of workspace that xsv_page_attention needs on the current device; 0 for arguments that it would refuse. */
+size_t xsv_page_attention_workspace(int n_seqs, int max_new, int q_heads, int kv_heads, int head_dim);
+
 /* Kernels launched by this library in the calling process since load (the paper has no counterpart). */
 long long xsv_kernel_launches(void);
 

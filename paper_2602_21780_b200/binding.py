@@ -4,6 +4,7 @@ the path runs in the library's CUDA kernels.  Loading fails loudly when the
 shared library has not been built (there is no fallback of any kind)."""
 from __future__ import annotations
 
+import collections
 import ctypes as C
 import os
 
@@ -16,6 +17,9 @@ XSV_OK = 0
 F16, BF16 = 0, 1
 ATTN_AUTO, ATTN_MMA, ATTN_TC5 = 0, 1, 2
 PHASES = ("attn", "score", "select", "quant")
+NORMS = {None: 0, "none": 0, "rms": 1, "layer": 2}
+ROPES = {None: 0, "none": 0, "half": 1, "pairs": 2, "2d": 3}
+PAGE_TOKENS = 64
 
 # every symbol include/xsv.h declares: name -> (restype, argtypes)
 _vp, _i, _ll = C.c_void_p, C.c_int, C.c_longlong
@@ -49,6 +53,13 @@ SYMBOLS = {
     "xsv_selftest_bounded_wait": (_i, [_vp]),
     "xsv_selftest_device_table": (_i, []),
     "xsv_plan_batch_groups": (_i, [_i, C.POINTER(_i), C.POINTER(_i), _i, _i]),
+    "xsv_qk_norm_rope": (_i, [_vp, _vp, _vp, _ll, _ll, _ll, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, C.c_float, _i, _i,
+                              _vp, _vp, _i, _vp, _vp, _vp, _vp]),
+    "xsv_page_plan": (_i, [_vp, _vp, _i, _vp, _i, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp]),
+    "xsv_page_append": (_i, [_vp, _vp, _vp, _ll, _ll, _i, _vp, _vp, _vp, _vp, _i, _vp]),
+    "xsv_page_read": (_i, [_vp, _vp, _i, _vp, _i, _vp, _vp, _i, _vp, _vp, _vp]),
+    "xsv_page_attention": (_i, [_vp, _vp, _ll, _i, _i, _vp, _i, _vp, _vp, _i, _i, C.c_float, _i, _vp, _vp, C.c_size_t, _vp]),
+    "xsv_page_attention_workspace": (C.c_size_t, [_i, _i, _i, _i, _i]),
     "xsv_kernel_launches": (_ll, []),
     "xsv_strerror": (C.c_char_p, [_i]),
     "xsv_last_cuda_error": (C.c_char_p, []),
@@ -289,3 +300,182 @@ def selftest_bounded_wait(stream=None):
 
 def kernel_launches():
     return int(load().xsv_kernel_launches())
+
+
+# ------------------------------------------------------------------ many sequences over a shared pool of 4-bit pages
+# Tensors in, tensors out: the calls run on the device of their tensors and, unless `stream` is given, on its current
+# stream; with `stream`, outputs and workspaces are allocated for that stream.  Nothing synchronises.
+
+class _PagePool(C.Structure):
+    _fields_ = [("records", C.c_void_p), ("k_tail", C.c_void_p), ("n_pages", C.c_longlong), ("max_seqs", C.c_int),
+                ("kv_heads", C.c_int), ("head_dim", C.c_int), ("dtype", C.c_int)]
+
+
+PagePlan = collections.namedtuple("PagePlan", "cu_new total_len slot_map token_seq positions ring_state")
+PagePlan.__doc__ = """What page_plan() says of a step (see xsv_page_plan); ring_state is the next step's."""
+
+
+def _on_device(call, first, stream):
+    """Runs call(stream pointer) with the tensor's device current and, if a stream is given, that stream current."""
+    import torch
+    if not first.is_cuda:
+        raise ValueError("xsv: CUDA tensors are needed")
+    dev = first.device.index
+    if stream is not None:
+        if stream.device != first.device:
+            raise ValueError("xsv: the stream belongs to another device than the tensors")
+        with torch.cuda.stream(stream):
+            return call(stream.cuda_stream)
+    if dev != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return call(torch.cuda.current_stream(dev).cuda_stream)
+    return call(torch.cuda.current_stream(dev).cuda_stream)
+
+
+def _tensor(t, name, dtype, device, *shape):
+    """A contiguous tensor of this type, device and shape (None: any size); its address."""
+    if t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"xsv: {name} must be a contiguous {dtype} tensor on {device}")
+    if t.dim() != len(shape) or any(w is not None and w != h for w, h in zip(shape, t.shape)):
+        raise ValueError(f"xsv: {name} has shape {tuple(t.shape)}, expected {shape}")
+    return t.data_ptr()
+
+
+def _rows(t, name, dtype, device, *shape):
+    """Rows [tokens, heads, head_dim] whose heads are contiguous, at any stride: (address, stride in elements)."""
+    if t.dtype != dtype or t.device != device:
+        raise ValueError(f"xsv: {name} must be a {dtype} tensor on {device}")
+    if t.dim() != 3 or any(w is not None and w != h for w, h in zip(shape, t.shape)):
+        raise ValueError(f"xsv: {name} has shape {tuple(t.shape)}, expected {shape}")
+    if t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2])):
+        raise ValueError(f"xsv: {name} needs contiguous heads and channels")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _pool(pages, k_tail):
+    import torch
+    if pages.dim() != 3 or k_tail.dim() != 5 or pages.shape[2] != 72 * k_tail.shape[4]:
+        raise ValueError("xsv: pages are [pages, kv_heads, 72 * head_dim], k_tail is [sequences, 2, kv_heads, 64, head_dim]")
+    rec = _tensor(pages, "pages", torch.uint8, pages.device, None, None, None)
+    tail = _tensor(k_tail, "k_tail", k_tail.dtype, pages.device, None, 2, pages.shape[1], PAGE_TOKENS, None)
+    return _PagePool(rec, tail, pages.shape[0], k_tail.shape[0], pages.shape[1], k_tail.shape[4], _dtype_code(k_tail))
+
+
+def page_pool(n_pages, max_seqs, kv_heads, head_dim, dtype, device="cuda"):
+    """Uninitialised storage of one layer's pool: (pages, k_tail), as the page_* calls take them."""
+    import torch
+    return (torch.empty(n_pages, kv_heads, 72 * head_dim, dtype=torch.uint8, device=device),
+            torch.empty(max_seqs, 2, kv_heads, PAGE_TOKENS, head_dim, dtype=dtype, device=device))
+
+
+def qk_norm_rope(q, k, v=None, *, norm=None, q_weight=None, q_bias=None, k_weight=None, k_bias=None, eps=1e-6, rope=None,
+                 inv_freq=None, positions=None, head_major=False, stream=None):
+    """xsv_qk_norm_rope: q [n, q_heads, d], k and v [n, kv_heads, d] (rows may be views into a projection's output) ->
+    normalised, rotated and laid out (q, k, v), [n, heads, d] or, with head_major, [heads, n, d].  norm: None, "rms",
+    "layer"; rope: None, "half", "pairs", "2d" with inv_freq float32 [rotary_dim / 2] ([d / 4] for "2d") and positions
+    int32 [n] ([n, 2])."""
+    import torch
+    if norm not in NORMS or rope not in ROPES:
+        raise ValueError(f"xsv: norm {norm!r} or rope {rope!r} is unknown")
+
+    def call(st):
+        dt, dev, n, d = q.dtype, q.device, q.shape[0], q.shape[-1]
+        qp, qs = _rows(q, "q", dt, dev, None, None, None)
+        kp, ks = _rows(k, "k", dt, dev, n, None, d)
+        vp, vs = _rows(v, "v", dt, dev, n, k.shape[1], d) if v is not None else (None, 0)
+        w = [None if t is None else _tensor(t, "weight", dt, dev, d) for t in (q_weight, q_bias, k_weight, k_bias)]
+        code, rot, fp, pp = ROPES[rope], 0, None, None
+        if code:
+            if inv_freq is None or positions is None:
+                raise ValueError("xsv: rope needs inv_freq and positions")
+            rot = d if code == 3 else 2 * inv_freq.numel()
+            fp = _tensor(inv_freq, "inv_freq", torch.float32, dev, d // 4 if code == 3 else None)
+            pp = _tensor(positions, "positions", torch.int32, dev, *((n, 2) if code == 3 else (n,)))
+        shape = (lambda t: (t.shape[1], n, d)) if head_major else (lambda t: (n, t.shape[1], d))
+        out = [torch.empty(shape(t), dtype=dt, device=dev) if t is not None else None for t in (q, k, v)]
+        _check(load().xsv_qk_norm_rope(qp, kp, vp, qs, ks, vs, n, q.shape[1], k.shape[1], d, _dtype_code(q), NORMS[norm],
+                                       *w, eps, code, rot, fp, pp, int(head_major), out[0].data_ptr(), out[1].data_ptr(),
+                                       out[2].data_ptr() if v is not None else None, st), "xsv_qk_norm_rope")
+        return tuple(out) if v is not None else tuple(out[:2])
+
+    return _on_device(call, q, stream)
+
+
+def page_plan(cached_len, new_len, block_table, free_ring, ring_state, max_tokens, stream=None):
+    """xsv_page_plan: int32 CUDA tensors cached_len, new_len [sequences], block_table [sequences, width] and free_ring
+    [pages] (both updated in place), ring_state [2 or more] -> PagePlan."""
+    import torch
+
+    def call(st):
+        i32, dev, n = torch.int32, cached_len.device, cached_len.shape[0]
+        ptr = [_tensor(cached_len, "cached_len", i32, dev, n), _tensor(new_len, "new_len", i32, dev, n)]
+        table = _tensor(block_table, "block_table", i32, dev, n, None)
+        ring, state = _tensor(free_ring, "free_ring", i32, dev, None), _tensor(ring_state, "ring_state", i32, dev, None)
+        if ring_state.shape[0] < 2 or max_tokens < 0:
+            raise ValueError("xsv: ring_state holds head and count; max_tokens is not negative")
+        one = torch.empty(4 + (n + 1) + n + 3 * max_tokens, dtype=i32, device=dev)      # one allocation for all outputs
+        new_state, cu, total, slot, seq, pos = one.split((4, n + 1, n, max_tokens, max_tokens, max_tokens))
+        _check(load().xsv_page_plan(*ptr, n, table, block_table.shape[1], ring, free_ring.shape[0], state, new_state.data_ptr(),
+                                    cu.data_ptr(), total.data_ptr(), slot.data_ptr(), seq.data_ptr(), pos.data_ptr(),
+                                    max_tokens, st), "xsv_page_plan")
+        return PagePlan(cu, total, slot, seq, pos, new_state)
+
+    return _on_device(call, cached_len, stream)
+
+
+def page_append(pages, k_tail, K, V, slot_map, token_seq, cu_new, total_len, stream=None):
+    """xsv_page_append: K, V [n, kv_heads, d] (rows at any stride) into the pool, by the plan's arrays."""
+    import torch
+
+    def call(st):
+        pool, dev, n, i32 = _pool(pages, k_tail), pages.device, K.shape[0], torch.int32
+        kp, ks = _rows(K, "K", k_tail.dtype, dev, n, pool.kv_heads, pool.head_dim)
+        vp, vs = _rows(V, "V", k_tail.dtype, dev, n, pool.kv_heads, pool.head_dim)
+        seqs = total_len.shape[0]
+        if slot_map.shape[0] < n or token_seq.shape[0] < n:
+            raise ValueError("xsv: the plan lists fewer tokens than K and V hold")
+        _check(load().xsv_page_append(C.byref(pool), kp, vp, ks, vs, n, _tensor(slot_map, "slot_map", i32, dev, None),
+                                      _tensor(token_seq, "token_seq", i32, dev, None), _tensor(cu_new, "cu_new", i32, dev, seqs + 1),
+                                      _tensor(total_len, "total_len", i32, dev, seqs), seqs, st), "xsv_page_append")
+
+    _on_device(call, pages, stream)
+
+
+def page_read(pages, k_tail, block_table, total_len, token_seq, positions, stream=None):
+    """xsv_page_read: the tokens (token_seq[i], positions[i]) as values, (K, V) [rows, kv_heads, d]."""
+    import torch
+
+    def call(st):
+        pool, dev, i32, n, seqs = _pool(pages, k_tail), pages.device, torch.int32, token_seq.shape[0], total_len.shape[0]
+        K = torch.empty(n, pool.kv_heads, pool.head_dim, dtype=k_tail.dtype, device=dev)
+        V = torch.empty_like(K)
+        _check(load().xsv_page_read(C.byref(pool), _tensor(block_table, "block_table", i32, dev, seqs, None), block_table.shape[1],
+                                    _tensor(total_len, "total_len", i32, dev, seqs), seqs, _tensor(token_seq, "token_seq", i32, dev, n),
+                                    _tensor(positions, "positions", i32, dev, n), n, K.data_ptr(), V.data_ptr(), st), "xsv_page_read")
+        return K, V
+
+    return _on_device(call, pages, stream)
+
+
+def page_attention(Q, pages, k_tail, block_table, cu_new, total_len, max_new, *, scale=None, window=0, out=None, stream=None):
+    """xsv_page_attention: Q [n, q_heads, d] (rows at any stride), new tokens of all sequences in a row -> out
+    [n, q_heads, d].  max_new: the most new tokens of a sequence.  Rows behind the last sequence are not written: they
+    keep what `out` held, and hold nothing defined if it was not given."""
+    import torch
+
+    def call(st):
+        pool, dev, i32, n, seqs = _pool(pages, k_tail), pages.device, torch.int32, Q.shape[0], total_len.shape[0]
+        qp, qs = _rows(Q, "Q", k_tail.dtype, dev, n, None, pool.head_dim)
+        heads = Q.shape[1]
+        to = out if out is not None else torch.empty(n, heads, pool.head_dim, dtype=Q.dtype, device=dev)
+        op = _tensor(to, "out", Q.dtype, dev, n, heads, pool.head_dim)
+        need = load().xsv_page_attention_workspace(seqs, max_new, heads, pool.kv_heads, pool.head_dim)
+        space = torch.empty(need, dtype=torch.uint8, device=dev)
+        _check(load().xsv_page_attention(C.byref(pool), qp, qs, n, heads, _tensor(block_table, "block_table", i32, dev, seqs, None),
+                                         block_table.shape[1], _tensor(cu_new, "cu_new", i32, dev, seqs + 1),
+                                         _tensor(total_len, "total_len", i32, dev, seqs), seqs, max_new,
+                                         pool.head_dim ** -0.5 if scale is None else scale, window, op, space.data_ptr(), need, st),
+               "xsv_page_attention")
+        return to
+
+    return _on_device(call, pages, stream)

@@ -1,0 +1,66 @@
+// The record in which a page holds 64 tokens of one key/value head at 4 bits, and the device helpers of the kernels
+// that read and write it.  For head_dim d a record is 72 d bytes:
+//   [0, 32 d)     key codes    [d/16 k][8 g][4 j][4 m] 32-bit words
+//   [32 d, 64 d)  value codes  [4 k][d/64 c][8 g][4 j][4 m] 32-bit words
+//   [64 d, 72 d)  fp16: key scale [d], key offset [d], value scale [d/64][8 g][8 i], value offset [d/64][8 g][8 i]
+//                 (token 8 i + g)
+// A word is one lane's A operand of mma.m16n8k16 (row, k) = keys: (token, channel), values: (channel, token), with
+// lane = 4 g + j: nibbles 0..7 are, from the low end,
+//   (g, lo0) (g + 8, lo0) (g, hi0) (g + 8, hi0) (g, lo1) (g + 8, lo1) (g, hi1) (g + 8, hi1)
+// where lo = k columns 2 j + {0, 1} and hi = 2 j + 8 + {0, 1}.  Masking with 0x000F000F therefore yields the fp16 pair
+// of an operand register as subnormals, code * 2^-24, and with 0x00F000F0 that of the row eight below as
+// code * 2^-20: no subtraction and no conversion, one logic operation per two codes; the powers of two are taken
+// out of the float32 accumulator, where each row has its own.
+//   keys:   row r of word m is token 16 m + r; column 2 j + {0, 1} of step k is channel 32 (k/2) + 8 j + 4 (k%2) + {0, 1},
+//           column 2 j + 8 + {0, 1} the two after it: a lane's channels are 8 consecutive ones per two steps, so that
+//           a row of 16-bit queries or keys is read 16 bytes at a time;
+//   values: column r of step k is token 16 k + r; row g of word m is channel 64 c + 8 g + 2 m, row g + 8 the one after
+//           it: a lane's output channels are 8 consecutive ones.
+// Scales and offsets are fp16, rounded outwards (offset down, scale up), so that no value leaves the code range and a
+// value is off by at most half a scale.
+#pragma once
+#include "../../include/xsv.h"
+#include "xsv_common.cuh"
+
+#define XSV_PAGE XSV_PAGE_TOKENS
+
+template <int D> struct PageRec {
+    static constexpr int K_CODES = 0, V_CODES = 32 * D, K_SCALE = 64 * D, K_ZERO = 66 * D, V_SCALE = 68 * D,
+                         V_ZERO = 70 * D, BYTES = 72 * D;
+};
+
+// The pool as the kernels see it (host struct xsv_page_pool).
+struct PoolView {
+    uint8_t* rec;
+    void* k_tail;        // [max_seqs][2][heads][64][d], 16-bit
+    long long n_pages;
+    int max_seqs, heads;
+};
+
+// Checks of a pool's description, on the host; fills the kernels' view of it.
+xsv_status xsv_pool_view(const xsv_page_pool* pool, PoolView* v);   // page_cache.cu
+// Turns a CUDA error into XSV_ERR_CUDA and keeps it for xsv_last_cuda_error.
+xsv_status xsv_cuda_status(cudaError_t e);                          // xsv_api.cu
+
+template <typename T, int D> __device__ __forceinline__ T* tail_rows(const PoolView& pv, int seq, int page, int head) {
+    return static_cast<T*>(pv.k_tail) + ((((size_t)seq * 2 + (page & 1)) * pv.heads + head) * XSV_PAGE) * D;
+}
+template <int D> __device__ __forceinline__ uint8_t* page_rec(const PoolView& pv, int page, int head) {
+    return pv.rec + ((size_t)page * pv.heads + head) * PageRec<D>::BYTES;
+}
+
+// two 16-bit values of a word as floats
+template <typename T> __device__ __forceinline__ float2 xsv_unpack2(uint32_t w);
+template <> __device__ __forceinline__ float2 xsv_unpack2<__half>(uint32_t w) { return __half22float2(*reinterpret_cast<__half2*>(&w)); }
+template <> __device__ __forceinline__ float2 xsv_unpack2<__nv_bfloat16>(uint32_t w) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+
+// Scale and offset of a group from its minimum and maximum (already inside +-65504): every operation rounds outwards.
+// 15 * fp16 is exact in float32, so the two float32 roundings never carry the quotient past the fp16 it rounds up to.
+__device__ __forceinline__ void page_params(float mn, float mx, __half& s, __half& z) {
+    z = __float2half_rd(mn);
+    s = __float2half_ru(__fdiv_ru(__fsub_ru(mx, __half2float(z)), 15.f));
+    if (__half2float(s) == 0.f) s = __float2half_rn(1.f);
+}
+__device__ __forceinline__ float clamp_half(float x) { return fminf(fmaxf(x, -65504.f), 65504.f); }

@@ -1,0 +1,216 @@
+// One step's bookkeeping for sequences that share a pool of pages, from their lengths alone and without the host:
+// pages taken from and given back to a ring of free pages, block-table entries of the new pages, and for every new
+// token its slot, sequence and position.
+//
+// Bound by latency: a few bytes per sequence and 12 per token.  Two scans over the sequences (tokens; pages) give
+// every sequence its place among the tokens and in the ring.  Each block repeats the scans for all sequences (they
+// are at most XSV_PAGE_MAX_SEQS, 16 per thread) instead of waiting for another block's, so that one launch without
+// any communication does it; the blocks then share out the tokens (found in the scanned offsets by bisection, in
+// shared memory) and the table rows.  Nothing that is read is written: ring positions that are pushed never meet
+// those that are popped (free pages plus pages in use are never more than the ring holds), so a call can be repeated.
+#include <algorithm>
+
+#include "../../include/xsv.h"
+#include "page_layout.cuh"
+#include "xsv_kernels.h"
+
+namespace {
+
+constexpr int THREADS = 512;
+constexpr int TOKENS_PER_BLOCK = 2048;
+
+struct Plan {
+    const int* cached;
+    const int* fresh;
+    int* table;
+    int* ring;
+    const int* state_in;
+    int* state_out;
+    int* cu;
+    int* total;
+    int* slot;
+    int* seq;
+    int* pos;
+    int n_seqs, width, n_pages, max_tokens;
+};
+
+// exclusive scan of one pair per thread over the block; returns the block's totals in `all`
+__device__ __forceinline__ void block_scan2(long long& a, long long& b, long long (&all)[2], long long (*sh)[2]) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    long long x = a, y = b;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long u = __shfl_up_sync(0xFFFFFFFFu, x, o), v = __shfl_up_sync(0xFFFFFFFFu, y, o);
+        if (lane >= o) { x += u; y += v; }
+    }
+    if (lane == 31) { sh[warp][0] = x; sh[warp][1] = y; }
+    __syncthreads();
+    if (warp == 0) {
+        long long u = lane < THREADS / 32 ? sh[lane][0] : 0, v = lane < THREADS / 32 ? sh[lane][1] : 0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long s = __shfl_up_sync(0xFFFFFFFFu, u, o), t = __shfl_up_sync(0xFFFFFFFFu, v, o);
+            if (lane >= o) { u += s; v += t; }
+        }
+        sh[lane][0] = u;
+        sh[lane][1] = v;
+    }
+    __syncthreads();
+    a = x - a + (warp ? sh[warp - 1][0] : 0);
+    b = y - b + (warp ? sh[warp - 1][1] : 0);
+    all[0] = sh[31][0];
+    all[1] = sh[31][1];
+    __syncthreads();
+}
+
+__global__ void __launch_bounds__(THREADS) page_plan_kernel(const __grid_constant__ Plan p) {
+    extern __shared__ int dyn[];
+    int* s_cu = dyn;                         // [n_seqs + 1] first token of each sequence
+    int* s_page = dyn + p.n_seqs + 1;        // [n_seqs] pages popped before it; -1 - that if it was refused
+    int* s_free = s_page + p.n_seqs;         // [n_seqs] pages pushed before it
+    __shared__ long long sh[32][2];
+    __shared__ int s_refused;
+    xsv_dep_release();
+    xsv_dep_sync();
+    const int tid = threadIdx.x, per = (p.n_seqs + THREADS - 1) / THREADS;
+    const int s0 = min(p.n_seqs, tid * per), s1 = min(p.n_seqs, s0 + per);
+    if (tid == 0) s_refused = 0;
+    const int head = p.n_pages > 0 ? (int)(((long long)p.state_in[0] % p.n_pages + p.n_pages) % p.n_pages) : 0;
+    const int count = max(0, min(p.state_in[1], p.n_pages));
+
+    long long tok = 0, zero = 0, all[2];
+    for (int s = s0; s < s1; ++s) tok += max(0, p.fresh[s]);
+    block_scan2(tok, zero, all, sh);
+    const int n_live = (int)min(all[0], (long long)p.max_tokens);
+    // pages each sequence needs or gives back; a sequence that its table row or the token arrays cannot hold needs none
+    auto pages_of = [&](int s, long long cu, long long& need, long long& freed, bool& bad) {
+        const long long c = max(0, p.cached[s]), n = p.fresh[s];
+        const long long have = (c + XSV_PAGE - 1) / XSV_PAGE;
+        need = freed = 0;
+        bad = false;
+        if (n < 0) { freed = min(have, (long long)p.width); return; }
+        need = (c + n + XSV_PAGE - 1) / XSV_PAGE - have;
+        bad = have + need > p.width || (n > 0 && cu + n > p.max_tokens);
+        if (bad) need = 0;
+    };
+    long long need_sum = 0, freed_sum = 0, cu = tok;
+    for (int s = s0; s < s1; ++s) {
+        long long need, freed;
+        bool bad;
+        pages_of(s, cu, need, freed, bad);
+        need_sum += need;
+        freed_sum += freed;
+        s_cu[s] = (int)min(cu, (long long)p.max_tokens);
+        cu += max(0, p.fresh[s]);
+    }
+    block_scan2(need_sum, freed_sum, all, sh);
+    cu = tok;
+    int refused = 0;
+    long long taken = 0;
+    for (int s = s0; s < s1; ++s) {
+        long long need, freed;
+        bool bad;
+        pages_of(s, cu, need, freed, bad);
+        cu += max(0, p.fresh[s]);
+        if (need > 0 && need_sum + need > count) bad = true;
+        const int before = (int)min(need_sum, (long long)p.n_pages);
+        s_page[s] = bad ? -1 - before : before;
+        s_free[s] = (int)min(freed_sum, (long long)p.n_pages);
+        refused += bad;
+        if (!bad) taken += need;
+        need_sum += need;
+        freed_sum += freed;
+    }
+    if (tid == 0) s_cu[p.n_seqs] = n_live;
+    if (refused) atomicAdd(&s_refused, refused);
+    const long long freed_all = all[1];
+    zero = 0;
+    block_scan2(taken, zero, all, sh);       // also orders the shared arrays
+    const long long taken_all = all[0];
+    auto at_ring = [&](long long i) { return (int)(((long long)head + i) % p.n_pages); };
+
+    if (blockIdx.x == 0) {
+        if (tid == 0) {
+            p.state_out[0] = p.n_pages > 0 ? at_ring(taken_all) : 0;
+            p.state_out[1] = (int)min((long long)count - taken_all + freed_all, (long long)p.n_pages);
+            p.state_out[2] = s_refused;
+            p.state_out[3] = n_live;
+            p.cu[p.n_seqs] = n_live;
+        }
+        for (int s = tid; s < p.n_seqs; s += THREADS) {
+            const int c = max(0, p.cached[s]), n = p.fresh[s];
+            p.cu[s] = s_cu[s];
+            p.total[s] = n < 0 ? 0 : s_page[s] < 0 ? c : c + n;
+        }
+    }
+    // table rows and ring, a warp per sequence
+    const int warp = (blockIdx.x * THREADS + tid) >> 5, n_warps = gridDim.x * (THREADS >> 5), lane = tid & 31;
+    for (int s = warp; s < p.n_seqs; s += n_warps) {
+        const long long c = max(0, p.cached[s]), n = p.fresh[s];
+        const long long have = (c + XSV_PAGE - 1) / XSV_PAGE;
+        int* row = p.table + (size_t)s * p.width;
+        if (n < 0) {
+            for (long long w = lane; w < min(have, (long long)p.width); w += 32) p.ring[at_ring((long long)count + s_free[s] + w)] = row[w];
+        } else if (s_page[s] >= 0) {
+            const long long blocks = (c + n + XSV_PAGE - 1) / XSV_PAGE;
+            for (long long w = have + lane; w < blocks; w += 32) row[w] = p.ring[at_ring(s_page[s] + w - have)];
+        }
+    }
+    // tokens
+    const int t0 = blockIdx.x * TOKENS_PER_BLOCK, t1 = min(p.max_tokens, t0 + TOKENS_PER_BLOCK);
+    for (int t = t0 + tid; t < t1; t += THREADS) {
+        int slot = -1, seq = -1, pos = 0;
+        if (t < n_live) {
+            int lo = 0, hi = p.n_seqs - 1;   // the last sequence that starts at or before t and is not empty
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (s_cu[mid] <= t) lo = mid; else hi = mid - 1;
+            }
+            seq = lo;
+            const long long c = max(0, p.cached[seq]);
+            const long long at = c + (t - s_cu[seq]);
+            pos = (int)at;
+            if (s_page[seq] >= 0) {
+                const long long have = (c + XSV_PAGE - 1) / XSV_PAGE, b = at / XSV_PAGE;
+                const int page = b < have ? p.table[(size_t)seq * p.width + b] : p.ring[at_ring(s_page[seq] + b - have)];
+                if (page >= 0 && page < XSV_PAGE_MAX_PAGES) slot = page * XSV_PAGE + (int)(at % XSV_PAGE);
+            }
+        }
+        p.slot[t] = slot;
+        p.seq[t] = seq;
+        p.pos[t] = pos;
+    }
+}
+
+}  // namespace
+
+
+extern "C" xsv_status xsv_page_plan(const int* cached_len, const int* new_len, int n_seqs, int* block_table, int table_width,
+                                    int* free_ring, int n_pages, const int* ring_state, int* ring_state_out, int* cu_new,
+                                    int* total_len, int* slot_map, int* token_seq, int* positions, int max_tokens,
+                                    void* stream) {
+    if (!cached_len || !new_len || !block_table || !free_ring || !ring_state || !ring_state_out || !cu_new || !total_len) return XSV_ERR_ARG;
+    if (n_seqs <= 0 || table_width <= 0 || n_pages <= 0 || max_tokens < 0) return XSV_ERR_ARG;
+    if (max_tokens > 0 && (!slot_map || !token_seq || !positions)) return XSV_ERR_ARG;
+    if (n_pages > XSV_PAGE_MAX_PAGES || n_seqs > XSV_PAGE_MAX_SEQS) return XSV_ERR_LIMIT;
+    // blocks read the inputs while others write the outputs
+    if (ring_state == ring_state_out || cached_len == total_len || new_len == total_len || cached_len == cu_new || new_len == cu_new) return XSV_ERR_ARG;
+    Plan p{cached_len, new_len, block_table, free_ring, ring_state, ring_state_out, cu_new, total_len, slot_map, token_seq, positions,
+           n_seqs, table_width, n_pages, max_tokens};
+    const long long blocks = std::max(1LL, ((long long)max_tokens + TOKENS_PER_BLOCK - 1) / TOKENS_PER_BLOCK);
+    const size_t smem = (3 * (size_t)n_seqs + 1) * sizeof(int);
+    cudaError_t e = cudaSuccess;
+    if (smem > 40 * 1024) {
+        static XsvPerDeviceInt ready;
+        const int dev = xsv_current_device();
+        if (!ready.get(dev)) {
+            e = cudaFuncSetAttribute(page_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)((3 * XSV_PAGE_MAX_SEQS + 1) * sizeof(int)));
+            if (e != cudaSuccess) return xsv_cuda_status(e);
+            ready.set(dev, 1);
+        }
+    }
+    e = xsv_launch_dep(page_plan_kernel, dim3((unsigned)blocks), dim3(THREADS), smem, (cudaStream_t)stream, p);
+    if (e != cudaSuccess) return xsv_cuda_status(e);
+    xsv_count_launch(1);
+    return XSV_OK;
+}

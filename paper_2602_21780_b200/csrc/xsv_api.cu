@@ -38,6 +38,9 @@ struct PendingEvent {
 
 }  // namespace
 
+// The same for entry points in other files.
+xsv_status xsv_cuda_status(cudaError_t e) { return cuda_fail(e); }
+
 struct xsv_cache {
     int device = 0;
     int layers = 0, H = 0, d = 0, bits = 0;
