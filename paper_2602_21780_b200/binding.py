@@ -320,7 +320,7 @@ def _on_device(call, first, stream):
     import torch
     if not first.is_cuda:
         raise ValueError("xsv: CUDA tensors are needed")
-    dev = first.device.index
+    dev = first.get_device()
     if stream is not None:
         if stream.device != first.device:
             raise ValueError("xsv: the stream belongs to another device than the tensors")
@@ -332,33 +332,48 @@ def _on_device(call, first, stream):
     return call(torch.cuda.current_stream(dev).cuda_stream)
 
 
-def _tensor(t, name, dtype, device, *shape):
-    """A contiguous tensor of this type, device and shape (None: any size); its address."""
-    if t.dtype != dtype or t.device != device or not t.is_contiguous():
-        raise ValueError(f"xsv: {name} must be a contiguous {dtype} tensor on {device}")
-    if t.dim() != len(shape) or any(w is not None and w != h for w, h in zip(shape, t.shape)):
-        raise ValueError(f"xsv: {name} has shape {tuple(t.shape)}, expected {shape}")
+# Checks of the arguments.  They cost more host time than a small kernel runs, so each is one pass of plain comparisons.
+def _tensor(t, name, dtype, dev, shape):
+    """The address of a contiguous tensor of this type, device index and shape."""
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"xsv: {name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on device {dev}, "
+                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _rows(t, name, dtype, device, *shape):
+def _list(t, name, dev):
+    """The address of an int32 list, or table, of any length."""
+    import torch
+    if t.dtype is not torch.int32 or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"xsv: {name} must be a contiguous int32 tensor on device {dev}, not {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _rows(t, name, dtype, dev, shape):
     """Rows [tokens, heads, head_dim] whose heads are contiguous, at any stride: (address, stride in elements)."""
-    if t.dtype != dtype or t.device != device:
-        raise ValueError(f"xsv: {name} must be a {dtype} tensor on {device}")
-    if t.dim() != 3 or any(w is not None and w != h for w, h in zip(shape, t.shape)):
-        raise ValueError(f"xsv: {name} has shape {tuple(t.shape)}, expected {shape}")
-    if t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2])):
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape or len(shape) != 3:
+        raise ValueError(f"xsv: {name} must be a {dtype} tensor [tokens, heads, head_dim] of shape {tuple(shape)} on device {dev}, "
+                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
+    n, h, d = shape
+    st, sh, sd = t.stride()
+    if n and (sd != 1 or (sh != d and h > 1)):
         raise ValueError(f"xsv: {name} needs contiguous heads and channels")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    return t.data_ptr(), st if n > 1 else h * d
 
 
 def _pool(pages, k_tail):
     import torch
-    if pages.dim() != 3 or k_tail.dim() != 5 or pages.shape[2] != 72 * k_tail.shape[4]:
+    if pages.dim() != 3 or k_tail.dim() != 5:
         raise ValueError("xsv: pages are [pages, kv_heads, 72 * head_dim], k_tail is [sequences, 2, kv_heads, 64, head_dim]")
-    rec = _tensor(pages, "pages", torch.uint8, pages.device, None, None, None)
-    tail = _tensor(k_tail, "k_tail", k_tail.dtype, pages.device, None, 2, pages.shape[1], PAGE_TOKENS, None)
-    return _PagePool(rec, tail, pages.shape[0], k_tail.shape[0], pages.shape[1], k_tail.shape[4], _dtype_code(k_tail))
+    (n, h, b), (seqs, _, _, _, d), dev = pages.shape, k_tail.shape, pages.get_device()
+    return _PagePool(_tensor(pages, "pages", torch.uint8, dev, (n, h, 72 * d)),
+                     _tensor(k_tail, "k_tail", k_tail.dtype, dev, (seqs, 2, h, PAGE_TOKENS, d)), n, seqs, h, d, _dtype_code(k_tail))
+
+
+def _table(t, dev, seqs):
+    if t.dim() != 2 or t.shape[0] != seqs:
+        raise ValueError(f"xsv: block_table has shape {tuple(t.shape)}, expected a row for each of {seqs} sequences")
+    return _list(t, "block_table", dev)
 
 
 def page_pool(n_pages, max_seqs, kv_heads, head_dim, dtype, device="cuda"):
@@ -379,25 +394,29 @@ def qk_norm_rope(q, k, v=None, *, norm=None, q_weight=None, q_bias=None, k_weigh
         raise ValueError(f"xsv: norm {norm!r} or rope {rope!r} is unknown")
 
     def call(st):
-        dt, dev, n, d = q.dtype, q.device, q.shape[0], q.shape[-1]
-        qp, qs = _rows(q, "q", dt, dev, None, None, None)
-        kp, ks = _rows(k, "k", dt, dev, n, None, d)
-        vp, vs = _rows(v, "v", dt, dev, n, k.shape[1], d) if v is not None else (None, 0)
-        w = [None if t is None else _tensor(t, "weight", dt, dev, d) for t in (q_weight, q_bias, k_weight, k_bias)]
+        dt, dev, (n, hq, d), hk = q.dtype, q.get_device(), q.shape, k.shape[1]
+        qp, qs = _rows(q, "q", dt, dev, (n, hq, d))
+        kp, ks = _rows(k, "k", dt, dev, (n, hk, d))
+        vp, vs = _rows(v, "v", dt, dev, (n, hk, d)) if v is not None else (None, 0)
+        qw, qb, kw, kb = [None if t is None else _tensor(t, "weight", dt, dev, (d,)) for t in (q_weight, q_bias, k_weight, k_bias)]
         code, rot, fp, pp = ROPES[rope], 0, None, None
         if code:
             if inv_freq is None or positions is None:
                 raise ValueError("xsv: rope needs inv_freq and positions")
-            rot = d if code == 3 else 2 * inv_freq.numel()
-            fp = _tensor(inv_freq, "inv_freq", torch.float32, dev, d // 4 if code == 3 else None)
-            pp = _tensor(positions, "positions", torch.int32, dev, *((n, 2) if code == 3 else (n,)))
-        shape = (lambda t: (t.shape[1], n, d)) if head_major else (lambda t: (n, t.shape[1], d))
-        out = [torch.empty(shape(t), dtype=dt, device=dev) if t is not None else None for t in (q, k, v)]
-        _check(load().xsv_qk_norm_rope(qp, kp, vp, qs, ks, vs, n, q.shape[1], k.shape[1], d, _dtype_code(q), NORMS[norm],
-                                       *w, eps, code, rot, fp, pp, int(head_major), out[0].data_ptr(), out[1].data_ptr(),
-                                       out[2].data_ptr() if v is not None else None, st), "xsv_qk_norm_rope")
-        return tuple(out) if v is not None else tuple(out[:2])
+            nf = inv_freq.shape[0] if code != 3 else d // 4
+            rot = d if code == 3 else 2 * nf
+            fp = _tensor(inv_freq, "inv_freq", torch.float32, dev, (nf,))
+            pp = _tensor(positions, "positions", torch.int32, dev, (n, 2) if code == 3 else (n,))
+        qo = q.new_empty((hq, n, d) if head_major else (n, hq, d))
+        ko = q.new_empty((hk, n, d) if head_major else (n, hk, d))
+        vo = torch.empty_like(ko) if v is not None else None
+        _check(load().xsv_qk_norm_rope(qp, kp, vp, qs, ks, vs, n, hq, hk, d, _dtype_code(q), NORMS[norm], qw, qb, kw, kb, eps,
+                                       code, rot, fp, pp, 1 if head_major else 0, qo.data_ptr(), ko.data_ptr(),
+                                       None if vo is None else vo.data_ptr(), st), "xsv_qk_norm_rope")
+        return (qo, ko) if vo is None else (qo, ko, vo)
 
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("xsv: q and k are [tokens, heads, head_dim]")
     return _on_device(call, q, stream)
 
 
@@ -407,18 +426,20 @@ def page_plan(cached_len, new_len, block_table, free_ring, ring_state, max_token
     import torch
 
     def call(st):
-        i32, dev, n = torch.int32, cached_len.device, cached_len.shape[0]
-        ptr = [_tensor(cached_len, "cached_len", i32, dev, n), _tensor(new_len, "new_len", i32, dev, n)]
-        table = _tensor(block_table, "block_table", i32, dev, n, None)
-        ring, state = _tensor(free_ring, "free_ring", i32, dev, None), _tensor(ring_state, "ring_state", i32, dev, None)
-        if ring_state.shape[0] < 2 or max_tokens < 0:
-            raise ValueError("xsv: ring_state holds head and count; max_tokens is not negative")
-        one = torch.empty(4 + (n + 1) + n + 3 * max_tokens, dtype=i32, device=dev)      # one allocation for all outputs
-        new_state, cu, total, slot, seq, pos = one.split((4, n + 1, n, max_tokens, max_tokens, max_tokens))
-        _check(load().xsv_page_plan(*ptr, n, table, block_table.shape[1], ring, free_ring.shape[0], state, new_state.data_ptr(),
-                                    cu.data_ptr(), total.data_ptr(), slot.data_ptr(), seq.data_ptr(), pos.data_ptr(),
-                                    max_tokens, st), "xsv_page_plan")
-        return PagePlan(cu, total, slot, seq, pos, new_state)
+        i32, dev, n = torch.int32, cached_len.get_device(), cached_len.shape[0]
+        if ring_state.dim() != 1 or ring_state.shape[0] < 2 or free_ring.dim() != 1 or max_tokens < 0:
+            raise ValueError("xsv: ring_state holds head and count, free_ring is a list; max_tokens is not negative")
+        one = cached_len.new_empty(4 + (n + 1) + n + 3 * max_tokens)      # one allocation for all outputs
+        state, cu, total, slot, seq, pos = one.split((4, n + 1, n, max_tokens, max_tokens, max_tokens))
+        at = one.data_ptr()
+        cu_at = at + 16
+        total_at = cu_at + 4 * (n + 1)
+        slot_at = total_at + 4 * n
+        _check(load().xsv_page_plan(_tensor(cached_len, "cached_len", i32, dev, (n,)), _tensor(new_len, "new_len", i32, dev, (n,)), n,
+                                    _table(block_table, dev, n), block_table.shape[1], _list(free_ring, "free_ring", dev),
+                                    free_ring.shape[0], _list(ring_state, "ring_state", dev), at, cu_at, total_at, slot_at,
+                                    slot_at + 4 * max_tokens, slot_at + 8 * max_tokens, max_tokens, st), "xsv_page_plan")
+        return PagePlan(cu, total, slot, seq, pos, state)
 
     return _on_device(call, cached_len, stream)
 
@@ -428,15 +449,15 @@ def page_append(pages, k_tail, K, V, slot_map, token_seq, cu_new, total_len, str
     import torch
 
     def call(st):
-        pool, dev, n, i32 = _pool(pages, k_tail), pages.device, K.shape[0], torch.int32
-        kp, ks = _rows(K, "K", k_tail.dtype, dev, n, pool.kv_heads, pool.head_dim)
-        vp, vs = _rows(V, "V", k_tail.dtype, dev, n, pool.kv_heads, pool.head_dim)
-        seqs = total_len.shape[0]
+        pool, dev, n, seqs = _pool(pages, k_tail), pages.get_device(), K.shape[0], total_len.shape[0]
+        shape = (n, pool.kv_heads, pool.head_dim)
+        kp, ks = _rows(K, "K", k_tail.dtype, dev, shape)
+        vp, vs = _rows(V, "V", k_tail.dtype, dev, shape)
         if slot_map.shape[0] < n or token_seq.shape[0] < n:
             raise ValueError("xsv: the plan lists fewer tokens than K and V hold")
-        _check(load().xsv_page_append(C.byref(pool), kp, vp, ks, vs, n, _tensor(slot_map, "slot_map", i32, dev, None),
-                                      _tensor(token_seq, "token_seq", i32, dev, None), _tensor(cu_new, "cu_new", i32, dev, seqs + 1),
-                                      _tensor(total_len, "total_len", i32, dev, seqs), seqs, st), "xsv_page_append")
+        _check(load().xsv_page_append(C.byref(pool), kp, vp, ks, vs, n, _list(slot_map, "slot_map", dev),
+                                      _list(token_seq, "token_seq", dev), _tensor(cu_new, "cu_new", torch.int32, dev, (seqs + 1,)),
+                                      _tensor(total_len, "total_len", torch.int32, dev, (seqs,)), seqs, st), "xsv_page_append")
 
     _on_device(call, pages, stream)
 
@@ -446,12 +467,13 @@ def page_read(pages, k_tail, block_table, total_len, token_seq, positions, strea
     import torch
 
     def call(st):
-        pool, dev, i32, n, seqs = _pool(pages, k_tail), pages.device, torch.int32, token_seq.shape[0], total_len.shape[0]
-        K = torch.empty(n, pool.kv_heads, pool.head_dim, dtype=k_tail.dtype, device=dev)
+        pool, dev, i32, n, seqs = _pool(pages, k_tail), pages.get_device(), torch.int32, token_seq.shape[0], total_len.shape[0]
+        K = k_tail.new_empty((n, pool.kv_heads, pool.head_dim))
         V = torch.empty_like(K)
-        _check(load().xsv_page_read(C.byref(pool), _tensor(block_table, "block_table", i32, dev, seqs, None), block_table.shape[1],
-                                    _tensor(total_len, "total_len", i32, dev, seqs), seqs, _tensor(token_seq, "token_seq", i32, dev, n),
-                                    _tensor(positions, "positions", i32, dev, n), n, K.data_ptr(), V.data_ptr(), st), "xsv_page_read")
+        _check(load().xsv_page_read(C.byref(pool), _table(block_table, dev, seqs), block_table.shape[1],
+                                    _tensor(total_len, "total_len", i32, dev, (seqs,)), seqs,
+                                    _tensor(token_seq, "token_seq", i32, dev, (n,)), _tensor(positions, "positions", i32, dev, (n,)), n,
+                                    K.data_ptr(), V.data_ptr(), st), "xsv_page_read")
         return K, V
 
     return _on_device(call, pages, stream)
@@ -464,18 +486,18 @@ def page_attention(Q, pages, k_tail, block_table, cu_new, total_len, max_new, *,
     import torch
 
     def call(st):
-        pool, dev, i32, n, seqs = _pool(pages, k_tail), pages.device, torch.int32, Q.shape[0], total_len.shape[0]
-        qp, qs = _rows(Q, "Q", k_tail.dtype, dev, n, None, pool.head_dim)
-        heads = Q.shape[1]
-        to = out if out is not None else torch.empty(n, heads, pool.head_dim, dtype=Q.dtype, device=dev)
-        op = _tensor(to, "out", Q.dtype, dev, n, heads, pool.head_dim)
-        need = load().xsv_page_attention_workspace(seqs, max_new, heads, pool.kv_heads, pool.head_dim)
-        space = torch.empty(need, dtype=torch.uint8, device=dev)
-        _check(load().xsv_page_attention(C.byref(pool), qp, qs, n, heads, _tensor(block_table, "block_table", i32, dev, seqs, None),
-                                         block_table.shape[1], _tensor(cu_new, "cu_new", i32, dev, seqs + 1),
-                                         _tensor(total_len, "total_len", i32, dev, seqs), seqs, max_new,
-                                         pool.head_dim ** -0.5 if scale is None else scale, window, op, space.data_ptr(), need, st),
-               "xsv_page_attention")
+        pool, dev, i32, seqs, lib = _pool(pages, k_tail), pages.get_device(), torch.int32, total_len.shape[0], load()
+        n, heads, hkv, d = *Q.shape[:2], pool.kv_heads, pool.head_dim
+        qp, qs = _rows(Q, "Q", k_tail.dtype, dev, (n, heads, d))
+        to = out if out is not None else Q.new_empty((n, heads, d))
+        need = lib.xsv_page_attention_workspace(seqs, max_new, heads, hkv, d)
+        space = pages.new_empty(need)
+        _check(lib.xsv_page_attention(C.byref(pool), qp, qs, n, heads, _table(block_table, dev, seqs), block_table.shape[1],
+                                      _tensor(cu_new, "cu_new", i32, dev, (seqs + 1,)), _tensor(total_len, "total_len", i32, dev, (seqs,)),
+                                      seqs, max_new, d ** -0.5 if scale is None else scale, window,
+                                      _tensor(to, "out", Q.dtype, dev, (n, heads, d)), space.data_ptr(), need, st), "xsv_page_attention")
         return to
 
+    if Q.dim() != 3:
+        raise ValueError("xsv: Q is [tokens, heads, head_dim]")
     return _on_device(call, pages, stream)

@@ -11,8 +11,8 @@
 //     channels of O);
 //   - P^T comes out of S^T by one movmatrix per 8 x 8 block, O^T leaves with 8 consecutive channels a lane.
 // q is scaled by a power of two per row so that its largest element lies in [2, 4): with s <= 8734, q s never leaves fp16,
-// and elements below 2^-14 lose at most 2^-25 absolutely.  P s is scaled by a running power of two per warp (like the
-// running maximum) so that it uses fp16's range whatever the values' magnitude.  Rounding q s, P s and the result
+// and elements below 2^-14 lose at most 2^-25 absolutely.  P s is scaled by a power of two per page, from the page's largest
+// value scale, so that it uses fp16's range whatever the values' magnitude.  Rounding q s, P s and the result
 // to fp16 / the output type are the only roundings below float32; sums, maxima and the output accumulate in float32.
 //
 // Work split.  A unit is (sequence, key/value head, tile of 8 NT query rows); its pages are the steps.  All steps of all
@@ -31,6 +31,10 @@ namespace {
 
 constexpr int WARPS = 4, THREADS = WARPS * 32;
 constexpr unsigned long long WAIT_LIMIT_NS = 2000000000ull;
+// Probabilities are 2^(x - m + P_BIAS) with m a logit that was the row's maximum when it was last looked for: as long as
+// none exceeds m by more than P_SLACK, m stays (one vote instead of a reduction and a rescale).  At most 2^10, they
+// keep fp16's full significand down to 2^-20 of the row's maximum; times a value scale of at most 16 they stay in range.
+constexpr float P_BIAS = 6.f, P_SLACK = 4.f, NO_MAX = -1e30f;
 
 struct Attn {
     PoolView pool;
@@ -39,7 +43,7 @@ struct Attn {
     const int* table;
     const int* cu;
     const int* total;
-    int4* desc;          // [workers] units that are shared: {sequence, unit in it, parts, -}; parts 0: none starts here
+    int4* desc;          // [workers] units that are shared: {sequence, head, tile, parts}; parts 0: none begins to be shared here
     float* part;         // [2 workers][slot] unnormalised rows
     long long q_stride;
     float scale;         // times log2 e
@@ -49,6 +53,14 @@ struct Attn {
 
 // one unnormalised tile: [NT][D / 16][32 lanes] float4, then maxima and sums [8 NT] float2
 template <int D, int NT> struct Part { static constexpr int FLOATS = NT * (D / 16) * 128 + NT * 16; };
+
+// Blocks per multiprocessor and stages per warp: as many warps as the registers allow (the tile's accumulators set
+// them: 12 warps of 168, 8 of 255; head_dim 64: 16 of 128, 12 of 168), as many stages as shared memory then does.
+template <int D, int NT> struct Shape {
+    static constexpr int BLOCKS = D == 64 ? (NT == 1 ? 4 : 3) : (NT == 1 ? 3 : 2);
+    static constexpr int STAGES = D == 64 ? (NT == 1 ? 3 : 4) : (NT == 1 ? 2 : 3);
+    static constexpr size_t SMEM = (size_t)WARPS * STAGES * PageRec<D>::BYTES;
+};
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ unsigned long long globaltimer() {
@@ -72,6 +84,17 @@ __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// c = a b
+__device__ __forceinline__ void mma0(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+// d = a b + c
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, const float (&c)[4]) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1),
+                   "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
     uint32_t y;
@@ -98,17 +121,28 @@ __device__ __forceinline__ uint32_t hmul2_u(uint32_t a, uint32_t b) {
     asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     return d;
 }
+__device__ __forceinline__ uint32_t hfma2_u(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t d;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+__device__ __forceinline__ uint32_t hfnma2_u(uint32_t a, uint32_t b, uint32_t c) {      // c - a b
+    const __half2 r = __hfma2(__hneg2(*reinterpret_cast<__half2*>(&a)), *reinterpret_cast<__half2*>(&b), *reinterpret_cast<__half2*>(&c));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+constexpr uint32_t ONES = 0x3C003C00u, EIGHTS = 0x48004800u, MINUS_EIGHTS = 0xC800C800u;   // pairs of fp16
+constexpr uint32_t MINUS_LO = 0x80088008u, MINUS_HI = 0x80808080u;   // -8 in the codes' units: rows g, rows g + 8
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
-__device__ __forceinline__ float half_at(const uint4& v, int i) {
-    const uint32_t w = word(v, i >> 1);
-    return __half2float(__ushort_as_half((unsigned short)(i & 1 ? w >> 16 : w & 0xFFFFu)));
+// halves i of two 8-half vectors as a pair
+__device__ __forceinline__ uint32_t pair_at(const uint4& a, const uint4& b, int i) {
+    return __byte_perm(word(a, i >> 1), word(b, i >> 1), i & 1 ? 0x7632 : 0x5410);
 }
 __device__ __forceinline__ float pow2i(int e) {            // 2^e, clamped to what float32 holds as a normal number
     return __int_as_float((min(max(e, -126), 127) + 127) << 23);
 }
 
 // A sequence as the split sees it.
-struct Seq { int new_, total, p0, pages, units; };
+struct Seq { int new_, total, p0, pages, tiles; };
 __device__ __forceinline__ Seq seq_of(const Attn& p, int s, int rows) {
     Seq q;
     const int a = min(max(p.cu[s], 0), p.n_tokens), b = min(max(p.cu[s + 1], a), p.n_tokens);
@@ -117,27 +151,29 @@ __device__ __forceinline__ Seq seq_of(const Attn& p, int s, int rows) {
     const int first = q.total - q.new_;                       // position of the first new token
     q.p0 = p.window > 0 ? max(0, first - p.window + 1) / XSV_PAGE : 0;
     q.pages = max(1, (q.total + XSV_PAGE - 1) / XSV_PAGE - q.p0);
-    q.units = q.new_ > 0 ? p.pool.heads * ((q.new_ * p.group + rows - 1) / rows) : 0;
+    q.tiles = (q.new_ * p.group + rows - 1) / rows;
     return q;
 }
 
-// A place in the list of steps: unit `u` of sequence `s`, page `p` of its `q.pages`.
-struct Cursor { int s, u, pg; Seq q; };
+// A place in the list of steps: page `pg` of the `q.pages` of (sequence, head, tile).
+struct Cursor { int s, head, tile, pg; Seq q; };
 __device__ __forceinline__ void advance(const Attn& p, Cursor& c, int rows) {
     if (++c.pg < c.q.pages) return;
     c.pg = 0;
-    if (++c.u < c.q.units) return;
-    c.u = 0;
+    if (++c.tile < c.q.tiles) return;
+    c.tile = 0;
+    if (++c.head < p.pool.heads) return;
+    c.head = 0;
     while (++c.s < p.n_seqs) {
         c.q = seq_of(p, c.s, rows);
-        if (c.q.units > 0) return;
+        if (c.q.tiles > 0) return;
     }
 }
 
-template <typename T, int D, int NT, int STAGES>
-__global__ void __launch_bounds__(THREADS) page_attn_kernel(const __grid_constant__ Attn p) {
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kernel(const __grid_constant__ Attn p) {
     using R = PageRec<D>;
-    constexpr int ROWS = 8 * NT, KS = D / 16, CT = D / 16, VG = D / 64;
+    constexpr int ROWS = 8 * NT, KS = D / 16, CT = D / 16, VG = D / 64, STAGES = Shape<D, NT>::STAGES;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(8) unsigned long long bars[WARPS][STAGES];
     __shared__ int stage_page[WARPS][STAGES];
@@ -154,7 +190,7 @@ __global__ void __launch_bounds__(THREADS) page_attn_kernel(const __grid_constan
         long long sum = 0;
         for (int s = tid * per; s < min(p.n_seqs, (tid + 1) * per); ++s) {
             const Seq q = seq_of(p, s, ROWS);
-            sum += (long long)q.units * q.pages;
+            sum += (long long)p.pool.heads * q.tiles * q.pages;
         }
         long long x = sum;
 #pragma unroll
@@ -188,12 +224,14 @@ __global__ void __launch_bounds__(THREADS) page_attn_kernel(const __grid_constan
         cur.s = lo * per;
         for (;; ++cur.s) {
             cur.q = seq_of(p, cur.s, ROWS);
-            const long long n = (long long)cur.q.units * cur.q.pages;
+            const long long n = (long long)p.pool.heads * cur.q.tiles * cur.q.pages;
             if (at < n) break;
             at -= n;
         }
-        cur.u = (int)(at / cur.q.pages);
-        cur.pg = (int)(at % cur.q.pages);
+        const int u = (int)(at / cur.q.pages);
+        cur.pg = (int)(at - (long long)u * cur.q.pages);
+        cur.head = u / cur.q.tiles;
+        cur.tile = u - cur.head * cur.q.tiles;
         // The first worker that continues a unit describes how many parts it has.
         if (cur.pg > 0) {
             const long long unit0 = x0 - cur.pg, unit1 = unit0 + cur.q.pages;
@@ -203,42 +241,44 @@ __global__ void __launch_bounds__(THREADS) page_attn_kernel(const __grid_constan
                 if (k > last) last = (int)k;
                 while (last + 1 < workers && steps * (last + 1) / workers < unit1) ++last;
                 while (last > worker && steps * last / workers >= unit1) --last;
-                if (lane == 0) p.desc[worker] = make_int4(cur.s, cur.u, last - worker + 2, 0);
+                if (lane == 0) p.desc[worker] = make_int4(cur.s, cur.head, cur.tile, last - worker + 2);
             }
         }
     }
 
     uint8_t* ring = smem + wid * STAGES * R::BYTES;
-    // Page record of the step at `c` into stage `st`.  The unfilled page's keys are not in the record.
+    // Page record of the step at `ld` into stage `st`, then on to the next step, whose page index is fetched already.  The
+    // unfilled page's keys are not in its record.
     Cursor ld = cur;
-    long long ld_at = x0;
-    auto table_at = [&](const Cursor& c) {
-        const int pg = c.q.p0 + c.pg;
-        int id = -1;
-        if (c.s < p.n_seqs && c.s < p.pool.max_seqs && pg < p.width && pg * XSV_PAGE < c.q.total) id = p.table[(size_t)c.s * p.width + pg];
-        return id >= 0 && id < p.pool.n_pages ? id : -1;
+    int ld_left = (int)(x1 - x0), ld_page = -1, ld_part = 0, ld_end = 0;
+    const int* ld_row = p.table;
+    auto ld_unit = [&]() {                                     // a sequence begins: its table row, the pages there are
+        ld_row = p.table + (size_t)min(ld.s, p.n_seqs - 1) * p.width + ld.q.p0;
+        ld_part = ld.q.total % XSV_PAGE ? ld.q.total / XSV_PAGE - ld.q.p0 : -1;
+        ld_end = ld.s < p.n_seqs ? (ld.q.total + XSV_PAGE - 1) / XSV_PAGE - ld.q.p0 : 0;
     };
-    int ld_page = table_at(ld);
-    auto issue = [&](int st) {                                 // loads the step at `ld` and advances it
-        if (ld_at >= x1) return;
-        const int tiles = ld.q.units / p.pool.heads, head = ld.u / tiles;
+    ld_unit();
+    if (ld.pg < ld_end) ld_page = ld_row[ld.pg];
+    auto issue = [&](int st) {
+        if (ld_left == 0) return;
         if (lane == 0) {
-            stage_page[wid][st] = ld_page;
-            if (ld_page >= 0) {
-                const uint8_t* rec = page_rec<D>(p.pool, ld_page, head);
-                const bool part = (ld.q.p0 + ld.pg + 1) * XSV_PAGE > ld.q.total;
-                const uint32_t off = part ? R::V_CODES : 0, bytes = R::BYTES - off, bar = smem_u32(&bars[wid][st]);
+            const bool there = (unsigned long long)(long long)ld_page < (unsigned long long)p.pool.n_pages;
+            const uint32_t bar = smem_u32(&bars[wid][st]);
+            stage_page[wid][st] = there;
+            if (there) {
+                const uint32_t off = ld.pg == ld_part ? R::V_CODES : 0, bytes = R::BYTES - off;
                 asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
                 asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                             ::"r"(smem_u32(ring + st * R::BYTES + off)), "l"(rec + off), "r"(bytes), "r"(bar) : "memory");
+                             ::"r"(smem_u32(ring + st * R::BYTES + off)), "l"(page_rec<D>(p.pool, ld_page, ld.head) + off), "r"(bytes), "r"(bar) : "memory");
             } else {
-                asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(&bars[wid][st])) : "memory");
+                asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
             }
         }
-        ++ld_at;
-        if (ld_at < x1) {
+        if (--ld_left > 0) {
+            const int seq = ld.s;
             advance(p, ld, ROWS);
-            ld_page = table_at(ld);
+            if (ld.s != seq) ld_unit();
+            ld_page = ld.pg < ld_end ? ld_row[ld.pg] : -1;
         }
     };
 #pragma unroll
@@ -246,17 +286,16 @@ __global__ void __launch_bounds__(THREADS) page_attn_kernel(const __grid_constan
 
     int stage = 0, parity = 0;
     bool failed = false;
-    uint32_t qf[NT][KS][2];
+    uint32_t qf[NT][KS / 2][2][2];                             // [32 channels][operand register][step]
     float fac[NT][2], m[NT][2], l[NT][2], zs[NT][2][VG], o[NT][CT][4];
-    int qpos[NT][2], e_run = 0, pos_lo = 0, pos_hi = 0;
-    bool fresh = true;                                         // no page of the unit yet: e_run is not set
+    int qpos[NT][2], pos_lo = 0, pos_hi = 0;
     bool whole = false;                                        // the span holds the unit's first step
-    for (long long at = x0; at < x1; ++at) {
-        const int tiles = cur.q.units / p.pool.heads, head = cur.u / tiles, tile = cur.u - head * tiles;
-        if (at == x0 || cur.pg == 0) {
+    const int n_steps = (int)(x1 - x0);
+    for (int at = 0; at < n_steps; ++at) {
+        const int head = cur.head, tile = cur.tile;
+        if (at == 0 || cur.pg == 0) {
             // ---- a unit begins: its query rows
             whole = cur.pg == 0;
-            fresh = true;
             const int n_rows = cur.q.new_ * p.group, t0 = min(max(p.cu[cur.s], 0), p.n_tokens), first = cur.q.total - cur.q.new_;
             auto split = [&](int r, int& i, int& h) {
                 i = p.group_shift >= 0 ? r >> p.group_shift : r / p.group;
@@ -301,7 +340,7 @@ __global__ void __launch_bounds__(THREADS) page_attn_kernel(const __grid_constan
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
                         const float2 f = xsv_unpack2<T>(word(raw[k], w));
-                        qf[n][2 * k + (w >> 1)][w & 1] = pack_h2(f.x * s1 * s2, f.y * s1 * s2);
+                        qf[n][k][w & 1][w >> 1] = pack_h2(f.x * s1 * s2, f.y * s1 * s2);
                     }
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
@@ -311,7 +350,7 @@ __global__ void __launch_bounds__(THREADS) page_attn_kernel(const __grid_constan
                     int i, h;
                     split(row, i, h);
                     qpos[n][c] = row < n_rows ? first + i : -1;
-                    m[n][c] = -INFINITY;
+                    m[n][c] = NO_MAX;
                     l[n][c] = 0.f;
 #pragma unroll
                     for (int v = 0; v < VG; ++v) zs[n][c][v] = 0.f;
@@ -333,27 +372,30 @@ __global__ void __launch_bounds__(THREADS) page_attn_kernel(const __grid_constan
         }
         __syncwarp();
         const uint8_t* rec = ring + stage * R::BYTES;
-        const int page = stage_page[wid][stage], pg = cur.q.p0 + cur.pg, tok0 = pg * XSV_PAGE;
-        if (page >= 0 && !failed) {
+        const int pg = cur.q.p0 + cur.pg, tok0 = pg * XSV_PAGE;
+        if (stage_page[wid][stage] && !failed) {
+            float up_lo, up_hi;                                    // what brings the value products' rows g, g + 8 to real units
             const bool part = tok0 + XSV_PAGE > cur.q.total;
             const bool mask = tok0 + XSV_PAGE - 1 > pos_lo || part || (p.window > 0 && tok0 <= pos_hi - p.window);
-            float s[NT][4][4];
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[n][t][i] = 0.f;
+            // logits (in log2 units) are s * f + z, f by row half (i / 2) and column (i % 2)
+            float s[NT][4][4], f[NT][4], z[NT][2];
             if (!part) {
-                float qz[NT][4];
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) qz[n][i] = 0.f;
+                // q . z and, below it, what the rounding of q s leaves out (exact) times the middle code, 8, so that the error
+                // that stays is that of the codes around their middle
+                float qz[NT][3][4];
 #pragma unroll
                 for (int k = 0; k < D / 32; ++k) {
                     const uint4 sc = *reinterpret_cast<const uint4*>(rec + R::K_SCALE + 64 * k + 16 * j);
                     const uint4 ze = *reinterpret_cast<const uint4*>(rec + R::K_ZERO + 64 * k + 16 * j);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            // the offsets as they lie in memory: words 0, 2 on rows g are the first operand register's channels
+                            // of both steps, words 1, 3 on rows g + 8 the second's; each product counts on its rows only
+                            if (k == 0) mma0(qz[n][h], ze.x, ze.y, ze.z, ze.w, qf[n][k][h][0], qf[n][k][h][1]);
+                            else mma(qz[n][h], ze.x, ze.y, ze.z, ze.w, qf[n][k][h][0], qf[n][k][h][1]);
+                        }
 #pragma unroll
                     for (int kl = 0; kl < 2; ++kl) {
                         const int ks = 2 * k + kl;
@@ -361,30 +403,30 @@ __global__ void __launch_bounds__(THREADS) page_attn_kernel(const __grid_constan
                         uint32_t b0[NT], b1[NT];
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            b0[n] = hmul2_u(qf[n][ks][0], word(sc, 2 * kl));
-                            b1[n] = hmul2_u(qf[n][ks][1], word(sc, 2 * kl + 1));
-                            mma(qz[n], word(ze, 2 * kl), word(ze, 2 * kl), word(ze, 2 * kl + 1), word(ze, 2 * kl + 1), qf[n][ks][0], qf[n][ks][1]);
+                            b0[n] = hmul2_u(qf[n][k][0][kl], word(sc, 2 * kl));
+                            b1[n] = hmul2_u(qf[n][k][1][kl], word(sc, 2 * kl + 1));
+                            const uint32_t e0 = hfnma2_u(qf[n][k][0][kl], word(sc, 2 * kl), b0[n]), e1 = hfnma2_u(qf[n][k][1][kl], word(sc, 2 * kl + 1), b1[n]);
+                            if (ks == 0) mma0(qz[n][2], MINUS_EIGHTS, MINUS_EIGHTS, MINUS_EIGHTS, MINUS_EIGHTS, e0, e1);
+                            else mma(qz[n][2], MINUS_EIGHTS, MINUS_EIGHTS, MINUS_EIGHTS, MINUS_EIGHTS, e0, e1);
                         }
 #pragma unroll
                         for (int t = 0; t < 4; ++t) {
                             const uint32_t w = word(code, t), v = w >> 8;
 #pragma unroll
-                            for (int n = 0; n < NT; ++n)
-                                mma(s[n][t], w & 0x000F000Fu, w & 0x00F000F0u, v & 0x000F000Fu, v & 0x00F000F0u, b0[n], b1[n]);
+                            for (int n = 0; n < NT; ++n) {
+                                if (ks == 0) mma0(s[n][t], w & 0x000F000Fu, w & 0x00F000F0u, v & 0x000F000Fu, v & 0x00F000F0u, b0[n], b1[n]);
+                                else mma(s[n][t], w & 0x000F000Fu, w & 0x00F000F0u, v & 0x000F000Fu, v & 0x00F000F0u, b0[n], b1[n]);
+                            }
                         }
                     }
                 }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    const float z0 = qz[n][0] * fac[n][0], z1 = qz[n][1] * fac[n][1];
-                    const float lo0 = fac[n][0] * 16777216.f, lo1 = fac[n][1] * 16777216.f;      // 2^24: row g
-                    const float hi0 = fac[n][0] * 1048576.f, hi1 = fac[n][1] * 1048576.f;        // 2^20: row g + 8
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        s[n][t][0] = fmaf(s[n][t][0], lo0, z0);
-                        s[n][t][1] = fmaf(s[n][t][1], lo1, z1);
-                        s[n][t][2] = fmaf(s[n][t][2], hi0, z0);
-                        s[n][t][3] = fmaf(s[n][t][3], hi1, z1);
+                    for (int c = 0; c < 2; ++c) {
+                        z[n][c] = (qz[n][0][c] + qz[n][1][c + 2] + qz[n][2][c]) * fac[n][c];
+                        f[n][c] = fac[n][c] * 16777216.f;          // 2^24: rows g
+                        f[n][c + 2] = fac[n][c] * 1048576.f;       // 2^20: rows g + 8
                     }
                 }
             } else {
@@ -392,6 +434,10 @@ __global__ void __launch_bounds__(THREADS) page_attn_kernel(const __grid_constan
                 const int held = cur.q.total - tok0;
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) s[n][t][i] = 0.f;
                     if (16 * t < held) {
 #pragma unroll
                         for (int k = 0; k < D / 32; ++k) {
@@ -402,14 +448,14 @@ __global__ void __launch_bounds__(THREADS) page_attn_kernel(const __grid_constan
 #pragma unroll
                                 for (int n = 0; n < NT; ++n)
                                     mma(s[n][t], to_h2<T>(word(a, 2 * kl)), to_h2<T>(word(b, 2 * kl)), to_h2<T>(word(a, 2 * kl + 1)),
-                                        to_h2<T>(word(b, 2 * kl + 1)), qf[n][2 * k + kl][0], qf[n][2 * k + kl][1]);
+                                        to_h2<T>(word(b, 2 * kl + 1)), qf[n][k][0][kl], qf[n][k][1][kl]);
                         }
                     }
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) s[n][t][i] *= fac[n][i & 1];
                 }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) { z[n][c] = 0.f; f[n][c] = f[n][c + 2] = fac[n][c]; }
             }
             if (mask) {
 #pragma unroll
@@ -423,127 +469,172 @@ __global__ void __launch_bounds__(THREADS) page_attn_kernel(const __grid_constan
                             if (!seen) s[n][t][i] = -INFINITY;     // whatever stood there, NaN included
                         }
             }
-            // ---- value parameters of the lane's tokens 8 i + g; the running power of two
-            uint4 vsc[VG], vze[VG];
-            uint32_t top = 0;
-#pragma unroll
-            for (int v = 0; v < VG; ++v) {
-                vsc[v] = *reinterpret_cast<const uint4*>(rec + R::V_SCALE + 128 * v + 16 * g);
-                vze[v] = *reinterpret_cast<const uint4*>(rec + R::V_ZERO + 128 * v + 16 * g);
-                if (part) {                                        // places that hold no token: no bits of theirs count
-                    uint32_t keep[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int a = tok0 + 16 * i + g;
-                        keep[i] = (a < cur.q.total ? 0xFFFFu : 0u) | (a + 8 < cur.q.total ? 0xFFFF0000u : 0u);
-                    }
-                    vsc[v] = make_uint4(vsc[v].x & keep[0], vsc[v].y & keep[1], vsc[v].z & keep[2], vsc[v].w & keep[3]);
-                    vze[v] = make_uint4(vze[v].x & keep[0], vze[v].y & keep[1], vze[v].z & keep[2], vze[v].w & keep[3]);
-                }
-                top = __vmaxu2(top, __vmaxu2(__vmaxu2(vsc[v].x, vsc[v].y), __vmaxu2(vsc[v].z, vsc[v].w)));
-            }
-            top = max(top >> 16, top & 0xFFFFu);                   // scales are positive: their order is that of their bits
-            top = __reduce_max_sync(0xFFFFFFFFu, top);
-            // exponent of the largest scale (fp16 bits; 2^(field - 15), subnormals counted as 2^-14): P s <= 2^14
-            const int e_page = (int)(max(top, 0x0400u) >> 10) - 15 - 13;
-            bool raise = fresh || e_page > e_run;
-            // ---- running maximum
-            float mn[NT][2];
+            // ---- maximum: looked for only when a logit exceeds the one in use
+            float xm[NT][2];
+            bool raise = false;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    float x = fmaxf(fmaxf(fmaxf(s[n][0][c], s[n][0][c + 2]), fmaxf(s[n][1][c], s[n][1][c + 2])),
-                                    fmaxf(fmaxf(s[n][2][c], s[n][2][c + 2]), fmaxf(s[n][3][c], s[n][3][c + 2])));
-                    x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 4));
-                    x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 8));
-                    x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 16));
-                    mn[n][c] = fmaxf(m[n][c], x);
-                    raise = raise || mn[n][c] > m[n][c];
+                    const float lo = fmaxf(fmaxf(s[n][0][c], s[n][1][c]), fmaxf(s[n][2][c], s[n][3][c]));
+                    const float hi = fmaxf(fmaxf(s[n][0][c + 2], s[n][1][c + 2]), fmaxf(s[n][2][c + 2], s[n][3][c + 2]));
+                    xm[n][c] = fmaxf(lo * f[n][c], hi * f[n][c + 2]) + z[n][c];
+                    raise = raise || xm[n][c] > m[n][c] + P_SLACK;
                 }
             if (__any_sync(0xFFFFFFFFu, raise)) {
-                const int e_new = fresh ? e_page : max(e_run, e_page);
-                const float down = fresh ? 1.f : pow2i(e_run - e_new);
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        const float a = m[n][c] == -INFINITY ? 0.f : ex2(m[n][c] - mn[n][c]);
-                        m[n][c] = mn[n][c];
+                        float x = xm[n][c];
+                        x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 4));
+                        x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 8));
+                        x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 16));
+                        x = fmaxf(x, m[n][c]);
+                        const float a = ex2(m[n][c] - x);
+                        m[n][c] = x;
                         l[n][c] *= a;
 #pragma unroll
                         for (int v = 0; v < VG; ++v) zs[n][c][v] *= a;
 #pragma unroll
-                        for (int ct = 0; ct < CT; ++ct) { o[n][ct][c] *= a * down; o[n][ct][c + 2] *= a * down; }
+                        for (int ct = 0; ct < CT; ++ct) { o[n][ct][c] *= a; o[n][ct][c + 2] *= a; }
                     }
-                e_run = e_new;
-                fresh = false;
             }
-            const float unit = pow2i(-e_run);
-            // ---- probabilities, scaled by the tokens' value scales, and the product with the value codes
+            // ---- probabilities, as the products' second operand: tokens 16 t + {2 j, 2 j + 1} (+ 8), row g
+            uint32_t b[4][NT][2];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                float sc[VG][2], ze[VG][2];
+            for (int n = 0; n < NT; ++n) {
+                const float off0 = z[n][0] - m[n][0] + P_BIAS, off1 = z[n][1] - m[n][1] + P_BIAS;
 #pragma unroll
-                for (int v = 0; v < VG; ++v)
+                for (int t = 0; t < 4; ++t) {
+                    b[t][n][0] = transpose8(pack_h2(ex2(fmaf(s[n][t][0], f[n][0], off0)), ex2(fmaf(s[n][t][1], f[n][1], off1))));
+                    b[t][n][1] = transpose8(pack_h2(ex2(fmaf(s[n][t][2], f[n][2], off0)), ex2(fmaf(s[n][t][3], f[n][3], off1))));
+                }
+            }
+            // ---- value scales of the same tokens in pairs; sum of p (z + 8 s) per 64 channels, and sum of p, as products too
+            uint32_t sp[VG][8];
+            {
+                uint32_t top = 0;
+                float sum[2][NT][4];
+                uint32_t zp[VG][8];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        sc[v][h] = half_at(vsc[v], 2 * t + h) * unit;
-                        ze[v][h] = half_at(vze[v], 2 * t + h);
+                for (int v = 0; v < VG; ++v) {
+                    const uint8_t* at_s = rec + R::V_SCALE + 128 * v + 32 * j;
+                    const uint8_t* at_z = rec + R::V_ZERO + 128 * v + 32 * j;
+                    const uint4 s0 = *reinterpret_cast<const uint4*>(at_s), s1 = *reinterpret_cast<const uint4*>(at_s + 16);
+                    const uint4 z0 = *reinterpret_cast<const uint4*>(at_z), z1 = *reinterpret_cast<const uint4*>(at_z + 16);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        sp[v][i] = pair_at(s0, s1, i);
+                        zp[v][i] = pair_at(z0, z1, i);
                     }
-                uint32_t b[NT][VG][2];
+                }
+                if (part) {                                        // places that hold no token: no bits of theirs count
+                    asm volatile("" ::: "memory");                 // a branch: as predicated code it would cost every page
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    float pr[4];
+                    for (int i = 0; i < 8; ++i) {
+                        const int a = cur.q.total - tok0 - 2 * j - 8 * i;
+                        const uint32_t keep = a >= 2 ? 0xFFFFFFFFu : a == 1 ? 0xFFFFu : 0u;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float mc = m[n][i & 1];
-                        pr[i] = ex2(s[n][t][i] - (mc == -INFINITY ? 0.f : mc));
-                    }
-                    l[n][0] += pr[0] + pr[2];
-                    l[n][1] += pr[1] + pr[3];
-#pragma unroll
-                    for (int v = 0; v < VG; ++v) {
-                        zs[n][0][v] = fmaf(pr[0], ze[v][0], fmaf(pr[2], ze[v][1], zs[n][0][v]));
-                        zs[n][1][v] = fmaf(pr[1], ze[v][0], fmaf(pr[3], ze[v][1], zs[n][1][v]));
-                        b[n][v][0] = transpose8(pack_h2(pr[0] * sc[v][0], pr[1] * sc[v][0]));
-                        b[n][v][1] = transpose8(pack_h2(pr[2] * sc[v][1], pr[3] * sc[v][1]));
+                        for (int v = 0; v < VG; ++v) { sp[v][i] &= keep; zp[v][i] &= keep; }
                     }
                 }
 #pragma unroll
-                for (int v = 0; v < VG; ++v) {
+                for (int v = 0; v < VG; ++v)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        zp[v][i] = hfma2_u(sp[v][i], EIGHTS, zp[v][i]);
+                        top = __vmaxu2(top, sp[v][i]);
+                    }
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        // rows g: the first 64 channels; rows g + 8: the second, or the sum of p
+                        const uint32_t h0 = VG == 2 ? zp[VG - 1][2 * t] : ONES, h1 = VG == 2 ? zp[VG - 1][2 * t + 1] : ONES;
+                        if (t == 0) mma0(sum[0][n], zp[0][0], h0, zp[0][1], h1, b[0][n][0], b[0][n][1]);
+                        else mma(sum[0][n], zp[0][2 * t], h0, zp[0][2 * t + 1], h1, b[t][n][0], b[t][n][1]);
+                        if (VG == 2) {
+                            if (t == 0) mma0(sum[1][n], ONES, ONES, ONES, ONES, b[0][n][0], b[0][n][1]);
+                            else mma(sum[1][n], ONES, ONES, ONES, ONES, b[t][n][0], b[t][n][1]);
+                        }
+                    }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        zs[n][c][0] += sum[0][n][c];
+                        if (VG == 2) zs[n][c][VG - 1] += sum[0][n][c + 2];
+                        l[n][c] += VG == 2 ? sum[1][n][c] : sum[0][n][c + 2];
+                    }
+                // Scales beyond 16, or all below 2^-8, are brought to [8, 16) by a power of two (of their bits: they are positive)
+                top = __reduce_max_sync(0xFFFFFFFFu, max(top >> 16, top & 0xFFFFu));
+                int e = 0;
+                if (top > 0x4C00u || top < 0x1C00u) {
+                    e = max((int)(top >> 10) - 18, -15);
+                    const uint32_t h = (uint32_t)(15 - e) << 10, down = h | h << 16;
+#pragma unroll
+                    for (int v = 0; v < VG; ++v)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) sp[v][i] = hmul2_u(sp[v][i], down);
+                }
+                up_lo = pow2i(24 + e);
+                up_hi = pow2i(20 + e);
+            }
+            // ---- times the value codes around their middle, 8: -8 sum P s, the same for all channels, starts the accumulators (and
+            // z + 8 s stands in for z above), so that neither the rounding of P s nor the tensor cores' truncating
+            // accumulation sees the codes' mean, which is much larger than what is left of it after sum p z.  For the same
+            // reason a page is summed in the tensor cores and the pages in float32 adds, which round (22 000 tokens in one
+            // accumulator, with the mean, were off by 0.6 %).
+#pragma unroll
+            for (int v = 0; v < VG; ++v) {
+                float acc[NT][4][4], mid[NT][4];
+                uint32_t ps[4][NT][2];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        ps[t][n][0] = hmul2_u(b[t][n][0], sp[v][2 * t]);
+                        ps[t][n][1] = hmul2_u(b[t][n][1], sp[v][2 * t + 1]);
+                        if (t == 0) mma0(mid[n], MINUS_LO, MINUS_HI, MINUS_LO, MINUS_HI, ps[0][n][0], ps[0][n][1]);
+                        else mma(mid[n], MINUS_LO, MINUS_HI, MINUS_LO, MINUS_HI, ps[t][n][0], ps[t][n][1]);
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
                     const uint4 code = *reinterpret_cast<const uint4*>(rec + R::V_CODES + ((t * VG + v) * 32 + lane) * 16);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const uint32_t w = word(code, i), x = w >> 8;
 #pragma unroll
-                        for (int n = 0; n < NT; ++n)
-                            mma(o[n][4 * v + i], w & 0x000F000Fu, w & 0x00F000F0u, x & 0x000F000Fu, x & 0x00F000F0u, b[n][v][0], b[n][v][1]);
+                        for (int n = 0; n < NT; ++n) {
+                            if (t == 0) mma(acc[n][i], w & 0x000F000Fu, w & 0x00F000F0u, x & 0x000F000Fu, x & 0x00F000F0u, ps[t][n][0], ps[t][n][1], mid[n]);
+                            else mma(acc[n][i], w & 0x000F000Fu, w & 0x00F000F0u, x & 0x000F000Fu, x & 0x00F000F0u, ps[t][n][0], ps[t][n][1]);
+                        }
                     }
                 }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) o[n][4 * v + i][c] = fmaf(acc[n][i][c], c < 2 ? up_lo : up_hi, o[n][4 * v + i][c]);
             }
         }
         if (++stage == STAGES) { stage = 0; parity ^= 1; }
 
         // ---- the unit, or this span's part of it, is done
         const bool ends = cur.pg + 1 == cur.q.pages;
-        if (ends || at + 1 == x1) {
-            const float up = fresh ? 0.f : pow2i(e_run);
+        if (ends || at + 1 == n_steps) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-#pragma unroll
-                    for (int x = 4; x < 32; x <<= 1) {
-                        l[n][c] += __shfl_xor_sync(0xFFFFFFFFu, l[n][c], x);
-#pragma unroll
-                        for (int v = 0; v < VG; ++v) zs[n][c][v] += __shfl_xor_sync(0xFFFFFFFFu, zs[n][c][v], x);
-                    }
                     if (failed) l[n][c] = NAN;
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct) {
-                        o[n][ct][c] = fmaf(o[n][ct][c] * 16777216.f, up, zs[n][c][ct / 4]);
-                        o[n][ct][c + 2] = fmaf(o[n][ct][c + 2] * 1048576.f, up, zs[n][c][ct / 4]);
+                        o[n][ct][c] += zs[n][c][ct / 4];
+                        o[n][ct][c + 2] += zs[n][c][ct / 4];
                     }
                 }
             if (whole && ends) {
@@ -577,77 +668,82 @@ __global__ void __launch_bounds__(THREADS) page_attn_kernel(const __grid_constan
                 }
             }
         }
-        if (at + 1 < x1) advance(p, cur, ROWS);
+        if (at + 1 < n_steps) advance(p, cur, ROWS);
     }
 }
 
-// Units that several warps share: parts in the order of the warps, one block per unit; a thread merges 4 values
-// (2 rows x 2 channels) over all parts.
+// Units that several warps share.  A block looks at 8 workers' descriptions and merges 16 channels of the units that
+// begin to be shared there: its 8 warps take the parts in turn, each lane 4 values (2 rows x 2 channels) of its parts,
+// and are merged in the order of the warps.
+constexpr int MERGE_WARPS = 8;
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(NT * D * 2) page_attn_merge_kernel(const __grid_constant__ Attn p) {
+__global__ void __launch_bounds__(MERGE_WARPS * 32) page_attn_merge_kernel(const __grid_constant__ Attn p, int workers) {
     constexpr int ROWS = 8 * NT, CT = D / 16, PF = Part<D, NT>::FLOATS;
-    __shared__ float s_max[ROWS];
+    __shared__ float4 s_o[MERGE_WARPS][32], s_ml[MERGE_WARPS][32];
     xsv_dep_release();
     xsv_dep_sync();
-    const int w = blockIdx.x + 1;
-    const int4 d = p.desc[w];
-    if (d.z == 0) return;
-    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-    auto part = [&](int i) { return p.part + (size_t)(i == 0 ? 2 * (w - 1) + 1 : 2 * (w + i - 1)) * PF; };
-    auto stats = [&](int i, int r) { return reinterpret_cast<const float2*>(part(i) + NT * CT * 128)[r]; };
-    for (int r = wid; r < ROWS; r += NT * D * 2 / 32) {
-        float mx = -INFINITY;
-        for (int i = lane; i < d.z; i += 32) mx = fmaxf(mx, stats(i, r).x);
-#pragma unroll
-        for (int x = 16; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, x));
-        if (lane == 0) s_max[r] = mx == -INFINITY ? 0.f : mx;
-    }
-    __syncthreads();
-    const Seq q = seq_of(p, d.x, ROWS);
-    const int tiles = q.units / p.pool.heads, head = d.y / tiles, tile = d.y - head * tiles;
-    const int n = tid / (CT * 32), ct = tid / 32 % CT, g = lane >> 2, j = lane & 3, r0 = 8 * n + 2 * j;
-    const float m0 = s_max[r0], m1 = s_max[r0 + 1];
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l0 = 0.f, l1 = 0.f;
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, n = blockIdx.y / CT, ct = blockIdx.y % CT;
+    const int g = lane >> 2, j = lane & 3, r0 = 8 * n + 2 * j;
+    struct Acc {
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f), ml = make_float4(NO_MAX, 0.f, NO_MAX, 0.f);
+        __device__ __forceinline__ void add(const float4& x, const float4& y) {      // y: maximum and sum of both rows
+            const float m0 = fmaxf(ml.x, y.x), m1 = fmaxf(ml.z, y.z);
+            const float a0 = ex2(ml.x - m0), b0 = ex2(y.x - m0), a1 = ex2(ml.z - m1), b1 = ex2(y.z - m1);
+            o.x = o.x * a0 + x.x * b0; o.z = o.z * a0 + x.z * b0;
+            o.y = o.y * a1 + x.y * b1; o.w = o.w * a1 + x.w * b1;
+            ml = make_float4(m0, ml.y * a0 + y.y * b0, m1, ml.w * a1 + y.w * b1);
+        }
+    };
+    const int w_end = min(workers, (int)(blockIdx.x + 1) * 8);
+    for (int w = max(1, (int)blockIdx.x * 8); w < w_end; ++w) {
+        const int4 d = p.desc[w];
+        if (d.w == 0) continue;                                 // the same for the whole block
+        Acc acc;
 #pragma unroll 4
-    for (int i = 0; i < d.z; ++i) {
-        const float4 x = reinterpret_cast<const float4*>(part(i))[tid];
-        const float4 ml = *reinterpret_cast<const float4*>(part(i) + NT * CT * 128 + 2 * r0);
-        const float a = ex2(ml.x - m0), b = ex2(ml.z - m1);
-        o.x = fmaf(x.x, a, o.x); o.y = fmaf(x.y, b, o.y); o.z = fmaf(x.z, a, o.z); o.w = fmaf(x.w, b, o.w);
-        l0 = fmaf(ml.y, a, l0); l1 = fmaf(ml.w, b, l1);
-    }
-    const int n_rows = q.new_ * p.group, t0 = min(max(p.cu[d.x], 0), p.n_tokens);
+        for (int i = wid; i < d.w; i += MERGE_WARPS) {
+            const float* part = p.part + (size_t)(i == 0 ? 2 * (w - 1) + 1 : 2 * (w + i - 1)) * PF;
+            acc.add(reinterpret_cast<const float4*>(part)[(n * CT + ct) * 32 + lane], *reinterpret_cast<const float4*>(part + NT * CT * 128 + 2 * r0));
+        }
+        __syncthreads();                                        // the last unit's reads of the shared arrays
+        s_o[wid][lane] = acc.o;
+        s_ml[wid][lane] = acc.ml;
+        __syncthreads();
+        if (wid != 0) continue;
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        const int r = tile * ROWS + r0 + c;
-        if (r >= n_rows) continue;
-        const int i = r / p.group, h = r - i * p.group;
-        const float l = c ? l1 : l0, inv = l == 0.f ? 0.f : 1.f / l;
-        T* dst = (T*)p.out + ((size_t)(t0 + i) * p.q_heads + head * p.group + h) * D + 64 * (ct / 4) + 8 * g + 2 * (ct % 4);
-        *reinterpret_cast<uint32_t*>(dst) = xsv_pack2<T>((c ? o.y : o.x) * inv, (c ? o.w : o.z) * inv);
+        for (int i = 1; i < MERGE_WARPS; ++i) acc.add(s_o[i][lane], s_ml[i][lane]);
+        const Seq q = seq_of(p, d.x, ROWS);
+        const int n_rows = q.new_ * p.group, t0 = min(max(p.cu[d.x], 0), p.n_tokens);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int r = d.z * ROWS + r0 + c;
+            if (r >= n_rows) continue;
+            const int i = r / p.group, h = r - i * p.group;
+            const float l = c ? acc.ml.w : acc.ml.y, inv = l == 0.f ? 0.f : 1.f / l;
+            T* dst = (T*)p.out + ((size_t)(t0 + i) * p.q_heads + d.y * p.group + h) * D + 64 * (ct / 4) + 8 * g + 2 * (ct % 4);
+            *reinterpret_cast<uint32_t*>(dst) = xsv_pack2<T>((c ? acc.o.y : acc.o.x) * inv, (c ? acc.o.w : acc.o.z) * inv);
+        }
     }
 }
 
 // ------------------------------------------------------------------ host side
-template <int D> constexpr int stages() { return 3; }
-template <int D> constexpr int blocks_per_sm() { return D == 64 ? 4 : 2; }
-template <int D> constexpr size_t ring_bytes() { return (size_t)WARPS * stages<D>() * PageRec<D>::BYTES; }
 constexpr size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 
-int grid_of(int head_dim) { return xsv_sm_count() * (head_dim == 64 ? blocks_per_sm<64>() : blocks_per_sm<128>()); }
+int grid_of(int head_dim, int nt) {
+    return xsv_sm_count() * (head_dim == 64 ? (nt == 1 ? Shape<64, 1>::BLOCKS : Shape<64, 2>::BLOCKS)
+                                            : (nt == 1 ? Shape<128, 1>::BLOCKS : Shape<128, 2>::BLOCKS));
+}
 // 8 query rows a tile where a head has no more, else 16
 int tiles_of(int max_new, int group) { return (long long)max_new * group <= 8 ? 1 : 2; }
 
 size_t workspace_of(int head_dim, int nt) {
-    const size_t workers = (size_t)grid_of(head_dim) * WARPS;
+    const size_t workers = (size_t)grid_of(head_dim, nt) * WARPS;
     const size_t pf = (size_t)nt * (head_dim / 16) * 128 + nt * 16;
     return align256(workers * sizeof(int4)) + 2 * workers * pf * sizeof(float);
 }
 
 template <typename T, int D, int NT> cudaError_t launch(Attn& p, cudaStream_t st) {
-    auto kernel = page_attn_kernel<T, D, NT, stages<D>()>;
-    constexpr size_t smem = ring_bytes<D>();
+    auto kernel = page_attn_kernel<T, D, NT>;
+    constexpr size_t smem = Shape<D, NT>::SMEM;
     static XsvPerDeviceInt ready;
     const int dev = xsv_current_device();
     if (!ready.get(dev)) {
@@ -655,11 +751,11 @@ template <typename T, int D, int NT> cudaError_t launch(Attn& p, cudaStream_t st
         if (e != cudaSuccess) return e;
         ready.set(dev, 1);
     }
-    const int grid = grid_of(D);
+    const int grid = grid_of(D, NT);
     cudaError_t e = xsv_launch_dep(kernel, dim3(grid), dim3(THREADS), smem, st, p);
     if (e != cudaSuccess) return e;
     xsv_count_launch(1);
-    e = xsv_launch_dep(page_attn_merge_kernel<T, D, NT>, dim3(grid * WARPS - 1), dim3(NT * D * 2), 0, st, p);
+    e = xsv_launch_dep(page_attn_merge_kernel<T, D, NT>, dim3((grid * WARPS + 7) / 8, NT * (D / 16)), dim3(MERGE_WARPS * 32), 0, st, p, grid * WARPS);
     if (e == cudaSuccess) xsv_count_launch(1);
     return e;
 }
@@ -697,7 +793,7 @@ extern "C" xsv_status xsv_page_attention(const xsv_page_pool* pool, const void* 
     if (workspace_bytes < workspace_of(pool->head_dim, nt)) return XSV_ERR_ARG;
     p.Q = Q; p.out = out; p.table = block_table; p.cu = cu_new; p.total = total_len; p.q_stride = q_stride;
     p.desc = (int4*)workspace;
-    p.part = (float*)((char*)workspace + align256((size_t)grid_of(pool->head_dim) * WARPS * sizeof(int4)));
+    p.part = (float*)((char*)workspace + align256((size_t)grid_of(pool->head_dim, nt) * WARPS * sizeof(int4)));
     p.scale = scale * 1.4426950408889634f;
     p.width = table_width; p.n_seqs = n_seqs; p.n_tokens = n_tokens; p.q_heads = q_heads; p.group = group; p.max_new = max_new;
     p.window = window;

@@ -63,4 +63,26 @@ __device__ __forceinline__ void page_params(float mn, float mx, __half& s, __hal
     s = __float2half_ru(__fdiv_ru(__fsub_ru(mx, __half2float(z)), 15.f));
     if (__half2float(s) == 0.f) s = __float2half_rn(1.f);
 }
+// Codes of x in a group with these parameters: nearest-even of the IEEE quotient (x - z) / s.  Outward rounding keeps the
+// quotient inside [0, 15 + 2^-19], so no clamping is needed.  code_bits() gives float bits whose low four are the code
+// (1.5 * 2^23 + code), from (x - z) * (1 / s), which is within 2^-19 of the quotient, and keeps in `near` the largest distance
+// to an integer that it met: where that exceeds CODE_NEAR, a quotient may lie on the other side of a half-integer
+// and code_bits_exact(), which divides, has to be asked.
+constexpr float CODE_NEAR = 0.49998f;                       // 0.5 - 2^-16 and a little
+__device__ __forceinline__ uint32_t code_bits(float x, float inv_s, float z, float& near) {
+    const float y = __fmul_rn(__fsub_rn(x, z), inv_s), t = __fadd_rn(y, 12582912.f);
+    near = fmaxf(near, fabsf(__fsub_rn(y, __fadd_rn(t, -12582912.f))));
+    return __float_as_uint(t);
+}
+__device__ __forceinline__ uint32_t code_bits_exact(float x, float s, float z) {
+    return __float_as_uint(__fadd_rn(__fdiv_rn(__fsub_rn(x, z), s), 12582912.f));
+}
+constexpr uint32_t CODE_BASE = 0x4B400000u;                 // the bits of 1.5 * 2^23
+// minimum and maximum of pairs of 16-bit values
+template <typename T> __device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b);
+template <typename T> __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b);
+template <> __device__ __forceinline__ uint32_t min2<__half>(uint32_t a, uint32_t b) { uint32_t d; asm("min.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b)); return d; }
+template <> __device__ __forceinline__ uint32_t max2<__half>(uint32_t a, uint32_t b) { uint32_t d; asm("max.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b)); return d; }
+template <> __device__ __forceinline__ uint32_t min2<__nv_bfloat16>(uint32_t a, uint32_t b) { uint32_t d; asm("min.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b)); return d; }
+template <> __device__ __forceinline__ uint32_t max2<__nv_bfloat16>(uint32_t a, uint32_t b) { uint32_t d; asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b)); return d; }
 __device__ __forceinline__ float clamp_half(float x) { return fminf(fmaxf(x, -65504.f), 65504.f); }

@@ -5,13 +5,16 @@
 // Bound by HBM: 2 bytes read and 2 written per element, about 10 float32 operations.  A head's row is held by d / 8
 // lanes, 8 channels each as two 8-byte pieces that are partners in the rotation (for half-split and 2-D rotation the
 // pieces lie half a rotated span apart), so the rotation needs no exchange between lanes; the norm's sum takes
-// log2(d / 8) shuffles.  A block serves one token: its first threads compute the token's cosines and sines once, in
+// log2(d / 8) shuffles.  A block walks through tokens: its first threads compute a token's cosines and sines once, in
 // shared memory, for all its heads; each lane group has two rows in flight.  With few tokens a token's heads are
 // spread over several blocks (a row per lane group), which trades repeated sines for latency.
 //
 // Angles: position * inv_freq in turns as a float64 product, its fraction in float32: a float32 angle of a position
 // near 10^6 would be off by 0.03 rad.  Norms are float32, the layer norm's variance from differences to the mean (two
 // passes over registers); results are rounded once, to the output type.
+#include <algorithm>
+#include <type_traits>
+
 #include "../../include/xsv.h"
 #include "page_layout.cuh"
 #include "xsv_kernels.h"
@@ -32,36 +35,22 @@ struct NormRope {
     int n_tokens, n_rot;     // n_rot: channels rotated (0: none)
 };
 
-template <typename T> __device__ __forceinline__ void load4(const T* p, float (&o)[4]) {
-    const uint2 w = *reinterpret_cast<const uint2*>(p);
+template <typename T> __device__ __forceinline__ void unpack4(const uint2& w, float* o) {
     const float2 a = xsv_unpack2<T>(w.x), b = xsv_unpack2<T>(w.y);
     o[0] = a.x; o[1] = a.y; o[2] = b.x; o[3] = b.y;
 }
 
-template <typename T, int D, int ROPE>
-__global__ void __launch_bounds__(128) qk_norm_rope_kernel(const __grid_constant__ NormRope p, int norm, int rows_per_group) {
-    constexpr int L = D / 8, GROUPS = 128 / L;
-    __shared__ float2 cs[D / 2];
+constexpr int THREADS = 128;
+
+template <typename T, int D, int ROPE, int NORM>
+__global__ void __launch_bounds__(THREADS, 8) qk_norm_rope_kernel(const __grid_constant__ NormRope p) {
+    constexpr int L = D / 8, GROUPS = THREADS / L;
+    __shared__ float2 cs[2][D / 2];
     xsv_dep_release();
-    xsv_dep_sync();
-    const int t = blockIdx.x, lane = threadIdx.x % L, group = threadIdx.x / L;
-    if (ROPE != XSV_ROPE_NONE) {
-        // frequency f of the token: a span of n_rot channels for one position, two half-width spans for two
-        const int n = p.n_rot / 2;
-        if ((int)threadIdx.x < n) {
-            const int per = ROPE == XSV_ROPE_2D ? n / 2 : n, f = threadIdx.x % per;
-            const int at = ROPE == XSV_ROPE_2D ? p.pos[2 * (size_t)t + threadIdx.x / per] : p.pos[t];
-            double turns = (double)at * (double)p.inv_freq[f] * 0.15915494309189533577;
-            turns -= rint(turns);
-            float s, c;
-            sincospif(2.f * (float)turns, &s, &c);
-            cs[threadIdx.x] = make_float2(c, s);
-        }
-        __syncthreads();
-    }
+    const int lane = threadIdx.x % L, group = threadIdx.x / L;
     // the lane's two pieces of four channels, and the index of the first frequency of each pair it rotates
-    int ca, cb, f;
-    bool rot;
+    int ca, cb, f = 0;
+    bool rot = false;
     if (ROPE == XSV_ROPE_PAIRS || ROPE == XSV_ROPE_NONE) {
         ca = 8 * lane; cb = ca + 4; f = 4 * lane; rot = ROPE != XSV_ROPE_NONE && ca < p.n_rot;
     } else {
@@ -72,108 +61,135 @@ __global__ void __launch_bounds__(128) qk_norm_rope_kernel(const __grid_constant
         cb = rot ? ca + half : ca + 4;
         f = part * half + 4 * i;
     }
-    float w[2][8], b[2][8];
+    xsv_dep_sync();
+    uint2 wgt[2][2], bias[2][2];                            // [q, k][piece], 16-bit
+    if (NORM != XSV_NORM_NONE) {
+        const uint32_t one = xsv_pack2<T>(1.f, 1.f);
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) { w[s][i] = 1.f; b[s][i] = 0.f; }
-        if (norm != XSV_NORM_NONE && p.w[s]) {
-            load4<T>((const T*)p.w[s] + ca, reinterpret_cast<float(&)[4]>(w[s][0]));
-            load4<T>((const T*)p.w[s] + cb, reinterpret_cast<float(&)[4]>(w[s][4]));
-        }
-        if (norm != XSV_NORM_NONE && p.b[s]) {
-            load4<T>((const T*)p.b[s] + ca, reinterpret_cast<float(&)[4]>(b[s][0]));
-            load4<T>((const T*)p.b[s] + cb, reinterpret_cast<float(&)[4]>(b[s][4]));
+        for (int s = 0; s < 2; ++s) {
+            wgt[s][0] = wgt[s][1] = make_uint2(one, one);
+            bias[s][0] = bias[s][1] = make_uint2(0u, 0u);
+            if (p.w[s]) {
+                wgt[s][0] = *reinterpret_cast<const uint2*>((const T*)p.w[s] + ca);
+                wgt[s][1] = *reinterpret_cast<const uint2*>((const T*)p.w[s] + cb);
+            }
+            if (p.b[s]) {
+                bias[s][0] = *reinterpret_cast<const uint2*>((const T*)p.b[s] + ca);
+                bias[s][1] = *reinterpret_cast<const uint2*>((const T*)p.b[s] + cb);
+            }
         }
     }
-    float2 r[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = rot ? cs[f + i] : make_float2(1.f, 0.f);
-
-    const int hq = p.heads[0], hk = hq + p.heads[1], hall = hk + p.heads[2];
-    const int first = (blockIdx.y * rows_per_group) * GROUPS + group;
-    auto locate = [&](int h, int& part, int& head) {
-        part = h < hq ? 0 : h < hk ? 1 : 2;
-        head = h - (part == 0 ? 0 : part == 1 ? hq : hk);
-    };
-    auto fetch = [&](int h, uint2& a, uint2& c) {
-        int part, head;
-        locate(h, part, head);
-        const T* src = (const T*)p.x[part] + (size_t)t * p.stride[part] + (size_t)head * D;
-        a = *reinterpret_cast<const uint2*>(src + ca);
-        c = *reinterpret_cast<const uint2*>(src + cb);
-    };
-    uint2 na = make_uint2(0, 0), nb = na;
-    if (first < hall) fetch(first, na, nb);
-    for (int k = 0; k < rows_per_group; ++k) {
-        const int h = first + k * GROUPS;
-        if (h - group >= hall) break;                       // the same for the whole block
-        const bool live = h < hall;
-        const uint2 a = na, c = nb;
-        if (k + 1 < rows_per_group && h + GROUPS < hall) fetch(h + GROUPS, na, nb);
-        int part = 0, head = 0;
-        locate(live ? h : 0, part, head);
-        uint2 oa = a, oc = c;
-        float v[8];
-        {
-            const float2 q0 = xsv_unpack2<T>(a.x), q1 = xsv_unpack2<T>(a.y), q2 = xsv_unpack2<T>(c.x), q3 = xsv_unpack2<T>(c.y);
-            v[0] = q0.x; v[1] = q0.y; v[2] = q1.x; v[3] = q1.y; v[4] = q2.x; v[5] = q2.y; v[6] = q3.x; v[7] = q3.y;
-        }
-        if (norm != XSV_NORM_NONE) {
-            // every lane of the warp takes part in the shuffles, whatever its row
-            float mean = 0.f;
-            if (norm == XSV_NORM_LAYER) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) mean += v[i];
-#pragma unroll
-                for (int o = L / 2; o > 0; o >>= 1) mean += __shfl_xor_sync(0xFFFFFFFFu, mean, o);
-                mean *= 1.f / D;
+    const int n_freq = p.n_rot / 2, h0 = blockIdx.y * GROUPS, step = gridDim.y * GROUPS;
+    int buf = 0;
+    for (int t = blockIdx.x; t < p.n_tokens; t += gridDim.x, buf ^= 1) {
+        float2 r[4];
+        if (ROPE != XSV_ROPE_NONE) {
+            if ((int)threadIdx.x < n_freq) {
+                const int per = ROPE == XSV_ROPE_2D ? n_freq / 2 : n_freq, i = threadIdx.x % per;
+                const int at = ROPE == XSV_ROPE_2D ? p.pos[2 * (size_t)t + threadIdx.x / per] : p.pos[t];
+                double turns = (double)at * (double)p.inv_freq[i] * 0.15915494309189533577;
+                turns -= rint(turns);
+                float s, c;
+                sincospif(2.f * (float)turns, &s, &c);
+                cs[buf][threadIdx.x] = make_float2(c, s);
             }
-            float ss = 0.f;
+            __syncthreads();                                // two buffers: the last token's are read before this one
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { v[i] -= mean; ss = fmaf(v[i], v[i], ss); }
-#pragma unroll
-            for (int o = L / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
-            const float inv = 1.f / sqrtf(ss * (1.f / D) + p.eps);
-            const int s = part == 1;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = fmaf(v[i] * inv, s ? w[1][i] : w[0][i], s ? b[1][i] : b[0][i]);
+            for (int i = 0; i < 4; ++i) r[i] = rot ? cs[buf][f + i] : make_float2(1.f, 0.f);
         }
-        if (part < 2) {
-            if (rot) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float& lo = ROPE == XSV_ROPE_PAIRS ? v[2 * i] : v[i];
-                    float& hi = ROPE == XSV_ROPE_PAIRS ? v[2 * i + 1] : v[4 + i];
-                    const float x0 = lo, x1 = hi;
-                    lo = x0 * r[i].x - x1 * r[i].y;
-                    hi = x1 * r[i].x + x0 * r[i].y;
+        for (int part = 0; part < 3; ++part) {
+            const int heads = p.heads[part];
+            if (h0 >= heads) continue;
+            const T* src = (const T*)p.x[part] + (size_t)t * p.stride[part];
+            T* dst = (T*)p.y[part] + (size_t)t * p.y_tok[part];
+            float w[8], b[8];
+            if (NORM != XSV_NORM_NONE && part < 2) {
+                unpack4<T>(wgt[part][0], w); unpack4<T>(wgt[part][1], w + 4);
+                unpack4<T>(bias[part][0], b); unpack4<T>(bias[part][1], b + 4);
+            }
+            // two rows of the group at a time; every lane of the warp takes part in the shuffles, whatever its row
+            for (int base = h0; base < heads; base += 2 * step) {
+                uint2 in[2][2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int h = base + u * step + group;
+                    in[u][0] = in[u][1] = make_uint2(0u, 0u);
+                    if (h < heads) {
+                        in[u][0] = *reinterpret_cast<const uint2*>(src + (size_t)h * D + ca);
+                        in[u][1] = *reinterpret_cast<const uint2*>(src + (size_t)h * D + cb);
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int h = base + u * step + group;
+                    if (base + u * step >= heads) break;    // the same for the whole block
+                    if (part < 2 && (NORM != XSV_NORM_NONE || ROPE != XSV_ROPE_NONE)) {
+                        float v[8];
+                        unpack4<T>(in[u][0], v);
+                        unpack4<T>(in[u][1], v + 4);
+                        if (NORM != XSV_NORM_NONE) {
+                            if (NORM == XSV_NORM_LAYER) {
+                                float mean = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+#pragma unroll
+                                for (int o = L / 2; o > 0; o >>= 1) mean += __shfl_xor_sync(0xFFFFFFFFu, mean, o);
+                                mean *= 1.f / D;
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) v[i] -= mean;
+                            }
+                            float ss = 0.f;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) ss = fmaf(v[i], v[i], ss);
+#pragma unroll
+                            for (int o = L / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
+                            const float inv = rsqrtf(ss * (1.f / D) + p.eps);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) v[i] = fmaf(v[i] * inv, w[i], b[i]);
+                        }
+                        if (ROPE != XSV_ROPE_NONE) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                float& lo = ROPE == XSV_ROPE_PAIRS ? v[2 * i] : v[i];
+                                float& hi = ROPE == XSV_ROPE_PAIRS ? v[2 * i + 1] : v[4 + i];
+                                const float x0 = lo, x1 = hi;
+                                lo = x0 * r[i].x - x1 * r[i].y;
+                                hi = x1 * r[i].x + x0 * r[i].y;
+                            }
+                        }
+                        in[u][0] = make_uint2(xsv_pack2<T>(v[0], v[1]), xsv_pack2<T>(v[2], v[3]));
+                        in[u][1] = make_uint2(xsv_pack2<T>(v[4], v[5]), xsv_pack2<T>(v[6], v[7]));
+                    }
+                    if (h < heads) {
+                        T* to = dst + (size_t)h * p.y_head[part];
+                        *reinterpret_cast<uint2*>(to + ca) = in[u][0];
+                        *reinterpret_cast<uint2*>(to + cb) = in[u][1];
+                    }
                 }
             }
-            oa = make_uint2(xsv_pack2<T>(v[0], v[1]), xsv_pack2<T>(v[2], v[3]));
-            oc = make_uint2(xsv_pack2<T>(v[4], v[5]), xsv_pack2<T>(v[6], v[7]));
-        }
-        if (live) {
-            T* dst = (T*)p.y[part] + (size_t)t * p.y_tok[part] + (size_t)head * p.y_head[part];
-            *reinterpret_cast<uint2*>(dst + ca) = oa;
-            *reinterpret_cast<uint2*>(dst + cb) = oc;
         }
     }
 }
 
 template <typename T, int D>
 cudaError_t launch(const NormRope& p, int norm, int rope, cudaStream_t st) {
-    const int groups = 128 / (D / 8), hall = p.heads[0] + p.heads[1] + p.heads[2];
-    const int each = (hall + groups - 1) / groups;          // rows per lane group if one block serves a token
-    // Below two blocks per multiprocessor the heads are spread over blocks as well.
-    const int rows = (long long)p.n_tokens >= 2LL * xsv_sm_count() ? each : 1;
-    const dim3 grid(p.n_tokens, (each + rows - 1) / rows);
-    auto go = [&](auto kernel) { return xsv_launch_dep(kernel, grid, dim3(128), 0, st, p, norm, rows); };
+    const int groups = THREADS / (D / 8), most = std::max(p.heads[0], std::max(p.heads[1], p.heads[2])), full = 8 * xsv_sm_count();
+    // With few tokens their heads are spread over several blocks as well, a row per lane group; with many a block walks
+    // through its share of them.
+    const dim3 grid(std::min(p.n_tokens, full), p.n_tokens >= 2 * xsv_sm_count() ? 1 : (most + groups - 1) / groups);
+    auto go = [&](auto kernel) { return xsv_launch_dep(kernel, grid, dim3(THREADS), 0, st, p); };
+    auto with = [&](auto rope_c) {
+        constexpr int ROPE = decltype(rope_c)::value;
+        switch (norm) {
+            case XSV_NORM_RMS: return go(qk_norm_rope_kernel<T, D, ROPE, XSV_NORM_RMS>);
+            case XSV_NORM_LAYER: return go(qk_norm_rope_kernel<T, D, ROPE, XSV_NORM_LAYER>);
+            default: return go(qk_norm_rope_kernel<T, D, ROPE, XSV_NORM_NONE>);
+        }
+    };
     switch (rope) {
-        case XSV_ROPE_HALF: return go(qk_norm_rope_kernel<T, D, XSV_ROPE_HALF>);
-        case XSV_ROPE_PAIRS: return go(qk_norm_rope_kernel<T, D, XSV_ROPE_PAIRS>);
-        case XSV_ROPE_2D: return go(qk_norm_rope_kernel<T, D, XSV_ROPE_2D>);
-        default: return go(qk_norm_rope_kernel<T, D, XSV_ROPE_NONE>);
+        case XSV_ROPE_HALF: return with(std::integral_constant<int, XSV_ROPE_HALF>{});
+        case XSV_ROPE_PAIRS: return with(std::integral_constant<int, XSV_ROPE_PAIRS>{});
+        case XSV_ROPE_2D: return with(std::integral_constant<int, XSV_ROPE_2D>{});
+        default: return with(std::integral_constant<int, XSV_ROPE_NONE>{});
     }
 }
 
