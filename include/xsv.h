@@ -527,7 +527,8 @@ xsv_status xsv_page_read(const xsv_page_pool* pool, const int* block_table, int 
  * Causal attention of the new tokens over what their sequences hold, themselves included (call it after the append):
  *   out[t][h] = softmax over positions j of the sequence, j <= position of t (and j > position - window if window > 0),
  *               of scale * q[t][h] . k[j][h / (q_heads / kv_heads)], times v[j].
- *   Q            : device, n_tokens rows of [q_heads][head_dim] at q_stride elements (a multiple of 8).
+ *   Q            : device, n_tokens rows of [q_heads][head_dim] at q_stride elements (a multiple of 8); magnitudes
+ *                  below 2^64.
  *   max_new      : at least the largest number of new tokens of a sequence (a host number; larger costs time only).
  *   scale        : positive, usually 1 / sqrt(head_dim).
  *   out          : [n_tokens][q_heads][head_dim], contiguous.  Rows behind cu_new[n_seqs] are left as they were; rows
@@ -543,7 +544,7 @@ xsv_status xsv_page_attention(const xsv_page_pool* pool, const void* Q, long lon
                               void* stream);
 
 /* Bytes of workspace that xsv_page_attention needs on the current device; 0 for arguments that it would refuse. */
-size_t xsv_page_attention_workspace(int n_seqs, int max_new, int q_heads, int kv_heads, int head_dim);
+size_t xsv_page_attention_workspace(int n_tokens, int n_seqs, int max_new, int q_heads, int kv_heads, int head_dim);
 
 /* Kernels launched by this library in the calling process since load (the paper has no counterpart). */
 long long xsv_kernel_launches(void);

@@ -59,7 +59,7 @@ SYMBOLS = {
     "xsv_page_append": (_i, [_vp, _vp, _vp, _ll, _ll, _i, _vp, _vp, _vp, _vp, _i, _vp]),
     "xsv_page_read": (_i, [_vp, _vp, _i, _vp, _i, _vp, _vp, _i, _vp, _vp, _vp]),
     "xsv_page_attention": (_i, [_vp, _vp, _ll, _i, _i, _vp, _i, _vp, _vp, _i, _i, C.c_float, _i, _vp, _vp, C.c_size_t, _vp]),
-    "xsv_page_attention_workspace": (C.c_size_t, [_i, _i, _i, _i, _i]),
+    "xsv_page_attention_workspace": (C.c_size_t, [_i, _i, _i, _i, _i, _i]),
     "xsv_kernel_launches": (_ll, []),
     "xsv_strerror": (C.c_char_p, [_i]),
     "xsv_last_cuda_error": (C.c_char_p, []),
@@ -490,7 +490,7 @@ def page_attention(Q, pages, k_tail, block_table, cu_new, total_len, max_new, *,
         n, heads, hkv, d = *Q.shape[:2], pool.kv_heads, pool.head_dim
         qp, qs = _rows(Q, "Q", k_tail.dtype, dev, (n, heads, d))
         to = out if out is not None else Q.new_empty((n, heads, d))
-        need = lib.xsv_page_attention_workspace(seqs, max_new, heads, hkv, d)
+        need = lib.xsv_page_attention_workspace(n, seqs, max_new, heads, hkv, d)
         space = pages.new_empty(need)
         _check(lib.xsv_page_attention(C.byref(pool), qp, qs, n, heads, _table(block_table, dev, seqs), block_table.shape[1],
                                       _tensor(cu_new, "cu_new", i32, dev, (seqs + 1,)), _tensor(total_len, "total_len", i32, dev, (seqs,)),

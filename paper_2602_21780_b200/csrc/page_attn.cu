@@ -24,31 +24,21 @@
 #include <cmath>
 
 #include "../../include/xsv.h"
-#include "page_layout.cuh"
+#include "page_attn.cuh"
+#include "tc5_ptx.cuh"
 #include "xsv_kernels.h"
 
 namespace {
 
 constexpr int WARPS = 4, THREADS = WARPS * 32;
-constexpr unsigned long long WAIT_LIMIT_NS = 2000000000ull;
 // Probabilities are 2^(x - m + P_BIAS) with m a logit that was the row's maximum when it was last looked for: as long as
 // none exceeds m by more than P_SLACK, m stays (one vote instead of a reduction and a rescale).  At most 2^10, they
 // keep fp16's full significand down to 2^-20 of the row's maximum; times a value scale of at most 16 they stay in range.
 constexpr float P_BIAS = 6.f, P_SLACK = 4.f, NO_MAX = -1e30f;
 
-struct Attn {
-    PoolView pool;
-    const void* Q;
-    void* out;
-    const int* table;
-    const int* cu;
-    const int* total;
+struct Attn : PageAttn {
     int4* desc;          // [workers] units that are shared: {sequence, head, tile, parts}; parts 0: none begins to be shared here
     float* part;         // [2 workers][slot] unnormalised rows
-    long long q_stride;
-    float scale;         // times log2 e
-    int width, n_seqs, n_tokens, q_heads, group, max_new, window;
-    int group_shift;     // log2 of group where it is a power of two, else -1
 };
 
 // one unnormalised tile: [NT][D / 16][32 lanes] float4, then maxima and sums [8 NT] float2
@@ -62,20 +52,8 @@ template <int D, int NT> struct Shape {
     static constexpr size_t SMEM = (size_t)WARPS * STAGES * PageRec<D>::BYTES;
 };
 
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ unsigned long long globaltimer() {
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    return t;
-}
-__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
 // Bounded: false once the limit has passed.
-__device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
+__device__ __noinline__ bool mbar_wait_bounded(uint32_t bar, uint32_t parity) {
     const unsigned long long t0 = globaltimer();
     while (globaltimer() - t0 < WAIT_LIMIT_NS)
         if (mbar_try(bar, parity)) return true;
@@ -101,29 +79,9 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t pack_h2(float a, float b) {   // saturating
-    uint32_t r;
-    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
-    return r;
-}
-template <typename T> __device__ __forceinline__ uint32_t to_h2(uint32_t w);
-template <> __device__ __forceinline__ uint32_t to_h2<__half>(uint32_t w) { return w; }
-template <> __device__ __forceinline__ uint32_t to_h2<__nv_bfloat16>(uint32_t w) {
-    return pack_h2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
-}
 __device__ __forceinline__ uint32_t hmul2_u(uint32_t a, uint32_t b) {
     uint32_t d;
     asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-__device__ __forceinline__ uint32_t hfma2_u(uint32_t a, uint32_t b, uint32_t c) {
-    uint32_t d;
-    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
     return d;
 }
 __device__ __forceinline__ uint32_t hfnma2_u(uint32_t a, uint32_t b, uint32_t c) {      // c - a b
@@ -144,14 +102,12 @@ __device__ __forceinline__ float pow2i(int e) {            // 2^e, clamped to wh
 // A sequence as the split sees it.
 struct Seq { int new_, total, p0, pages, tiles; };
 __device__ __forceinline__ Seq seq_of(const Attn& p, int s, int rows) {
-    Seq q;
-    const int a = min(max(p.cu[s], 0), p.n_tokens), b = min(max(p.cu[s + 1], a), p.n_tokens);
-    q.new_ = min(b - a, p.max_new);
-    q.total = (int)min((long long)max(p.total[s], 0), (long long)p.width * XSV_PAGE);
-    const int first = q.total - q.new_;                       // position of the first new token
-    q.p0 = p.window > 0 ? max(0, first - p.window + 1) / XSV_PAGE : 0;
-    q.pages = max(1, (q.total + XSV_PAGE - 1) / XSV_PAGE - q.p0);
-    q.tiles = (q.new_ * p.group + rows - 1) / rows;
+    const PageSeq x = page_seq(p, s);
+    Seq q{x.new_, x.total, 0, 0, 0};
+    q.p0 = p.window > 0 ? max(0, x.first - p.window + 1) / XSV_PAGE : 0;
+    q.pages = max(1, (x.total + XSV_PAGE - 1) / XSV_PAGE - q.p0);
+    const int n_rows = x.new_ * p.group;
+    q.tiles = n_rows > p.row_limit ? 0 : (n_rows + rows - 1) / rows;
     return q;
 }
 
@@ -297,15 +253,11 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
             // ---- a unit begins: its query rows
             whole = cur.pg == 0;
             const int n_rows = cur.q.new_ * p.group, t0 = min(max(p.cu[cur.s], 0), p.n_tokens), first = cur.q.total - cur.q.new_;
-            auto split = [&](int r, int& i, int& h) {
-                i = p.group_shift >= 0 ? r >> p.group_shift : r / p.group;
-                h = r - i * p.group;
-            };
             {
                 int i, h;
-                split(tile * ROWS, i, h);
+                page_row(p, tile * ROWS, i, h);
                 pos_lo = first + i;
-                split(min(n_rows, tile * ROWS + ROWS) - 1, i, h);
+                page_row(p, min(n_rows, tile * ROWS + ROWS) - 1, i, h);
                 pos_hi = first + i;
             }
 #pragma unroll
@@ -315,7 +267,7 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
                 float mx = 0.f;
                 if (r < n_rows) {
                     int i, h;
-                    split(r, i, h);
+                    page_row(p, r, i, h);
                     const T* row = (const T*)p.Q + (size_t)(t0 + i) * p.q_stride + (size_t)(head * p.group + h) * D + 8 * j;
 #pragma unroll
                     for (int k = 0; k < D / 32; ++k) raw[k] = *reinterpret_cast<const uint4*>(row + 32 * k);
@@ -348,7 +300,7 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
                     fac[n][c] = p.scale * pow2i(er);
                     const int row = tile * ROWS + 8 * n + 2 * j + c;
                     int i, h;
-                    split(row, i, h);
+                    page_row(p, row, i, h);
                     qpos[n][c] = row < n_rows ? first + i : -1;
                     m[n][c] = NO_MAX;
                     l[n][c] = 0.f;
@@ -365,9 +317,9 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
         __syncwarp();
         if (!failed) {
             issue(stage == 0 ? STAGES - 1 : stage - 1);        // the stage that the last step left
-            if (!mbar_try(smem_u32(&bars[wid][stage]), parity) && !mbar_wait_slow(smem_u32(&bars[wid][stage]), parity)) {
+            if (!mbar_try(smem_u32(&bars[wid][stage]), parity) && !mbar_wait_bounded(smem_u32(&bars[wid][stage]), parity)) {
                 failed = true;                                 // nothing is issued any more; what is in flight gets its time
-                for (int i = 0; i < STAGES; ++i) mbar_wait_slow(smem_u32(&bars[wid][(stage + i) % STAGES]), stage + i < STAGES ? parity : parity ^ 1);
+                for (int i = 0; i < STAGES; ++i) mbar_wait_bounded(smem_u32(&bars[wid][(stage + i) % STAGES]), stage + i < STAGES ? parity : parity ^ 1);
             }
         }
         __syncwarp();
@@ -735,10 +687,18 @@ int grid_of(int head_dim, int nt) {
 // 8 query rows a tile where a head has no more, else 16
 int tiles_of(int max_new, int group) { return (long long)max_new * group <= 8 ? 1 : 2; }
 
-size_t workspace_of(int head_dim, int nt) {
+// Sequences with more query rows a head go to the tensor-memory kernel.  A step of its 128-row tile costs about as much as
+// 3.4 steps of 16 rows here (frame of 1374 tokens on 21 984, 16 heads of 64: 788 us here), so 64 rows are where the
+// two meet.
+constexpr int FEW_ROWS = 64;
+bool many_rows(int max_new, int group) { return (long long)max_new * group > FEW_ROWS; }
+
+size_t workspace_of(int n_tokens, int n_seqs, int max_new, int group, int head_dim) {
+    const int nt = tiles_of(max_new, group);
     const size_t workers = (size_t)grid_of(head_dim, nt) * WARPS;
     const size_t pf = (size_t)nt * (head_dim / 16) * 128 + nt * 16;
-    return align256(workers * sizeof(int4)) + 2 * workers * pf * sizeof(float);
+    const size_t few = align256(workers * sizeof(int4)) + align256(2 * workers * pf * sizeof(float));
+    return few + (many_rows(max_new, group) ? xsv_page_tc5_workspace(n_tokens, n_seqs, group, head_dim) : 0);
 }
 
 template <typename T, int D, int NT> cudaError_t launch(Attn& p, cudaStream_t st) {
@@ -767,10 +727,10 @@ template <typename T> cudaError_t launch_any(Attn& p, int head_dim, int nt, cuda
 
 }  // namespace
 
-extern "C" size_t xsv_page_attention_workspace(int n_seqs, int max_new, int q_heads, int kv_heads, int head_dim) {
-    if (n_seqs <= 0 || n_seqs > XSV_PAGE_MAX_SEQS || max_new <= 0 || kv_heads <= 0 || q_heads < kv_heads || q_heads % kv_heads) return 0;
-    if (head_dim != 64 && head_dim != 128) return 0;
-    return workspace_of(head_dim, tiles_of(max_new, q_heads / kv_heads));
+extern "C" size_t xsv_page_attention_workspace(int n_tokens, int n_seqs, int max_new, int q_heads, int kv_heads, int head_dim) {
+    if (n_tokens <= 0 || n_seqs <= 0 || n_seqs > XSV_PAGE_MAX_SEQS || max_new <= 0) return 0;
+    if (kv_heads <= 0 || q_heads < kv_heads || q_heads % kv_heads || (head_dim != 64 && head_dim != 128)) return 0;
+    return workspace_of(n_tokens, n_seqs, std::min(max_new, n_tokens), q_heads / kv_heads, head_dim);
 }
 
 extern "C" xsv_status xsv_page_attention(const xsv_page_pool* pool, const void* Q, long long q_stride, int n_tokens, int q_heads,
@@ -790,16 +750,25 @@ extern "C" xsv_status xsv_page_attention(const xsv_page_pool* pool, const void* 
     if (((uintptr_t)Q | (uintptr_t)out | (uintptr_t)workspace) & 15 || q_stride & 7) return XSV_ERR_SHAPE;
     const int group = q_heads / pool->kv_heads, nt = tiles_of(max_new, group);
     if ((long long)max_new * group > 1LL << 30 || (long long)table_width * XSV_PAGE > 1LL << 30) return XSV_ERR_LIMIT;
-    if (workspace_bytes < workspace_of(pool->head_dim, nt)) return XSV_ERR_ARG;
+    if (workspace_bytes < workspace_of(n_tokens, n_seqs, max_new, group, pool->head_dim)) return XSV_ERR_ARG;
     p.Q = Q; p.out = out; p.table = block_table; p.cu = cu_new; p.total = total_len; p.q_stride = q_stride;
+    const size_t workers = (size_t)grid_of(pool->head_dim, nt) * WARPS, pf = (size_t)nt * (pool->head_dim / 16) * 128 + nt * 16;
     p.desc = (int4*)workspace;
-    p.part = (float*)((char*)workspace + align256((size_t)grid_of(pool->head_dim, nt) * WARPS * sizeof(int4)));
+    p.part = (float*)((char*)workspace + align256(workers * sizeof(int4)));
+    void* const more = (char*)p.part + align256(2 * workers * pf * sizeof(float));
     p.scale = scale * 1.4426950408889634f;
     p.width = table_width; p.n_seqs = n_seqs; p.n_tokens = n_tokens; p.q_heads = q_heads; p.group = group; p.max_new = max_new;
     p.window = window;
     p.group_shift = -1;
     for (int b = 0; b < 16; ++b) if (group == 1 << b) p.group_shift = b;
     cudaStream_t st = (cudaStream_t)stream;
-    const cudaError_t e = pool->dtype == XSV_F16 ? launch_any<__half>(p, pool->head_dim, nt, st) : launch_any<__nv_bfloat16>(p, pool->head_dim, nt, st);
+    cudaError_t e = cudaSuccess;
+    p.row_limit = 1 << 30;
+    if (many_rows(max_new, group)) {
+        p.row_limit = n_seqs == 1 ? 0 : FEW_ROWS;
+        e = xsv_launch_page_tc5(p, pool->dtype, pool->head_dim, more, st);
+    }
+    if (e == cudaSuccess && p.row_limit > 0)
+        e = pool->dtype == XSV_F16 ? launch_any<__half>(p, pool->head_dim, nt, st) : launch_any<__nv_bfloat16>(p, pool->head_dim, nt, st);
     return e == cudaSuccess ? XSV_OK : xsv_cuda_status(e);
 }

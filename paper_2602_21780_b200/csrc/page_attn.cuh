@@ -1,0 +1,37 @@
+// What the two attention kernels over pages share: the arguments, and a sequence as both split it.
+#pragma once
+#include "page_layout.cuh"
+
+struct PageAttn {
+    PoolView pool;
+    const void* Q;
+    void* out;
+    const int* table;
+    const int* cu;
+    const int* total;
+    long long q_stride;
+    float scale;         // times log2 e
+    int width, n_seqs, n_tokens, q_heads, group, max_new, window;
+    int group_shift;     // log2 of group where it is a power of two, else -1
+    int row_limit;       // sequences of at most so many query rows a head go to the kernel for few rows, the others to
+                         // the one for many
+};
+
+struct PageSeq { int new_, total, first; };     // first: position of the first new token
+__device__ __forceinline__ PageSeq page_seq(const PageAttn& p, int s) {
+    PageSeq q;
+    const int a = min(max(p.cu[s], 0), p.n_tokens), b = min(max(p.cu[s + 1], a), p.n_tokens);
+    q.new_ = min(b - a, p.max_new);
+    q.total = (int)min((long long)max(p.total[s], 0), (long long)p.width * XSV_PAGE);
+    q.first = q.total - q.new_;
+    return q;
+}
+// query row of a key/value head -> new token and query head of the group
+__device__ __forceinline__ void page_row(const PageAttn& p, int r, int& i, int& h) {
+    i = p.group_shift >= 0 ? r >> p.group_shift : r / p.group;
+    h = r - i * p.group;
+}
+
+// The kernel for many rows (page_attn_tc5.cu): work list, attention, merge.
+size_t xsv_page_tc5_workspace(int n_tokens, int n_seqs, int group, int head_dim);
+cudaError_t xsv_launch_page_tc5(const PageAttn& p, xsv_dtype dtype, int head_dim, void* workspace, cudaStream_t st);

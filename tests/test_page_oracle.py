@@ -100,8 +100,10 @@ def test_attention_arguments(bad, code):
 
 def test_attention_workspace_query():
     f = binding.load().xsv_page_attention_workspace
-    assert f(1, 1, 16, 16, 64) > 0 and f(64, 1, 32, 8, 128) > 0
-    for bad in ((0, 1, 4, 2, 64), (8193, 1, 4, 2, 64), (1, 0, 4, 2, 64), (1, 1, 3, 2, 64), (1, 1, 4, 0, 64), (1, 1, 4, 2, 96)):
+    assert f(1, 1, 1, 16, 16, 64) > 0 and f(64, 64, 1, 32, 8, 128) > 0
+    assert f(4000, 3, 2000, 32, 8, 128) > f(64, 64, 1, 32, 8, 128)
+    for bad in ((0, 1, 1, 4, 2, 64), (1, 0, 1, 4, 2, 64), (1, 8193, 1, 4, 2, 64), (1, 1, 0, 4, 2, 64), (1, 1, 1, 3, 2, 64), (1, 1, 1, 4, 0, 64),
+                (1, 1, 1, 4, 2, 96)):
         assert f(*bad) == 0
 
 
