@@ -184,7 +184,7 @@ struct Cta {
     uint32_t base, bars, tmem;
     volatile int* abort_flag;
     int* status;
-    volatile int* page_ok;       // [stages] whether the stage's page exists
+    uint32_t page_ok;            // [stages] ints: whether the stage's page exists
 };
 
 // ------------------------------------------------------------------ producers
@@ -199,6 +199,11 @@ __device__ __forceinline__ uint32_t pair_at(const uint4& a, const uint4& b, int 
 // the row of the key tile, and the column of S and the value tile, of token 16 m + 8 b + 2 j + h
 __host__ __device__ constexpr int place(int m, int b, int j, int h) { return 16 * j + 4 * m + 2 * b + h; }
 __host__ __device__ constexpr int token_at(int pos) { return 16 * (pos >> 2 & 3) + 8 * (pos >> 1 & 1) + 2 * (pos >> 4) + (pos & 1); }
+
+__device__ __forceinline__ uint4 ldg16(const uint8_t* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
+__device__ __forceinline__ void sts16(uint32_t at, const uint4& v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
 
 template <typename T, int D>
 __device__ __noinline__ void producer_loop(const PageAttn& p, const Work& w, const Cta c, Units u) {
@@ -219,7 +224,7 @@ __device__ __noinline__ void producer_loop(const PageAttn& p, const Work& w, con
             if (k - ids_from >= 32) {
                 ids_from = k & ~31;
                 const int pg = u.en.p0 + u.kv0 + ids_from + lane;
-                ids = ids_from + lane < n && pg < p.width && pg * XSV_PAGE < total ? row[ids_from + lane] : -1;
+                ids = ids_from + lane < n && pg < p.width && pg * XSV_PAGE < total ? __ldg(row + ids_from + lane) : -1;
                 if ((unsigned long long)(long long)ids >= (unsigned long long)p.pool.n_pages) ids = -1;
             }
             return __shfl_sync(0xFFFFFFFFu, ids, k & 31);
@@ -233,19 +238,19 @@ __device__ __noinline__ void producer_loop(const PageAttn& p, const Work& w, con
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int kg = 2 * part + (i ^ odd);
-                    r.code[2 * i] = *reinterpret_cast<const uint4*>(rec + R::K_CODES + (2 * kg * 32 + lane) * 16);
-                    r.code[2 * i + 1] = *reinterpret_cast<const uint4*>(rec + R::K_CODES + ((2 * kg + 1) * 32 + lane) * 16);
-                    r.a[i] = *reinterpret_cast<const uint4*>(rec + R::K_SCALE + 64 * kg + 16 * j);
-                    r.b[i] = *reinterpret_cast<const uint4*>(rec + R::K_ZERO + 64 * kg + 16 * j);
+                    r.code[2 * i] = ldg16(rec + R::K_CODES + (2 * kg * 32 + lane) * 16);
+                    r.code[2 * i + 1] = ldg16(rec + R::K_CODES + ((2 * kg + 1) * 32 + lane) * 16);
+                    r.a[i] = ldg16(rec + R::K_SCALE + 64 * kg + 16 * j);
+                    r.b[i] = ldg16(rec + R::K_ZERO + 64 * kg + 16 * j);
                 }
             } else {
                 const int v = part - C::BLK;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) r.code[t] = *reinterpret_cast<const uint4*>(rec + R::V_CODES + ((t * C::BLK + v) * 32 + lane) * 16);
+                for (int t = 0; t < 4; ++t) r.code[t] = ldg16(rec + R::V_CODES + ((t * C::BLK + v) * 32 + lane) * 16);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    r.a[i] = *reinterpret_cast<const uint4*>(rec + R::V_SCALE + 128 * v + 32 * j + 16 * i);
-                    r.b[i] = *reinterpret_cast<const uint4*>(rec + R::V_ZERO + 128 * v + 32 * j + 16 * i);
+                    r.a[i] = ldg16(rec + R::V_SCALE + 128 * v + 32 * j + 16 * i);
+                    r.b[i] = ldg16(rec + R::V_ZERO + 128 * v + 32 * j + 16 * i);
                 }
             }
         };
@@ -264,10 +269,10 @@ __device__ __noinline__ void producer_loop(const PageAttn& p, const Work& w, con
             const uint32_t step = it + (uint32_t)k, st = step % C::NSTAGE;
             if (step >= (uint32_t)C::NSTAGE) mbar_wait(BAR(C::EMPTY + (int)st), (step / C::NSTAGE - 1u) & 1u, c.abort_flag, c.status, XSV_DEV_SITE_STAGE);
             const int pg = u.en.p0 + u.kv0 + k, held = total - pg * XSV_PAGE;      // tokens of the page
-            uint8_t* stage = c.smem + C::OFF_KV + st * C::STAGE;
+            const uint32_t stage = c.base + C::OFF_KV + st * C::STAGE;
             if (part < C::BLK) {
-                uint8_t* tile = stage + part * 8192;
-                if (part == 0 && lane == 0) c.page_ok[st] = page >= 0;
+                const uint32_t tile = stage + part * 8192;
+                if (part == 0 && lane == 0) asm volatile("st.shared.b32 [%0], %1;" ::"r"(c.page_ok + 4u * st), "r"(page >= 0 ? 1 : 0) : "memory");
                 if (page >= 0 && held >= XSV_PAGE) {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
@@ -279,8 +284,8 @@ __device__ __noinline__ void producer_loop(const PageAttn& p, const Work& w, con
                                                         dq_lo(w1, cur.a[i].z, cur.b[i].z), dq_lo(w1 >> 8, cur.a[i].w, cur.b[i].w));
                             const uint4 hi = make_uint4(dq_hi(w0, cur.a[i].x, cur.b[i].x), dq_hi(w0 >> 8, cur.a[i].y, cur.b[i].y),
                                                         dq_hi(w1, cur.a[i].z, cur.b[i].z), dq_hi(w1 >> 8, cur.a[i].w, cur.b[i].w));
-                            *reinterpret_cast<uint4*>(tile + swz(place(m, 0, g >> 1, odd), chunk)) = lo;
-                            *reinterpret_cast<uint4*>(tile + swz(place(m, 1, g >> 1, odd), chunk)) = hi;
+                            sts16(tile + swz(place(m, 0, g >> 1, odd), chunk), lo);
+                            sts16(tile + swz(place(m, 1, g >> 1, odd), chunk), hi);
                         }
                     }
                 } else {
@@ -291,13 +296,12 @@ __device__ __noinline__ void producer_loop(const PageAttn& p, const Work& w, con
                         const int m = i >> 2, b = i >> 1 & 1, half = (i & 1) ^ odd, tok = 16 * m + 8 * b + g;
                         uint4 x = make_uint4(0u, 0u, 0u, 0u);
                         if (page >= 0 && tok < held) x = *reinterpret_cast<const uint4*>(tail + (size_t)tok * D + 32 * half);
-                        *reinterpret_cast<uint4*>(tile + swz(place(m, b, g >> 1, odd), 4 * half + j)) =
-                            make_uint4(to_h2<T>(x.x), to_h2<T>(x.y), to_h2<T>(x.z), to_h2<T>(x.w));
+                        sts16(tile + swz(place(m, b, g >> 1, odd), 4 * half + j), make_uint4(to_h2<T>(x.x), to_h2<T>(x.y), to_h2<T>(x.z), to_h2<T>(x.w)));
                     }
                 }
             } else {
                 const int v = part - C::BLK;
-                uint8_t* tile = stage + C::K_TILE + v * 8192;
+                const uint32_t tile = stage + C::K_TILE + v * 8192;
                 uint32_t s[8], z[8];                           // tokens 8 i + 2 j, 8 i + 2 j + 1
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -327,10 +331,10 @@ __device__ __noinline__ void producer_loop(const PageAttn& p, const Work& w, con
                     const uint4 e0 = make_uint4(e[0], e[1], e[2], e[3]), e1 = make_uint4(e[4], e[5], e[6], e[7]);
                     const uint4 o0 = make_uint4(o[0], o[1], o[2], o[3]), o1 = make_uint4(o[4], o[5], o[6], o[7]);
                     const int re = 8 * g + 2 * i;
-                    *reinterpret_cast<uint4*>(tile + swz(re, 2 * j + odd)) = odd ? e1 : e0;
-                    *reinterpret_cast<uint4*>(tile + swz(re, 2 * j + (odd ^ 1))) = odd ? e0 : e1;
-                    *reinterpret_cast<uint4*>(tile + swz(re + 1, 2 * j + odd)) = odd ? o1 : o0;
-                    *reinterpret_cast<uint4*>(tile + swz(re + 1, 2 * j + (odd ^ 1))) = odd ? o0 : o1;
+                    sts16(tile + swz(re, 2 * j + odd), odd ? e1 : e0);
+                    sts16(tile + swz(re, 2 * j + (odd ^ 1)), odd ? e0 : e1);
+                    sts16(tile + swz(re + 1, 2 * j + odd), odd ? o1 : o0);
+                    sts16(tile + swz(re + 1, 2 * j + (odd ^ 1)), odd ? o0 : o1);
                 }
             }
             fence_async_smem();
@@ -412,6 +416,9 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
         __syncwarp();
         if (lane == 0) mbar_arrive(BAR(C::QFULL + X));
 
+        // pages that every row of the warp sees whole: no mask
+        const int q_min = min(__reduce_min_sync(0xFFFFFFFFu, qpos), total - 1), q_max = __reduce_max_sync(0xFFFFFFFFu, qpos);
+        const int tok_lo = p.window > 0 ? q_max - p.window + 1 : 0, tok_hi = q_min - (XSV_PAGE - 1);
         float m_used = NO_MAX, l = 0.f;
         bool first = true;
         for (int k = 0; k < n; ++k) {
@@ -421,11 +428,11 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
             tc_fence_after();
             uint32_t va[32], vb[32], pk[16];
             tmem_ld32(tSb, va);
-            tmem_ld32(tSb + 32u, vb);
-            const bool ok = c.page_ok[(it + (uint32_t)k) % C::NSTAGE] != 0;
-            const int hi = ok ? min(qpos, total - 1) - tok0 : -1, lo = p.window > 0 ? qpos - p.window - tok0 : -1;   // visible: lo < token <= hi
-            const bool mask = __any_sync(0xFFFFFFFFu, hi < XSV_PAGE - 1 || lo >= 0);
+            int ok;
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(ok) : "r"(c.page_ok + 4u * ((it + (uint32_t)k) % C::NSTAGE)) : "memory");
             tc_wait_ld();
+            tmem_ld32(tSb + 32u, vb);              // arrives under the first half's exponentials
+            const bool mask = !(tok0 >= tok_lo && tok0 <= tok_hi && ok);     // uniform
             float ls = 0.f;
             bool careful = first || mask;
             if (!careful) {
@@ -433,15 +440,19 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
                 unsigned long long ls2 = f2_pack(0.f, 0.f);
                 softmax32(va, sc2, nm2, ls2, pk);
                 tmem_st16(tSb, pk);
+                tc_wait_ld();
                 softmax32(vb, sc2, nm2, ls2, pk);
                 tmem_st16(tSb + 16u, pk);
                 float l0, l1;
                 f2_unpack(ls2, l0, l1);
                 ls = l0 + l1;
                 careful = __any_sync(0xFFFFFFFFu, !(ls < SUM_LIMIT));
+            } else {
+                tc_wait_ld();
             }
             if (careful) {
-                if (mask) {                                // masked places, whatever stands there
+                if (mask) {                                // masked places, whatever stands there; visible: lo < token <= hi
+                    const int hi = ok ? min(qpos, total - 1) - tok0 : -1, lo = p.window > 0 ? qpos - p.window - tok0 : -1;
 #pragma unroll
                     for (int q = 0; q < 32; ++q) {
                         if (token_at(q) > hi || token_at(q) <= lo) va[q] = 0xFF800000u;
@@ -672,7 +683,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) page_attn_tc5_kernel(const __grid
         }
         w.desc[b] = d;
     }
-    const Cta cta{smem, base, bars, tmem, misc + 1, misc + 2, misc + 4};
+    const Cta cta{smem, base, bars, tmem, misc + 1, misc + 2, smem_u32(misc + 4)};
     if (warp < 8) softmax_loop<T, D>(p, w, cta, u);
     else if (warp < 8 + NPROD) producer_loop<T, D>(p, w, cta, u);
     else mma_loop<D>(w, cta, u, warp - (8 + NPROD));
