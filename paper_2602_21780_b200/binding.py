@@ -318,9 +318,9 @@ PagePlan.__doc__ = """What page_plan() says of a step (see xsv_page_plan); ring_
 def _on_device(call, first, stream):
     """Runs call(stream pointer) with the tensor's device current and, if a stream is given, that stream current."""
     import torch
-    if not first.is_cuda:
-        raise ValueError("xsv: CUDA tensors are needed")
     dev = first.get_device()
+    if dev < 0:
+        raise ValueError("xsv: CUDA tensors are needed")
     if stream is not None:
         if stream.device != first.device:
             raise ValueError("xsv: the stream belongs to another device than the tensors")
@@ -329,7 +329,7 @@ def _on_device(call, first, stream):
     if dev != torch.cuda.current_device():
         with torch.cuda.device(dev):
             return call(torch.cuda.current_stream(dev).cuda_stream)
-    return call(torch.cuda.current_stream(dev).cuda_stream)
+    return call(torch._C._cuda_getCurrentRawStream(dev))     # current_stream(dev).cuda_stream without the wrapper object
 
 
 # Checks of the arguments.  They cost more host time than a small kernel runs, so each is one pass of plain comparisons.
@@ -339,6 +339,12 @@ def _tensor(t, name, dtype, dev, shape):
         raise ValueError(f"xsv: {name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on device {dev}, "
                          f"not {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
+
+
+def _like(t):
+    """Uninitialised contiguous tensor of t's shape."""
+    import torch
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
 
 
 def _list(t, name, dev):
@@ -407,8 +413,8 @@ def qk_norm_rope(q, k, v=None, *, norm=None, q_weight=None, q_bias=None, k_weigh
             rot = d if code == 3 else 2 * nf
             fp = _tensor(inv_freq, "inv_freq", torch.float32, dev, (nf,))
             pp = _tensor(positions, "positions", torch.int32, dev, (n, 2) if code == 3 else (n,))
-        qo = q.new_empty((hq, n, d) if head_major else (n, hq, d))
-        ko = q.new_empty((hk, n, d) if head_major else (n, hk, d))
+        qo = q.new_empty((hq, n, d)) if head_major else _like(q)
+        ko = q.new_empty((hk, n, d)) if head_major else _like(k)
         vo = torch.empty_like(ko) if v is not None else None
         _check(load().xsv_qk_norm_rope(qp, kp, vp, qs, ks, vs, n, hq, hk, d, _dtype_code(q), NORMS[norm], qw, qb, kw, kb, eps,
                                        code, rot, fp, pp, 1 if head_major else 0, qo.data_ptr(), ko.data_ptr(),
@@ -430,7 +436,7 @@ def page_plan(cached_len, new_len, block_table, free_ring, ring_state, max_token
         if ring_state.dim() != 1 or ring_state.shape[0] < 2 or free_ring.dim() != 1 or max_tokens < 0:
             raise ValueError("xsv: ring_state holds head and count, free_ring is a list; max_tokens is not negative")
         one = cached_len.new_empty(4 + (n + 1) + n + 3 * max_tokens)      # one allocation for all outputs
-        state, cu, total, slot, seq, pos = one.split((4, n + 1, n, max_tokens, max_tokens, max_tokens))
+        state, cu, total, slot, seq, pos = one.split_with_sizes((4, n + 1, n, max_tokens, max_tokens, max_tokens))
         at = one.data_ptr()
         cu_at = at + 16
         total_at = cu_at + 4 * (n + 1)
@@ -489,7 +495,7 @@ def page_attention(Q, pages, k_tail, block_table, cu_new, total_len, max_new, *,
         pool, dev, i32, seqs, lib = _pool(pages, k_tail), pages.get_device(), torch.int32, total_len.shape[0], load()
         n, heads, hkv, d = *Q.shape[:2], pool.kv_heads, pool.head_dim
         qp, qs = _rows(Q, "Q", k_tail.dtype, dev, (n, heads, d))
-        to = out if out is not None else Q.new_empty((n, heads, d))
+        to = out if out is not None else _like(Q)
         need = lib.xsv_page_attention_workspace(n, seqs, max_new, heads, hkv, d)
         space = pages.new_empty(need)
         _check(lib.xsv_page_attention(C.byref(pool), qp, qs, n, heads, _table(block_table, dev, seqs), block_table.shape[1],

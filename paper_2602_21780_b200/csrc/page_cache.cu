@@ -1,6 +1,7 @@
 // Writing the pages of the shared pool, and reading them back as values.
 //
-// xsv_page_append: one block per (new tokens of one page, head).  Values are quantised per token over 64 channels as
+// xsv_page_append: one block per (new tokens of one page, head), or, where a few tokens do not fill their page
+// (decoding), one warp.  Values are quantised per token over 64 channels as
 // they come and merged into the page's code words (a token is one byte of each word it touches); keys need all 64
 // tokens of a page for their per-channel scale, so a page's keys wait in the sequence's tail, in 16 bits, and are
 // quantised by the call that brings the page's last token.  The tail has two halves, by the page's parity: the page
@@ -26,7 +27,7 @@ struct Append {
     const int* seq;
     const int* cu;
     const int* total;
-    int n_tokens, n_seqs, chunk;
+    int n_tokens, n_seqs, few_blocks, few_heads;     // blocks of one token; groups of heads that they are split into
 };
 
 template <typename T> __device__ __forceinline__ void unpack8(const uint4& w, float (&o)[8]) {
@@ -49,22 +50,61 @@ __device__ __forceinline__ bool place_of(const Append& p, int t, Place& q) {
     return q.pos >= q.off && q.pos - (t - q.begin) >= 0 && q.pos % XSV_PAGE == q.off;
 }
 
+// What codes are computed from: bf16 values beyond fp16 are brought to +-65504, fp16 ones have no such values.
+template <typename T> __device__ __forceinline__ float code_input(float x);
+template <> __device__ __forceinline__ float code_input<__half>(float x) { return x; }
+template <> __device__ __forceinline__ float code_input<__nv_bfloat16>(float x) { return clamp_half(x); }
+__device__ __noinline__ uint32_t code_bits_slow(float x, float s, float z) { return code_bits_exact(x, s, z); }
+// Codes of 8 values with the same parameters.  The mask keeps an infinite or NaN value from its neighbours in a code word.
+template <typename T> __device__ __forceinline__ void codes8(const float (&x)[8], float s, float inv, float z, uint32_t (&c)[8]) {
+    float near = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = code_bits(code_input<T>(x[i]), inv, z, near);
+    if (near > CODE_NEAR) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = code_bits_slow(code_input<T>(x[i]), s, z);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] &= 15u;
+}
+template <typename T> __device__ __forceinline__ void range8(const uint4& v, float& mn, float& mx) {
+    const float2 lo = xsv_unpack2<T>(min2<T>(min2<T>(v.x, v.y), min2<T>(v.z, v.w)));
+    const float2 hi = xsv_unpack2<T>(max2<T>(max2<T>(v.x, v.y), max2<T>(v.z, v.w)));
+    mn = fminf(lo.x, lo.y);
+    mx = fmaxf(hi.x, hi.y);
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {                       // the 8 pieces of 64 channels are 8 neighbouring lanes
+        mn = fminf(mn, __shfl_xor_sync(0xFFFFFFFFu, mn, o));
+        mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, o));
+    }
+}
+
+constexpr int FEW = 8;                       // new tokens of a page up to which one warp appends them
+
 template <typename T, int D>
 __global__ void __launch_bounds__(D, D == 128 ? 5 : 10) page_append_kernel(const __grid_constant__ Append p) {
     using R = PageRec<D>;
-    constexpr int C = D / 8;                 // 8-channel pieces of a row
+    constexpr int C = D / 8, W = D / 32;     // 8-channel pieces of a row, warps
     __shared__ uint32_t s_mn[8][D / 2], s_mx[8][D / 2];
     __shared__ float s_scale[D], s_zero[D], s_inv[D];
     xsv_dep_release();
     xsv_dep_sync();
-    const int tid = threadIdx.x, piece = tid % C, g = tid / C, head = blockIdx.y, lane = tid & 31;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     // the chunk's tokens that are the first new ones of their page; every warp finds the same
     Place mine{};
-    bool first = false;
-    const int t_lane = blockIdx.x * p.chunk + lane;
-    if (lane < p.chunk && t_lane < p.n_tokens) first = place_of(p, t_lane, mine) && (t_lane == mine.begin || mine.off == 0);
-    for (uint32_t todo = __ballot_sync(0xFFFFFFFFu, first); todo; todo &= todo - 1) {
-        const int from = __ffs(todo) - 1, t = blockIdx.x * p.chunk + from;
+    bool first = false, few = false;
+    // The first blocks (decoding) have a token and a head a warp and take the few-token pages, the others 32 tokens and a head.
+    const bool one = (int)blockIdx.x < p.few_blocks;
+    const int index = one ? blockIdx.x : blockIdx.x - p.few_blocks, across = one ? p.few_heads : p.pool.heads;
+    const int t_block = index / across * (one ? 1 : 32), head0 = index % across * (one ? W : 1), head1 = min(p.pool.heads, head0 + (one ? W : 1));
+    const int t_lane = t_block + lane;
+    if (lane < (one ? 1 : 32) && t_lane < p.n_tokens) first = place_of(p, t_lane, mine) && (t_lane == mine.begin || mine.off == 0);
+    if (first) {
+        const int run = min(XSV_PAGE - mine.off, mine.end - t_lane);
+        few = run <= FEW && mine.off + run < XSV_PAGE;
+    }
+    const uint32_t firsts = __ballot_sync(0xFFFFFFFFu, first), fews = __ballot_sync(0xFFFFFFFFu, few);
+    auto place_at = [&](int from) {
         Place q;
         q.seq = __shfl_sync(0xFFFFFFFFu, mine.seq, from);
         q.begin = __shfl_sync(0xFFFFFFFFu, mine.begin, from);
@@ -72,156 +112,193 @@ __global__ void __launch_bounds__(D, D == 128 ? 5 : 10) page_append_kernel(const
         q.page = __shfl_sync(0xFFFFFFFFu, mine.page, from);
         q.off = __shfl_sync(0xFFFFFFFFu, mine.off, from);
         q.pos = __shfl_sync(0xFFFFFFFFu, mine.pos, from);
-        const int run = min(XSV_PAGE - q.off, q.end - t), total = q.pos + q.end - t;
-        const bool full = q.off + run == XSV_PAGE;
-        uint8_t* rec = page_rec<D>(p.pool, q.page, head);
-        const T* K = (const T*)p.K + (size_t)head * D + 8 * piece;
-        const T* V = (const T*)p.V + (size_t)head * D + 8 * piece;
-        const int page_no = q.pos / XSV_PAGE;
-        // The last, unfilled page's keys go to the tail half of its parity.  Where the sequence's first page here still
-        // reads old keys from that half, the block of that first page writes them, after its reads.
-        const int p0 = q.pos - (t - q.begin), first_no = p0 / XSV_PAGE, last_no = total / XSV_PAGE;
-        const bool handed = p0 % XSV_PAGE != 0 && last_no > first_no && ((last_no - first_no) & 1) == 0;
+        return q;
+    };
+    // The last, unfilled page's keys go to the tail half of its parity.  Where the sequence's first page here still
+    // reads old keys from that half, the block of that first page writes them, after its reads.
+    auto handed_on = [&](const Place& q, int t) {
+        const int p0 = q.pos - (t - q.begin), first_no = p0 / XSV_PAGE, last_no = (q.pos + q.end - t) / XSV_PAGE;
+        return p0 % XSV_PAGE != 0 && last_no > first_no && ((last_no - first_no) & 1) == 0;
+    };
 
-        // ---- values: 4 tokens x 8 channels a thread, twice
-#pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
-            const int combo = g + 8 * half, tok0 = 16 * (combo >> 2) + 2 * (combo & 3);
-            uint4 raw[4];
-            bool there[4];
-            uint32_t mask = 0;
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const int tok = tok0 + 8 * (b & 1) + (b >> 1);
-                there[b] = tok >= q.off && tok < q.off + run;
-                raw[b] = make_uint4(0, 0, 0, 0);
-                if (there[b]) {
-                    raw[b] = *reinterpret_cast<const uint4*>(V + (size_t)(t + tok - q.off) * p.v_stride);
-                    mask |= 0xFFu << (8 * b);
+    // ---- a few tokens that do not fill their page (decoding): a warp each, every lane 8 channels of a token
+    int turn = 0;
+    for (uint32_t todo = one || p.few_blocks == 0 ? fews : 0; todo; todo &= todo - 1) {
+        const int from = __ffs(todo) - 1, t = t_block + from;
+        const Place q = place_at(from);
+        for (int head = head0; head < head1; ++head, ++turn) {
+            if (turn % W != warp) continue;
+            const int run = min(XSV_PAGE - q.off, q.end - t), page_no = q.pos / XSV_PAGE, piece = lane % C;
+            const bool skip_keys = handed_on(q, t) && page_no != (q.pos - (t - q.begin)) / XSV_PAGE;
+            uint8_t* rec = page_rec<D>(p.pool, q.page, head);
+            T* tail = tail_rows<T, D>(p.pool, q.seq, page_no, head) + 8 * piece;
+            for (int r0 = 0; r0 < run; r0 += 32 / C) {          // the same for the whole warp
+                const int r = r0 + lane / C, tok = q.off + r;
+                const bool live = r < run;
+                uint4 k = make_uint4(0, 0, 0, 0), v = k;
+                if (live) {
+                    k = *reinterpret_cast<const uint4*>((const T*)p.K + (size_t)(t + r) * p.k_stride + (size_t)head * D + 8 * piece);
+                    v = *reinterpret_cast<const uint4*>((const T*)p.V + (size_t)(t + r) * p.v_stride + (size_t)head * D + 8 * piece);
                 }
-            }
-            if (!__any_sync(0xFFFFFFFFu, mask != 0)) continue;
-            uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const int tok = tok0 + 8 * (b & 1) + (b >> 1);
-                float mn, mx;
-                {
-                    const float2 lo = xsv_unpack2<T>(min2<T>(min2<T>(raw[b].x, raw[b].y), min2<T>(raw[b].z, raw[b].w)));
-                    const float2 hi = xsv_unpack2<T>(max2<T>(max2<T>(raw[b].x, raw[b].y), max2<T>(raw[b].z, raw[b].w)));
-                    mn = fminf(lo.x, lo.y);
-                    mx = fmaxf(hi.x, hi.y);
-                }
-#pragma unroll
-                for (int o = 1; o < 8; o <<= 1) {               // the 8 pieces of 64 channels are 8 neighbouring lanes
-                    mn = fminf(mn, __shfl_xor_sync(0xFFFFFFFFu, mn, o));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, o));
-                }
+                if (live && !skip_keys) *reinterpret_cast<uint4*>(tail + (size_t)tok * D) = k;
+                float mn, mx, x[8];
+                range8<T>(v, mn, mx);
                 __half hs, hz;
                 page_params(clamp_half(mn), clamp_half(mx), hs, hz);
-                const float s = __half2float(hs), z = __half2float(hz), inv = __frcp_rn(s);
-                float x[8], near = 0.f;
-                unpack8<T>(raw[b], x);
+                const float s = __half2float(hs), z = __half2float(hz);
                 uint32_t c[8];
+                unpack8<T>(v, x);
+                codes8<T>(x, s, __frcp_rn(s), z, c);
+                if (live) {
+                    // the token's byte of four words: [k = tok / 16][c][g][j = tok % 8 / 2][m], byte 2 (tok % 2) + tok / 8 % 2
+                    uint8_t* at = rec + R::V_CODES + (((tok / 16) * (D / 64) + piece / 8) * 32 + (piece % 8) * 4 + tok % 8 / 2) * 16 + 2 * (tok % 2) + tok / 8 % 2;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) c[i] = code_bits(clamp_half(x[i]), inv, z, near);
-                if (near > CODE_NEAR)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) c[i] = code_bits_exact(clamp_half(x[i]), s, z);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) w[i >> 1] += (c[i] - CODE_BASE) << (8 * b + 4 * (i & 1));
-                if (there[b] && piece % 8 == 0) {
-                    const int at = (piece / 8) * 64 + (tok % 8) * 8 + tok / 8;
-                    reinterpret_cast<__half*>(rec + R::V_SCALE)[at] = hs;
-                    reinterpret_cast<__half*>(rec + R::V_ZERO)[at] = hz;
-                }
-            }
-            if (mask) {
-                uint4* at = reinterpret_cast<uint4*>(rec + R::V_CODES + (((combo >> 2) * (D / 64) + piece / 8) * 32 + (piece % 8) * 4 + (combo & 3)) * 16);
-                uint4 old = make_uint4(0, 0, 0, 0);
-                if (mask != 0xFFFFFFFFu) old = *at;
-                *at = make_uint4((w[0] & mask) | (old.x & ~mask), (w[1] & mask) | (old.y & ~mask), (w[2] & mask) | (old.z & ~mask),
-                                 (w[3] & mask) | (old.w & ~mask));
-            }
-        }
-
-        // ---- keys
-        if (!full) {
-            if (!(handed && page_no != first_no)) {
-                T* tail = tail_rows<T, D>(p.pool, q.seq, page_no, head) + 8 * piece;
-                for (int r = g; r < run; r += 8)
-                    *reinterpret_cast<uint4*>(tail + (size_t)(q.off + r) * D) = *reinterpret_cast<const uint4*>(K + (size_t)(t + r) * p.k_stride);
-            }
-            continue;
-        }
-        uint4 row[8];
-        {
-            const T* tail = tail_rows<T, D>(p.pool, q.seq, page_no, head) + 8 * piece;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int r = 8 * i + g;
-                row[i] = *reinterpret_cast<const uint4*>(r < q.off ? tail + (size_t)r * D : K + (size_t)(t + r - q.off) * p.k_stride);
-            }
-        }
-        {
-            uint4 mn = row[0], mx = row[0];
-#pragma unroll
-            for (int i = 1; i < 8; ++i) {
-                mn = make_uint4(min2<T>(mn.x, row[i].x), min2<T>(mn.y, row[i].y), min2<T>(mn.z, row[i].z), min2<T>(mn.w, row[i].w));
-                mx = make_uint4(max2<T>(mx.x, row[i].x), max2<T>(mx.y, row[i].y), max2<T>(mx.z, row[i].z), max2<T>(mx.w, row[i].w));
-            }
-            *reinterpret_cast<uint4*>(&s_mn[g][4 * piece]) = mn;
-            *reinterpret_cast<uint4*>(&s_mx[g][4 * piece]) = mx;
-        }
-        __syncthreads();
-        if (tid < D / 2) {
-            uint32_t mn = s_mn[0][tid], mx = s_mx[0][tid];
-#pragma unroll
-            for (int i = 1; i < 8; ++i) { mn = min2<T>(mn, s_mn[i][tid]); mx = max2<T>(mx, s_mx[i][tid]); }
-            const float2 lo = xsv_unpack2<T>(mn), hi = xsv_unpack2<T>(mx);
-            __half s0, z0, s1, z1;
-            page_params(clamp_half(lo.x), clamp_half(hi.x), s0, z0);
-            page_params(clamp_half(lo.y), clamp_half(hi.y), s1, z1);
-            reinterpret_cast<__half2*>(rec + R::K_SCALE)[tid] = __halves2half2(s0, s1);
-            reinterpret_cast<__half2*>(rec + R::K_ZERO)[tid] = __halves2half2(z0, z1);
-            s_scale[2 * tid] = __half2float(s0); s_scale[2 * tid + 1] = __half2float(s1);
-            s_zero[2 * tid] = __half2float(z0); s_zero[2 * tid + 1] = __half2float(z1);
-            s_inv[2 * tid] = __frcp_rn(__half2float(s0)); s_inv[2 * tid + 1] = __frcp_rn(__half2float(s1));
-        }
-        __syncthreads();
-        {
-            // channel c of the piece: step 2 (piece / 4) + c / 4, byte 2 (c % 2) + (c % 4) / 2; row 8 i + g: word i / 2,
-            // nibble i % 2
-#pragma unroll
-            for (int kl = 0; kl < 2; ++kl) {
-                uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-                for (int c4 = 0; c4 < 4; ++c4) {
-                    const int c = 4 * kl + c4, sh = 8 * (2 * (c % 2) + (c % 4) / 2);
-                    const float s = s_scale[8 * piece + c], z = s_zero[8 * piece + c], inv = s_inv[8 * piece + c];
-                    float x[8], near = 0.f;
-                    uint32_t code[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const uint32_t pair = c < 2 ? row[i].x : c < 4 ? row[i].y : c < 6 ? row[i].z : row[i].w;
-                        const float2 two = xsv_unpack2<T>(pair);
-                        x[i] = clamp_half(c & 1 ? two.y : two.x);
-                        code[i] = code_bits(x[i], inv, z, near);
+                    for (int m = 0; m < 4; ++m) at[4 * m] = (uint8_t)(c[2 * m] | c[2 * m + 1] << 4);
+                    if (piece % 8 == 0) {
+                        const int i = (piece / 8) * 64 + (tok % 8) * 8 + tok / 8;
+                        reinterpret_cast<__half*>(rec + R::V_SCALE)[i] = hs;
+                        reinterpret_cast<__half*>(rec + R::V_ZERO)[i] = hz;
                     }
-                    if (near > CODE_NEAR)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) code[i] = code_bits_exact(x[i], s, z);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) w[i / 2] += (code[i] - CODE_BASE) << (sh + 4 * (i % 2));
                 }
-                *reinterpret_cast<uint4*>(rec + R::K_CODES + ((2 * (piece / 4) + kl) * 32 + g * 4 + piece % 4) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
             }
         }
-        if (handed && page_no == first_no) {                    // after the barriers: the old keys have been read
-            const int left = total % XSV_PAGE;
-            T* tail = tail_rows<T, D>(p.pool, q.seq, last_no, head) + 8 * piece;
-            for (int r = g; r < left; r += 8)
-                *reinterpret_cast<uint4*>(tail + (size_t)r * D) = *reinterpret_cast<const uint4*>(K + (size_t)(q.end - left + r) * p.k_stride);
+    }
+
+    // ---- the others: the whole block, one page and head at a time
+    const int piece = tid % C, g = tid / C;
+    for (uint32_t todo = one ? 0 : firsts & ~fews; todo; todo &= todo - 1) {
+        const int from = __ffs(todo) - 1, t = t_block + from;
+        const Place q = place_at(from);
+        const int run = min(XSV_PAGE - q.off, q.end - t), total = q.pos + q.end - t, page_no = q.pos / XSV_PAGE;
+        const bool full = q.off + run == XSV_PAGE, handed = handed_on(q, t);
+        const int first_no = (q.pos - (t - q.begin)) / XSV_PAGE, last_no = total / XSV_PAGE;
+#pragma unroll 1
+        for (int head = head0; head < head1; ++head) {
+            uint8_t* rec = page_rec<D>(p.pool, q.page, head);
+            const T* K = (const T*)p.K + (size_t)head * D + 8 * piece;
+            const T* V = (const T*)p.V + (size_t)head * D + 8 * piece;
+            // values: 4 tokens x 8 channels a thread, twice
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {
+                const int combo = g + 8 * half, tok0 = 16 * (combo >> 2) + 2 * (combo & 3);
+                uint4 raw[4];
+                uint32_t mask = 0;
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const int tok = tok0 + 8 * (b & 1) + (b >> 1);
+                    raw[b] = make_uint4(0, 0, 0, 0);
+                    if (tok >= q.off && tok < q.off + run) {
+                        raw[b] = *reinterpret_cast<const uint4*>(V + (size_t)(t + tok - q.off) * p.v_stride);
+                        mask |= 0xFFu << (8 * b);
+                    }
+                }
+                if (!__any_sync(0xFFFFFFFFu, mask != 0)) continue;
+                uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll 2
+                for (int b = 0; b < 4; ++b) {
+                    const uint4 v = b == 0 ? raw[0] : b == 1 ? raw[1] : b == 2 ? raw[2] : raw[3];
+                    float mn, mx, x[8];
+                    range8<T>(v, mn, mx);
+                    __half hs, hz;
+                    page_params(clamp_half(mn), clamp_half(mx), hs, hz);
+                    const float s = __half2float(hs), z = __half2float(hz);
+                    uint32_t c[8];
+                    unpack8<T>(v, x);
+                    codes8<T>(x, s, __frcp_rn(s), z, c);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] += (c[2 * i] + (c[2 * i + 1] << 4)) << (8 * b);
+                    if (piece % 8 == 0 && (mask >> (8 * b) & 1u)) {
+                        const int tok = tok0 + 8 * (b & 1) + (b >> 1), at = (piece / 8) * 64 + (tok % 8) * 8 + tok / 8;
+                        reinterpret_cast<__half*>(rec + R::V_SCALE)[at] = hs;
+                        reinterpret_cast<__half*>(rec + R::V_ZERO)[at] = hz;
+                    }
+                }
+                if (mask) {
+                    uint4* at = reinterpret_cast<uint4*>(rec + R::V_CODES + (((combo >> 2) * (D / 64) + piece / 8) * 32 + (piece % 8) * 4 + (combo & 3)) * 16);
+                    uint4 old = make_uint4(0, 0, 0, 0);
+                    if (mask != 0xFFFFFFFFu) old = *at;
+                    *at = make_uint4((w[0] & mask) | (old.x & ~mask), (w[1] & mask) | (old.y & ~mask), (w[2] & mask) | (old.z & ~mask),
+                                     (w[3] & mask) | (old.w & ~mask));
+                }
+            }
+            // keys
+            if (!full) {
+                if (!(handed && page_no != first_no)) {
+                    T* tail = tail_rows<T, D>(p.pool, q.seq, page_no, head) + 8 * piece;
+                    for (int r = g; r < run; r += 8)
+                        *reinterpret_cast<uint4*>(tail + (size_t)(q.off + r) * D) = *reinterpret_cast<const uint4*>(K + (size_t)(t + r) * p.k_stride);
+                }
+                continue;
+            }
+            uint4 row[8];
+            {
+                const T* tail = tail_rows<T, D>(p.pool, q.seq, page_no, head) + 8 * piece;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int r = 8 * i + g;
+                    row[i] = *reinterpret_cast<const uint4*>(r < q.off ? tail + (size_t)r * D : K + (size_t)(t + r - q.off) * p.k_stride);
+                }
+            }
+            {
+                uint4 mn = row[0], mx = row[0];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) {
+                    mn = make_uint4(min2<T>(mn.x, row[i].x), min2<T>(mn.y, row[i].y), min2<T>(mn.z, row[i].z), min2<T>(mn.w, row[i].w));
+                    mx = make_uint4(max2<T>(mx.x, row[i].x), max2<T>(mx.y, row[i].y), max2<T>(mx.z, row[i].z), max2<T>(mx.w, row[i].w));
+                }
+                *reinterpret_cast<uint4*>(&s_mn[g][4 * piece]) = mn;
+                *reinterpret_cast<uint4*>(&s_mx[g][4 * piece]) = mx;
+            }
+            __syncthreads();
+            if (tid < D / 2) {
+                uint32_t mn = s_mn[0][tid], mx = s_mx[0][tid];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) { mn = min2<T>(mn, s_mn[i][tid]); mx = max2<T>(mx, s_mx[i][tid]); }
+                const float2 lo = xsv_unpack2<T>(mn), hi = xsv_unpack2<T>(mx);
+                __half s0, z0, s1, z1;
+                page_params(clamp_half(lo.x), clamp_half(hi.x), s0, z0);
+                page_params(clamp_half(lo.y), clamp_half(hi.y), s1, z1);
+                reinterpret_cast<__half2*>(rec + R::K_SCALE)[tid] = __halves2half2(s0, s1);
+                reinterpret_cast<__half2*>(rec + R::K_ZERO)[tid] = __halves2half2(z0, z1);
+                const float f0 = __half2float(s0), f1 = __half2float(s1);
+                reinterpret_cast<float2*>(s_scale)[tid] = make_float2(f0, f1);
+                reinterpret_cast<float2*>(s_zero)[tid] = make_float2(__half2float(z0), __half2float(z1));
+                reinterpret_cast<float2*>(s_inv)[tid] = make_float2(__frcp_rn(f0), __frcp_rn(f1));
+            }
+            __syncthreads();
+            // channel c of the piece: step 2 (piece / 4) + c / 4, byte 2 (c % 2) + (c % 4) / 2; row 8 i + g: word i / 2,
+            // nibble i % 2.  Two channels a turn, the rows' next pair moved up after it: unrolled, this is more code than the
+            // instruction cache holds.
+            uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll 1
+            for (int c = 0; c < 8; c += 2) {
+                const float2 s = *reinterpret_cast<const float2*>(&s_scale[8 * piece + c]), z = *reinterpret_cast<const float2*>(&s_zero[8 * piece + c]),
+                             inv = *reinterpret_cast<const float2*>(&s_inv[8 * piece + c]);
+                float x0[8], x1[8];
+                uint32_t c0[8], c1[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float2 two = xsv_unpack2<T>(row[i].x);
+                    x0[i] = two.x;
+                    x1[i] = two.y;
+                    row[i].x = row[i].y; row[i].y = row[i].z; row[i].z = row[i].w;
+                }
+                codes8<T>(x0, s.x, inv.x, z.x, c0);
+                codes8<T>(x1, s.y, inv.y, z.y, c1);
+                const int sh = 4 * (c & 2);                     // byte (c % 4) / 2, and two bytes up for the second channel
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i / 2] += (c0[i] + (c1[i] << 16)) << (sh + 4 * (i % 2));
+                if (c & 2) {
+                    *reinterpret_cast<uint4*>(rec + R::K_CODES + ((2 * (piece / 4) + c / 4) * 32 + g * 4 + piece % 4) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+                    w[0] = w[1] = w[2] = w[3] = 0;
+                }
+            }
+            if (handed && page_no == first_no) {                // after the barriers: the old keys have been read
+                const int left = total % XSV_PAGE;
+                T* tail = tail_rows<T, D>(p.pool, q.seq, last_no, head) + 8 * piece;
+                for (int r = g; r < left; r += 8)
+                    *reinterpret_cast<uint4*>(tail + (size_t)r * D) = *reinterpret_cast<const uint4*>(K + (size_t)(q.end - left + r) * p.k_stride);
+            }
         }
     }
 }
@@ -238,8 +315,21 @@ struct Read {
 };
 
 constexpr int READ_ROWS = 32;                // rows of a block
-// the low four bits as a float, without the conversion unit
-__device__ __forceinline__ float small(uint32_t w) { return __fadd_rn(__uint_as_float((w & 15u) | 0x4B000000u), -8388608.f); }
+constexpr uint32_t LOW = 0x000F000Fu;
+// Two codes (in the halves of a word) times scale plus offset, rounded once: fp16 by one fused operation, bf16 from float32.
+// 1024 + code, as fp16 bits, minus 1024 is the code exactly.
+template <typename T> __device__ __forceinline__ uint32_t value2(uint32_t codes, uint32_t s, uint32_t z);
+template <> __device__ __forceinline__ uint32_t value2<__half>(uint32_t codes, uint32_t s, uint32_t z) {
+    uint32_t c = codes | 0x64006400u, d;
+    asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(c) : "r"(0x64006400u));
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(c), "r"(s), "r"(z));
+    return d;
+}
+template <> __device__ __forceinline__ uint32_t value2<__nv_bfloat16>(uint32_t codes, uint32_t s, uint32_t z) {
+    const float2 fs = xsv_unpack2<__half>(s), fz = xsv_unpack2<__half>(z);
+    const float c0 = __fadd_rn(__uint_as_float(codes & 15u | 0x4B000000u), -8388608.f), c1 = __fadd_rn(__uint_as_float(codes >> 16 | 0x4B000000u), -8388608.f);
+    return xsv_pack2<__nv_bfloat16>(fmaf(c0, fs.x, fz.x), fmaf(c1, fs.y, fz.y));
+}
 
 template <typename T, int D>
 __global__ void __launch_bounds__(256) page_read_kernel(const __grid_constant__ Read p) {
@@ -264,27 +354,25 @@ __global__ void __launch_bounds__(256) page_read_kernel(const __grid_constant__ 
             if (pos / XSV_PAGE == len / XSV_PAGE) {              // the unfilled page: keys as they came
                 k = *reinterpret_cast<const uint4*>(tail_rows<T, D>(p.pool, seq, pos / XSV_PAGE, head) + (size_t)tok * D + 8 * piece);
             } else {
-                const uint4 sc = *reinterpret_cast<const uint4*>(rec + R::K_SCALE + 16 * piece);
-                const uint4 ze = *reinterpret_cast<const uint4*>(rec + R::K_ZERO + 16 * piece);
-                float s[8], z[8], x[8];
-                unpack8<__half>(sc, s);
-                unpack8<__half>(ze, z);
-#pragma unroll
-                for (int kl = 0; kl < 2; ++kl) {
-                    const uint32_t w = *reinterpret_cast<const uint32_t*>(rec + R::K_CODES + ((2 * (piece / 4) + kl) * 32 + g * 4 + piece % 4) * 16 + (tok / 16) * 4) >> (4 * (tok / 8 % 2));
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) x[4 * kl + c] = fmaf(small(w >> (8 * (2 * (c % 2) + c / 2))), s[4 * kl + c], z[4 * kl + c]);
-                }
-                k = make_uint4(xsv_pack2<T>(x[0], x[1]), xsv_pack2<T>(x[2], x[3]), xsv_pack2<T>(x[4], x[5]), xsv_pack2<T>(x[6], x[7]));
+                const uint4 s = *reinterpret_cast<const uint4*>(rec + R::K_SCALE + 16 * piece);
+                const uint4 z = *reinterpret_cast<const uint4*>(rec + R::K_ZERO + 16 * piece);
+                const uint8_t* at = rec + R::K_CODES + (2 * (piece / 4) * 32 + g * 4 + piece % 4) * 16 + (tok / 16) * 4;
+                const int sh = tok / 8 % 2 * 4;
+                const uint32_t w0 = *reinterpret_cast<const uint32_t*>(at) >> sh, w1 = *reinterpret_cast<const uint32_t*>(at + 512) >> sh;
+                k = make_uint4(value2<T>(w0 & LOW, s.x, z.x), value2<T>(w0 >> 8 & LOW, s.y, z.y), value2<T>(w1 & LOW, s.z, z.z), value2<T>(w1 >> 8 & LOW, s.w, z.w));
             }
             const int at = (piece / 8) * 64 + g * 8 + tok / 8;
-            const float s = __half2float(reinterpret_cast<const __half*>(rec + R::V_SCALE)[at]);
-            const float z = __half2float(reinterpret_cast<const __half*>(rec + R::V_ZERO)[at]);
+            uint32_t s = reinterpret_cast<const unsigned short*>(rec + R::V_SCALE)[at], z = reinterpret_cast<const unsigned short*>(rec + R::V_ZERO)[at];
+            s |= s << 16;
+            z |= z << 16;
             const uint4 w = *reinterpret_cast<const uint4*>(rec + R::V_CODES + (((tok / 16) * (D / 64) + piece / 8) * 32 + (piece % 8) * 4 + tok % 8 / 2) * 16);
-            const int sh = 8 * (2 * (tok % 2) + tok / 8 % 2);
-            auto val = [&](uint32_t word, int i) { return fmaf(small(word >> (sh + 4 * i)), s, z); };
-            v = make_uint4(xsv_pack2<T>(val(w.x, 0), val(w.x, 1)), xsv_pack2<T>(val(w.y, 0), val(w.y, 1)),
-                           xsv_pack2<T>(val(w.z, 0), val(w.z, 1)), xsv_pack2<T>(val(w.w, 0), val(w.w, 1)));
+            // the token's byte at both ends of a word: its low nibble below, its high nibble four bits up above
+            const uint32_t sel = 0x4040u + 0x0101u * (uint32_t)(2 * (tok % 2) + tok / 8 % 2);
+            auto pair = [&](uint32_t word) {
+                const uint32_t x = __byte_perm(word, 0, sel);
+                return (x & 0xFu) | (x >> 4 & 0xF0000u);
+            };
+            v = make_uint4(value2<T>(pair(w.x), s, z), value2<T>(pair(w.y), s, z), value2<T>(pair(w.z), s, z), value2<T>(pair(w.w), s, z));
         }
         const size_t to = ((size_t)r * p.pool.heads + head) * D + 8 * piece;
         *reinterpret_cast<uint4*>((T*)p.K + to) = k;
@@ -321,10 +409,15 @@ extern "C" xsv_status xsv_page_append(const xsv_page_pool* pool, const void* K, 
     p.K = K; p.V = V; p.k_stride = k_stride; p.v_stride = v_stride;
     p.slot = slot_map; p.seq = token_seq; p.cu = cu_new; p.total = total_len;
     p.n_tokens = n_tokens; p.n_seqs = n_seqs;
-    // A block looks for first tokens of pages among `chunk` new tokens: one each where most sequences bring a few
-    // tokens (every token may be one), 16 where prompts do (one in 64 is one).
-    p.chunk = (long long)n_tokens <= 8LL * n_seqs ? 1 : 16;
-    const dim3 grid((n_tokens + p.chunk - 1) / p.chunk, pool->kv_heads);
+    // A block looks for first tokens of pages among 32 new tokens, for one head.  Where most sequences bring a few tokens
+    // (decoding) every token may be one, and a block each takes those that do not fill their page, a warp a head.
+    const bool decode = (long long)n_tokens <= 8LL * n_seqs;
+    const int warps = pool->head_dim / 32;
+    p.few_heads = (pool->kv_heads + warps - 1) / warps;
+    const long long few = decode ? (long long)n_tokens * p.few_heads : 0, blocks = few + (long long)((n_tokens + 31) / 32) * pool->kv_heads;
+    if (blocks > 0x7FFFFFFFLL) return XSV_ERR_LIMIT;
+    p.few_blocks = (int)few;
+    const dim3 grid((unsigned)blocks);
     auto go = [&](auto kernel) { return xsv_launch_dep(kernel, grid, dim3(pool->head_dim), 0, (cudaStream_t)stream, p); };
     cudaError_t e;
     if (pool->dtype == XSV_F16) e = pool->head_dim == 64 ? go(page_append_kernel<__half, 64>) : go(page_append_kernel<__half, 128>);

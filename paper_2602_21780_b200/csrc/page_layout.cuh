@@ -77,7 +77,6 @@ __device__ __forceinline__ uint32_t code_bits(float x, float inv_s, float z, flo
 __device__ __forceinline__ uint32_t code_bits_exact(float x, float s, float z) {
     return __float_as_uint(__fadd_rn(__fdiv_rn(__fsub_rn(x, z), s), 12582912.f));
 }
-constexpr uint32_t CODE_BASE = 0x4B400000u;                 // the bits of 1.5 * 2^23
 // minimum and maximum of pairs of 16-bit values
 template <typename T> __device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b);
 template <typename T> __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b);

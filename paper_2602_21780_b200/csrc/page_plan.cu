@@ -17,7 +17,7 @@
 namespace {
 
 constexpr int THREADS = 512;
-constexpr int TOKENS_PER_BLOCK = 2048;
+constexpr int TOKENS_PER_BLOCK = 512;
 
 struct Plan {
     const int* cached;

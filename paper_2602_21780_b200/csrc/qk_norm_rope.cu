@@ -40,7 +40,7 @@ template <typename T> __device__ __forceinline__ void unpack4(const uint2& w, fl
     o[0] = a.x; o[1] = a.y; o[2] = b.x; o[3] = b.y;
 }
 
-constexpr int THREADS = 128;
+constexpr int THREADS = 128, FLIGHT = 2;      // FLIGHT: rows of a lane group in flight
 
 template <typename T, int D, int ROPE, int NORM>
 __global__ void __launch_bounds__(THREADS, 8) qk_norm_rope_kernel(const __grid_constant__ NormRope p) {
@@ -80,18 +80,28 @@ __global__ void __launch_bounds__(THREADS, 8) qk_norm_rope_kernel(const __grid_c
         }
     }
     const int n_freq = p.n_rot / 2, h0 = blockIdx.y * GROUPS, step = gridDim.y * GROUPS;
+    // the frequency this thread serves; its position is fetched a token ahead
+    const bool serves = ROPE != XSV_ROPE_NONE && (int)threadIdx.x < n_freq;
+    int coord = 0, at = 0;
+    double freq = 0.0;
+    if (serves) {
+        const int per = ROPE == XSV_ROPE_2D ? n_freq / 2 : n_freq;
+        coord = threadIdx.x / per;
+        freq = (double)p.inv_freq[threadIdx.x - coord * per];
+        at = ROPE == XSV_ROPE_2D ? p.pos[2 * (size_t)blockIdx.x + coord] : p.pos[blockIdx.x];
+    }
     int buf = 0;
     for (int t = blockIdx.x; t < p.n_tokens; t += gridDim.x, buf ^= 1) {
         float2 r[4];
         if (ROPE != XSV_ROPE_NONE) {
-            if ((int)threadIdx.x < n_freq) {
-                const int per = ROPE == XSV_ROPE_2D ? n_freq / 2 : n_freq, i = threadIdx.x % per;
-                const int at = ROPE == XSV_ROPE_2D ? p.pos[2 * (size_t)t + threadIdx.x / per] : p.pos[t];
-                double turns = (double)at * (double)p.inv_freq[i] * 0.15915494309189533577;
+            if (serves) {
+                double turns = (double)at * freq * 0.15915494309189533577;
                 turns -= rint(turns);
                 float s, c;
                 sincospif(2.f * (float)turns, &s, &c);
                 cs[buf][threadIdx.x] = make_float2(c, s);
+                const int next = t + gridDim.x;
+                if (next < p.n_tokens) at = ROPE == XSV_ROPE_2D ? p.pos[2 * (size_t)next + coord] : p.pos[next];
             }
             __syncthreads();                                // two buffers: the last token's are read before this one
 #pragma unroll
@@ -109,10 +119,10 @@ __global__ void __launch_bounds__(THREADS, 8) qk_norm_rope_kernel(const __grid_c
                 unpack4<T>(bias[part][0], b); unpack4<T>(bias[part][1], b + 4);
             }
             // two rows of the group at a time; every lane of the warp takes part in the shuffles, whatever its row
-            for (int base = h0; base < heads; base += 2 * step) {
-                uint2 in[2][2];
+            for (int base = h0; base < heads; base += FLIGHT * step) {
+                uint2 in[FLIGHT][2];
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
+                for (int u = 0; u < FLIGHT; ++u) {
                     const int h = base + u * step + group;
                     in[u][0] = in[u][1] = make_uint2(0u, 0u);
                     if (h < heads) {
@@ -121,7 +131,7 @@ __global__ void __launch_bounds__(THREADS, 8) qk_norm_rope_kernel(const __grid_c
                     }
                 }
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
+                for (int u = 0; u < FLIGHT; ++u) {
                     const int h = base + u * step + group;
                     if (base + u * step >= heads) break;    // the same for the whole block
                     if (part < 2 && (NORM != XSV_NORM_NONE || ROPE != XSV_ROPE_NONE)) {
