@@ -27,7 +27,7 @@ struct Append {
     const int* seq;
     const int* cu;
     const int* total;
-    int n_tokens, n_seqs, few_blocks, few_heads;     // blocks of one token; groups of heads that they are split into
+    int n_tokens, n_seqs, chunk, few_blocks, few_heads;     // few_: blocks of one token, groups of heads that they are split into
 };
 
 template <typename T> __device__ __forceinline__ void unpack8(const uint4& w, float (&o)[8]) {
@@ -54,18 +54,11 @@ __device__ __forceinline__ bool place_of(const Append& p, int t, Place& q) {
 template <typename T> __device__ __forceinline__ float code_input(float x);
 template <> __device__ __forceinline__ float code_input<__half>(float x) { return x; }
 template <> __device__ __forceinline__ float code_input<__nv_bfloat16>(float x) { return clamp_half(x); }
-__device__ __noinline__ uint32_t code_bits_slow(float x, float s, float z) { return code_bits_exact(x, s, z); }
-// Codes of 8 values with the same parameters.  The mask keeps an infinite or NaN value from its neighbours in a code word.
 template <typename T> __device__ __forceinline__ void codes8(const float (&x)[8], float s, float inv, float z, uint32_t (&c)[8]) {
-    float near = 0.f;
+    float y[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = code_bits(code_input<T>(x[i]), inv, z, near);
-    if (near > CODE_NEAR) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) c[i] = code_bits_slow(code_input<T>(x[i]), s, z);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] &= 15u;
+    for (int i = 0; i < 8; ++i) y[i] = code_input<T>(x[i]);
+    page_codes(y, s, inv, z, c);
 }
 template <typename T> __device__ __forceinline__ void range8(const uint4& v, float& mn, float& mx) {
     const float2 lo = xsv_unpack2<T>(min2<T>(min2<T>(v.x, v.y), min2<T>(v.z, v.w)));
@@ -93,12 +86,12 @@ __global__ void __launch_bounds__(D, D == 128 ? 5 : 10) page_append_kernel(const
     // the chunk's tokens that are the first new ones of their page; every warp finds the same
     Place mine{};
     bool first = false, few = false;
-    // The first blocks (decoding) have a token and a head a warp and take the few-token pages, the others 32 tokens and a head.
+    // The first blocks (decoding) have a token and a head a warp and take the few-token pages, the others `chunk` tokens and a head.
     const bool one = (int)blockIdx.x < p.few_blocks;
     const int index = one ? blockIdx.x : blockIdx.x - p.few_blocks, across = one ? p.few_heads : p.pool.heads;
-    const int t_block = index / across * (one ? 1 : 32), head0 = index % across * (one ? W : 1), head1 = min(p.pool.heads, head0 + (one ? W : 1));
+    const int t_block = index / across * (one ? 1 : p.chunk), head0 = index % across * (one ? W : 1), head1 = min(p.pool.heads, head0 + (one ? W : 1));
     const int t_lane = t_block + lane;
-    if (lane < (one ? 1 : 32) && t_lane < p.n_tokens) first = place_of(p, t_lane, mine) && (t_lane == mine.begin || mine.off == 0);
+    if (lane < (one ? 1 : p.chunk) && t_lane < p.n_tokens) first = place_of(p, t_lane, mine) && (t_lane == mine.begin || mine.off == 0);
     if (first) {
         const int run = min(XSV_PAGE - mine.off, mine.end - t_lane);
         few = run <= FEW && mine.off + run < XSV_PAGE;
@@ -148,7 +141,7 @@ __global__ void __launch_bounds__(D, D == 128 ? 5 : 10) page_append_kernel(const
                 const float s = __half2float(hs), z = __half2float(hz);
                 uint32_t c[8];
                 unpack8<T>(v, x);
-                codes8<T>(x, s, __frcp_rn(s), z, c);
+                codes8<T>(x, s, page_inverse(s), z, c);
                 if (live) {
                     // the token's byte of four words: [k = tok / 16][c][g][j = tok % 8 / 2][m], byte 2 (tok % 2) + tok / 8 % 2
                     uint8_t* at = rec + R::V_CODES + (((tok / 16) * (D / 64) + piece / 8) * 32 + (piece % 8) * 4 + tok % 8 / 2) * 16 + 2 * (tok % 2) + tok / 8 % 2;
@@ -196,6 +189,7 @@ __global__ void __launch_bounds__(D, D == 128 ? 5 : 10) page_append_kernel(const
                 uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll 2
                 for (int b = 0; b < 4; ++b) {
+                    if (!__any_sync(0xFFFFFFFFu, mask >> (8 * b) & 1u)) continue;
                     const uint4 v = b == 0 ? raw[0] : b == 1 ? raw[1] : b == 2 ? raw[2] : raw[3];
                     float mn, mx, x[8];
                     range8<T>(v, mn, mx);
@@ -204,7 +198,7 @@ __global__ void __launch_bounds__(D, D == 128 ? 5 : 10) page_append_kernel(const
                     const float s = __half2float(hs), z = __half2float(hz);
                     uint32_t c[8];
                     unpack8<T>(v, x);
-                    codes8<T>(x, s, __frcp_rn(s), z, c);
+                    codes8<T>(x, s, page_inverse(s), z, c);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) w[i] += (c[2 * i] + (c[2 * i + 1] << 4)) << (8 * b);
                     if (piece % 8 == 0 && (mask >> (8 * b) & 1u)) {
@@ -263,7 +257,7 @@ __global__ void __launch_bounds__(D, D == 128 ? 5 : 10) page_append_kernel(const
                 const float f0 = __half2float(s0), f1 = __half2float(s1);
                 reinterpret_cast<float2*>(s_scale)[tid] = make_float2(f0, f1);
                 reinterpret_cast<float2*>(s_zero)[tid] = make_float2(__half2float(z0), __half2float(z1));
-                reinterpret_cast<float2*>(s_inv)[tid] = make_float2(__frcp_rn(f0), __frcp_rn(f1));
+                reinterpret_cast<float2*>(s_inv)[tid] = make_float2(page_inverse(f0), page_inverse(f1));
             }
             __syncthreads();
             // channel c of the piece: step 2 (piece / 4) + c / 4, byte 2 (c % 2) + (c % 4) / 2; row 8 i + g: word i / 2,
@@ -287,7 +281,7 @@ __global__ void __launch_bounds__(D, D == 128 ? 5 : 10) page_append_kernel(const
                 codes8<T>(x1, s.y, inv.y, z.y, c1);
                 const int sh = 4 * (c & 2);                     // byte (c % 4) / 2, and two bytes up for the second channel
 #pragma unroll
-                for (int i = 0; i < 8; ++i) w[i / 2] += (c0[i] + (c1[i] << 16)) << (sh + 4 * (i % 2));
+                for (int i = 0; i < 4; ++i) w[i] += (c0[2 * i] + (c0[2 * i + 1] << 4) + (c1[2 * i] << 16) + (c1[2 * i + 1] << 20)) << sh;
                 if (c & 2) {
                     *reinterpret_cast<uint4*>(rec + R::K_CODES + ((2 * (piece / 4) + c / 4) * 32 + g * 4 + piece % 4) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
                     w[0] = w[1] = w[2] = w[3] = 0;
@@ -410,11 +404,13 @@ extern "C" xsv_status xsv_page_append(const xsv_page_pool* pool, const void* K, 
     p.slot = slot_map; p.seq = token_seq; p.cu = cu_new; p.total = total_len;
     p.n_tokens = n_tokens; p.n_seqs = n_seqs;
     // A block looks for first tokens of pages among 32 new tokens, for one head.  Where most sequences bring a few tokens
-    // (decoding) every token may be one, and a block each takes those that do not fill their page, a warp a head.
+    // (decoding) every token may be one, and a block each takes those that do not fill their page, a warp a head; a page
+    // that one of them fills takes a block some 8 us, so that these are looked for among 8 tokens.
     const bool decode = (long long)n_tokens <= 8LL * n_seqs;
     const int warps = pool->head_dim / 32;
+    p.chunk = decode ? 8 : 32;
     p.few_heads = (pool->kv_heads + warps - 1) / warps;
-    const long long few = decode ? (long long)n_tokens * p.few_heads : 0, blocks = few + (long long)((n_tokens + 31) / 32) * pool->kv_heads;
+    const long long few = decode ? (long long)n_tokens * p.few_heads : 0, blocks = few + (long long)((n_tokens + p.chunk - 1) / p.chunk) * pool->kv_heads;
     if (blocks > 0x7FFFFFFFLL) return XSV_ERR_LIMIT;
     p.few_blocks = (int)few;
     const dim3 grid((unsigned)blocks);

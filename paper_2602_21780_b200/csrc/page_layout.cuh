@@ -56,26 +56,44 @@ template <> __device__ __forceinline__ float2 xsv_unpack2<__nv_bfloat16>(uint32_
     return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
 }
 
-// Scale and offset of a group from its minimum and maximum (already inside +-65504): every operation rounds outwards.
-// 15 * fp16 is exact in float32, so the two float32 roundings never carry the quotient past the fp16 it rounds up to.
+// Scale and offset of a group from its minimum and maximum (already inside +-65504).  The offset is the minimum rounded
+// down to fp16; the scale is the smallest fp16 whose 15-fold (exact in float32) reaches the maximum minus the offset: the
+// nearest fp16 to a fifteenth of that difference (rounded up), or the next one.
 __device__ __forceinline__ void page_params(float mn, float mx, __half& s, __half& z) {
     z = __float2half_rd(mn);
-    s = __float2half_ru(__fdiv_ru(__fsub_ru(mx, __half2float(z)), 15.f));
-    if (__half2float(s) == 0.f) s = __float2half_rn(1.f);
+    const float d = __fsub_ru(mx, __half2float(z));
+    s = __float2half_rn(d * 0.066666670f);
+    unsigned short bits = __half_as_ushort(s);
+    if (__half2float(s) * 15.f < d) ++bits;
+    s = __ushort_as_half(bits ? bits : (unsigned short)0x3C00);       // 1 for a group of one value
 }
-// Codes of x in a group with these parameters: nearest-even of the IEEE quotient (x - z) / s.  Outward rounding keeps the
-// quotient inside [0, 15 + 2^-19], so no clamping is needed.  code_bits() gives float bits whose low four are the code
-// (1.5 * 2^23 + code), from (x - z) * (1 / s), which is within 2^-19 of the quotient, and keeps in `near` the largest distance
-// to an integer that it met: where that exceeds CODE_NEAR, a quotient may lie on the other side of a half-integer
-// and code_bits_exact(), which divides, has to be asked.
-constexpr float CODE_NEAR = 0.49998f;                       // 0.5 - 2^-16 and a little
-__device__ __forceinline__ uint32_t code_bits(float x, float inv_s, float z, float& near) {
-    const float y = __fmul_rn(__fsub_rn(x, z), inv_s), t = __fadd_rn(y, 12582912.f);
-    near = fmaxf(near, fabsf(__fsub_rn(y, __fadd_rn(t, -12582912.f))));
-    return __float_as_uint(t);
+__device__ __forceinline__ float page_inverse(float s) {            // within 2^-23
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+    return r;
 }
-__device__ __forceinline__ uint32_t code_bits_exact(float x, float s, float z) {
-    return __float_as_uint(__fadd_rn(__fdiv_rn(__fsub_rn(x, z), s), 12582912.f));
+// Codes of 8 values with the same parameters: nearest-even of the quotients (x - z) / s.  Outward rounding keeps a quotient
+// inside [0, 15 + 2^-19]; (x - z) * inv is within 2^-18 of it.  Where that is nowhere within 2e-5 of a half-integer its
+// rounding (1.5 * 2^23 added: the integer is in the low bits) is the quotient's; else the remainders of all eight decide, which
+// are exact next to a half-integer.  The mask keeps an infinite or NaN value from its neighbours in a code word.
+__device__ __forceinline__ void page_codes(const float (&x)[8], float s, float inv, float z, uint32_t (&c)[8]) {
+    float d[8], near = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        d[i] = __fsub_rn(x[i], z);
+        const float y = __fmul_rn(d[i], inv), t = __fadd_rn(y, 12582912.f);
+        near = fmaxf(near, fabsf(__fsub_rn(y, __fadd_rn(t, -12582912.f))));
+        c[i] = __float_as_uint(t);
+    }
+    if (near > 0.49998f) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float k = __fadd_rn(__uint_as_float(c[i]), -12582912.f), r2 = 2.f * fmaf(-k, s, d[i]);
+            if (fabsf(r2) > s || (fabsf(r2) == s && (c[i] & 1u))) c[i] += r2 > 0.f ? 1u : 0xFFFFFFFFu;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] &= 15u;
 }
 // minimum and maximum of pairs of 16-bit values
 template <typename T> __device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b);
