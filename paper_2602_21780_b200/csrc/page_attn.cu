@@ -22,6 +22,7 @@
 // warps, so results do not depend on timing.  Each block finds its spans itself by scanning the lengths.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "../../include/xsv.h"
 #include "page_attn.cuh"
@@ -30,7 +31,6 @@
 
 namespace {
 
-constexpr int WARPS = 4, THREADS = WARPS * 32;
 // Probabilities are 2^(x - m + P_BIAS) with m a logit that was the row's maximum when it was last looked for: as long as
 // none exceeds m by more than P_SLACK, m stays (one vote instead of a reduction and a rescale).  At most 2^10, they
 // keep fp16's full significand down to 2^-20 of the row's maximum; times a value scale of at most 16 they stay in range.
@@ -44,12 +44,17 @@ struct Attn : PageAttn {
 // one unnormalised tile: [NT][D / 16][32 lanes] float4, then maxima and sums [8 NT] float2
 template <int D, int NT> struct Part { static constexpr int FLOATS = NT * (D / 16) * 128 + NT * 16; };
 
-// Blocks per multiprocessor and stages per warp: as many warps as the registers allow (the tile's accumulators set
-// them: 12 warps of 168, 8 of 255; head_dim 64: 16 of 128, 12 of 168), as many stages as shared memory then does.
+// Blocks per multiprocessor and stages (page records) per warp: as many warps as the registers allow (the tile's
+// accumulators set them: 16 warps of 128, 12 of 168, 8 of 255), as many stages as shared memory then does.  A tile of 16 rows
+// keeps its query operands in shared memory.  (16 warps of half-page stages and spilled registers at head_dim 128: 178 us
+// instead of 142 for 64 sequences.)
+constexpr int WARPS = 4, THREADS = WARPS * 32;
 template <int D, int NT> struct Shape {
     static constexpr int BLOCKS = D == 64 ? (NT == 1 ? 4 : 3) : (NT == 1 ? 3 : 2);
-    static constexpr int STAGES = D == 64 ? (NT == 1 ? 3 : 4) : (NT == 1 ? 2 : 3);
-    static constexpr size_t SMEM = (size_t)WARPS * STAGES * PageRec<D>::BYTES;
+    static constexpr int STAGES = D == 64 ? (NT == 1 ? 3 : 3) : (NT == 1 ? 2 : 2);
+    static constexpr bool Q_REGS = NT == 1;
+    static constexpr int PER_WARP = STAGES * PageRec<D>::BYTES + (Q_REGS ? 0 : NT * D * 16);
+    static constexpr size_t SMEM = (size_t)WARPS * PER_WARP;
 };
 
 // Bounded: false once the limit has passed.
@@ -129,7 +134,12 @@ __device__ __forceinline__ void advance(const Attn& p, Cursor& c, int rows) {
 template <typename T, int D, int NT>
 __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kernel(const __grid_constant__ Attn p) {
     using R = PageRec<D>;
-    constexpr int ROWS = 8 * NT, KS = D / 16, CT = D / 16, VG = D / 64, STAGES = Shape<D, NT>::STAGES;
+    constexpr int ROWS = 8 * NT, CT = D / 16, VG = D / 64;
+    using S = Shape<D, NT>;
+    constexpr int STAGES = S::STAGES;
+    // fp16 results are worth two more products a page (see where they are taken); at bf16 their effect, 0.0017 instead of
+    // 0.0018 of the result, of which 0.0017 is the output's own rounding, is not
+    constexpr bool FINE = std::is_same<T, __half>::value;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(8) unsigned long long bars[WARPS][STAGES];
     __shared__ int stage_page[WARPS][STAGES];
@@ -202,7 +212,14 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
         }
     }
 
-    uint8_t* ring = smem + wid * STAGES * R::BYTES;
+    uint8_t* ring = smem + wid * S::PER_WARP;
+    // query operands: [n][32 channels] of {operand register 0 of both steps, register 1 of both steps}, this lane's
+    uint4 q_regs[S::Q_REGS ? NT * (D / 32) : 1] = {};
+    uint4* const q_smem = reinterpret_cast<uint4*>(ring + STAGES * R::BYTES) + lane;
+    auto query = [&](int i, uint32_t (&q)[2][2]) {
+        const uint4 x = S::Q_REGS ? q_regs[S::Q_REGS ? i : 0] : q_smem[i * 32];
+        q[0][0] = x.x; q[0][1] = x.y; q[1][0] = x.z; q[1][1] = x.w;
+    };
     // Page record of the step at `ld` into stage `st`, then on to the next step, whose page index is fetched already.  The
     // unfilled page's keys are not in its record.
     Cursor ld = cur;
@@ -242,7 +259,18 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
 
     int stage = 0, parity = 0;
     bool failed = false;
-    uint32_t qf[NT][KS / 2][2][2];                             // [32 channels][operand register][step]
+    // Refills the stage that was left last, and waits for the one that comes now.
+    auto arrive = [&]() {
+        __syncwarp();
+        if (!failed) {
+            issue(stage == 0 ? STAGES - 1 : stage - 1);
+            if (!mbar_try(smem_u32(&bars[wid][stage]), parity) && !mbar_wait_bounded(smem_u32(&bars[wid][stage]), parity)) {
+                failed = true;                                 // nothing is issued any more; what is in flight gets its time
+                for (int i = 0; i < STAGES; ++i) mbar_wait_bounded(smem_u32(&bars[wid][(stage + i) % STAGES]), stage + i < STAGES ? parity : parity ^ 1);
+            }
+        }
+        __syncwarp();
+    };
     float fac[NT][2], m[NT][2], l[NT][2], zs[NT][2][VG], o[NT][CT][4];
     int qpos[NT][2], pos_lo = 0, pos_hi = 0;
     bool whole = false;                                        // the span holds the unit's first step
@@ -288,12 +316,17 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
                 const int e = mx > 0.f ? max((__float_as_int(mx) >> 23) - 128, -126) : 0;
                 const float s1 = pow2i(-(e / 2)), s2 = pow2i(-(e - e / 2));
 #pragma unroll
-                for (int k = 0; k < D / 32; ++k)
+                for (int k = 0; k < D / 32; ++k) {
+                    uint32_t y[4];
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
                         const float2 f = xsv_unpack2<T>(word(raw[k], w));
-                        qf[n][k][w & 1][w >> 1] = pack_h2(f.x * s1 * s2, f.y * s1 * s2);
+                        y[w] = pack_h2(f.x * s1 * s2, f.y * s1 * s2);
                     }
+                    const uint4 x = make_uint4(y[0], y[2], y[1], y[3]);
+                    if (S::Q_REGS) q_regs[S::Q_REGS ? n * (D / 32) + k : 0] = x;
+                    else q_smem[(n * (D / 32) + k) * 32] = x;
+                }
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     const int er = __shfl_sync(0xFFFFFFFFu, e, 4 * (2 * j + c));
@@ -314,19 +347,10 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
             }
         }
         // ---- the step's page
-        __syncwarp();
-        if (!failed) {
-            issue(stage == 0 ? STAGES - 1 : stage - 1);        // the stage that the last step left
-            if (!mbar_try(smem_u32(&bars[wid][stage]), parity) && !mbar_wait_bounded(smem_u32(&bars[wid][stage]), parity)) {
-                failed = true;                                 // nothing is issued any more; what is in flight gets its time
-                for (int i = 0; i < STAGES; ++i) mbar_wait_bounded(smem_u32(&bars[wid][(stage + i) % STAGES]), stage + i < STAGES ? parity : parity ^ 1);
-            }
-        }
-        __syncwarp();
-        const uint8_t* rec = ring + stage * R::BYTES;
+        arrive();
         const int pg = cur.q.p0 + cur.pg, tok0 = pg * XSV_PAGE;
         if (stage_page[wid][stage] && !failed) {
-            float up_lo, up_hi;                                    // what brings the value products' rows g, g + 8 to real units
+            const uint8_t* rec = ring + stage * R::BYTES;
             const bool part = tok0 + XSV_PAGE > cur.q.total;
             const bool mask = tok0 + XSV_PAGE - 1 > pos_lo || part || (p.window > 0 && tok0 <= pos_hi - p.window);
             // logits (in log2 units) are s * f + z, f by row half (i / 2) and column (i % 2)
@@ -339,14 +363,17 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
                 for (int k = 0; k < D / 32; ++k) {
                     const uint4 sc = *reinterpret_cast<const uint4*>(rec + R::K_SCALE + 64 * k + 16 * j);
                     const uint4 ze = *reinterpret_cast<const uint4*>(rec + R::K_ZERO + 64 * k + 16 * j);
+                    uint32_t q[NT][2][2];                          // [operand register][step]
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) query(n * (D / 32) + k, q[n]);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             // the offsets as they lie in memory: words 0, 2 on rows g are the first operand register's channels
                             // of both steps, words 1, 3 on rows g + 8 the second's; each product counts on its rows only
-                            if (k == 0) mma0(qz[n][h], ze.x, ze.y, ze.z, ze.w, qf[n][k][h][0], qf[n][k][h][1]);
-                            else mma(qz[n][h], ze.x, ze.y, ze.z, ze.w, qf[n][k][h][0], qf[n][k][h][1]);
+                            if (k == 0) mma0(qz[n][h], ze.x, ze.y, ze.z, ze.w, q[n][h][0], q[n][h][1]);
+                            else mma(qz[n][h], ze.x, ze.y, ze.z, ze.w, q[n][h][0], q[n][h][1]);
                         }
 #pragma unroll
                     for (int kl = 0; kl < 2; ++kl) {
@@ -355,9 +382,10 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
                         uint32_t b0[NT], b1[NT];
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            b0[n] = hmul2_u(qf[n][k][0][kl], word(sc, 2 * kl));
-                            b1[n] = hmul2_u(qf[n][k][1][kl], word(sc, 2 * kl + 1));
-                            const uint32_t e0 = hfnma2_u(qf[n][k][0][kl], word(sc, 2 * kl), b0[n]), e1 = hfnma2_u(qf[n][k][1][kl], word(sc, 2 * kl + 1), b1[n]);
+                            b0[n] = hmul2_u(q[n][0][kl], word(sc, 2 * kl));
+                            b1[n] = hmul2_u(q[n][1][kl], word(sc, 2 * kl + 1));
+                            if (!FINE) continue;
+                            const uint32_t e0 = hfnma2_u(q[n][0][kl], word(sc, 2 * kl), b0[n]), e1 = hfnma2_u(q[n][1][kl], word(sc, 2 * kl + 1), b1[n]);
                             if (ks == 0) mma0(qz[n][2], MINUS_EIGHTS, MINUS_EIGHTS, MINUS_EIGHTS, MINUS_EIGHTS, e0, e1);
                             else mma(qz[n][2], MINUS_EIGHTS, MINUS_EIGHTS, MINUS_EIGHTS, MINUS_EIGHTS, e0, e1);
                         }
@@ -376,7 +404,7 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
                 for (int n = 0; n < NT; ++n) {
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        z[n][c] = (qz[n][0][c] + qz[n][1][c + 2] + qz[n][2][c]) * fac[n][c];
+                        z[n][c] = (qz[n][0][c] + qz[n][1][c + 2] + (FINE ? qz[n][2][c] : 0.f)) * fac[n][c];
                         f[n][c] = fac[n][c] * 16777216.f;          // 2^24: rows g
                         f[n][c + 2] = fac[n][c] * 1048576.f;       // 2^20: rows g + 8
                     }
@@ -395,12 +423,15 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
                         for (int k = 0; k < D / 32; ++k) {
                             const uint4 a = *reinterpret_cast<const uint4*>(tail + (16 * t) * D + 32 * k);
                             const uint4 b = *reinterpret_cast<const uint4*>(tail + (16 * t + 8) * D + 32 * k);
+                            uint32_t q[NT][2][2];
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) query(n * (D / 32) + k, q[n]);
 #pragma unroll
                             for (int kl = 0; kl < 2; ++kl)
 #pragma unroll
                                 for (int n = 0; n < NT; ++n)
                                     mma(s[n][t], to_h2<T>(word(a, 2 * kl)), to_h2<T>(word(b, 2 * kl)), to_h2<T>(word(a, 2 * kl + 1)),
-                                        to_h2<T>(word(b, 2 * kl + 1)), qf[n][k][0][kl], qf[n][k][1][kl]);
+                                        to_h2<T>(word(b, 2 * kl + 1)), q[n][0][kl], q[n][1][kl]);
                         }
                     }
                 }
@@ -463,22 +494,20 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
                     b[t][n][1] = transpose8(pack_h2(ex2(fmaf(s[n][t][2], f[n][2], off0)), ex2(fmaf(s[n][t][3], f[n][3], off1))));
                 }
             }
-            // ---- value scales of the same tokens in pairs; sum of p (z + 8 s) per 64 channels, and sum of p, as products too
-            uint32_t sp[VG][8];
-            {
-                uint32_t top = 0;
-                float sum[2][NT][4];
-                uint32_t zp[VG][8];
+            // ---- its values
 #pragma unroll
-                for (int v = 0; v < VG; ++v) {
+            for (int v = 0; v < VG; ++v) {
+                // scales and offsets of the same tokens, in pairs
+                uint32_t sp[8], zp[8], top = 0;
+                {
                     const uint8_t* at_s = rec + R::V_SCALE + 128 * v + 32 * j;
                     const uint8_t* at_z = rec + R::V_ZERO + 128 * v + 32 * j;
                     const uint4 s0 = *reinterpret_cast<const uint4*>(at_s), s1 = *reinterpret_cast<const uint4*>(at_s + 16);
                     const uint4 z0 = *reinterpret_cast<const uint4*>(at_z), z1 = *reinterpret_cast<const uint4*>(at_z + 16);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        sp[v][i] = pair_at(s0, s1, i);
-                        zp[v][i] = pair_at(z0, z1, i);
+                        sp[i] = pair_at(s0, s1, i);
+                        zp[i] = pair_at(z0, z1, i);
                     }
                 }
                 if (part) {                                        // places that hold no token: no bits of theirs count
@@ -487,37 +516,30 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
                     for (int i = 0; i < 8; ++i) {
                         const int a = cur.q.total - tok0 - 2 * j - 8 * i;
                         const uint32_t keep = a >= 2 ? 0xFFFFFFFFu : a == 1 ? 0xFFFFu : 0u;
-#pragma unroll
-                        for (int v = 0; v < VG; ++v) { sp[v][i] &= keep; zp[v][i] &= keep; }
+                        sp[i] &= keep;
+                        zp[i] &= keep;
                     }
                 }
 #pragma unroll
-                for (int v = 0; v < VG; ++v)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        zp[v][i] = hfma2_u(sp[v][i], EIGHTS, zp[v][i]);
-                        top = __vmaxu2(top, sp[v][i]);
-                    }
+                for (int i = 0; i < 8; ++i) {
+                    if (FINE) zp[i] = hfma2_u(sp[i], EIGHTS, zp[i]);
+                    top = __vmaxu2(top, sp[i]);
+                }
+                // sum of p z (FINE: z + 8 s) on rows g, sum of p on rows g + 8
+                float sum[NT][4];
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        // rows g: the first 64 channels; rows g + 8: the second, or the sum of p
-                        const uint32_t h0 = VG == 2 ? zp[VG - 1][2 * t] : ONES, h1 = VG == 2 ? zp[VG - 1][2 * t + 1] : ONES;
-                        if (t == 0) mma0(sum[0][n], zp[0][0], h0, zp[0][1], h1, b[0][n][0], b[0][n][1]);
-                        else mma(sum[0][n], zp[0][2 * t], h0, zp[0][2 * t + 1], h1, b[t][n][0], b[t][n][1]);
-                        if (VG == 2) {
-                            if (t == 0) mma0(sum[1][n], ONES, ONES, ONES, ONES, b[0][n][0], b[0][n][1]);
-                            else mma(sum[1][n], ONES, ONES, ONES, ONES, b[t][n][0], b[t][n][1]);
-                        }
+                        if (t == 0) mma0(sum[n], zp[0], ONES, zp[1], ONES, b[0][n][0], b[0][n][1]);
+                        else mma(sum[n], zp[2 * t], ONES, zp[2 * t + 1], ONES, b[t][n][0], b[t][n][1]);
                     }
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        zs[n][c][0] += sum[0][n][c];
-                        if (VG == 2) zs[n][c][VG - 1] += sum[0][n][c + 2];
-                        l[n][c] += VG == 2 ? sum[1][n][c] : sum[0][n][c + 2];
+                        zs[n][c][v] += sum[n][c];
+                        if (v == 0) l[n][c] += sum[n][c + 2];
                     }
                 // Scales beyond 16, or all below 2^-8, are brought to [8, 16) by a power of two (of their bits: they are positive)
                 top = __reduce_max_sync(0xFFFFFFFFu, max(top >> 16, top & 0xFFFFu));
@@ -526,28 +548,23 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
                     e = max((int)(top >> 10) - 18, -15);
                     const uint32_t h = (uint32_t)(15 - e) << 10, down = h | h << 16;
 #pragma unroll
-                    for (int v = 0; v < VG; ++v)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) sp[v][i] = hmul2_u(sp[v][i], down);
+                    for (int i = 0; i < 8; ++i) sp[i] = hmul2_u(sp[i], down);
                 }
-                up_lo = pow2i(24 + e);
-                up_hi = pow2i(20 + e);
-            }
-            // ---- times the value codes around their middle, 8: -8 sum P s, the same for all channels, starts the accumulators (and
-            // z + 8 s stands in for z above), so that neither the rounding of P s nor the tensor cores' truncating
-            // accumulation sees the codes' mean, which is much larger than what is left of it after sum p z.  For the same
-            // reason a page is summed in the tensor cores and the pages in float32 adds, which round (22 000 tokens in one
-            // accumulator, with the mean, were off by 0.6 %).
-#pragma unroll
-            for (int v = 0; v < VG; ++v) {
+                const float up_lo = pow2i(24 + e), up_hi = pow2i(20 + e);          // back to real units: rows g, rows g + 8
+                // Times the value codes.  FINE: around their middle, 8: -8 sum P s, the same for all channels, starts the
+                // accumulators (and z + 8 s stands in for z above), so that neither the rounding of P s nor the tensor cores'
+                // truncating accumulation sees the codes' mean, which is much larger than what is left of it after sum p z.  For
+                // the same reason a page is summed in the tensor cores and the pages in float32 adds, which round (22 000
+                // tokens in one accumulator, with the mean, were off by 0.6 %).
                 float acc[NT][4][4], mid[NT][4];
                 uint32_t ps[4][NT][2];
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
-                        ps[t][n][0] = hmul2_u(b[t][n][0], sp[v][2 * t]);
-                        ps[t][n][1] = hmul2_u(b[t][n][1], sp[v][2 * t + 1]);
+                        ps[t][n][0] = hmul2_u(b[t][n][0], sp[2 * t]);
+                        ps[t][n][1] = hmul2_u(b[t][n][1], sp[2 * t + 1]);
+                        if (!FINE) continue;
                         if (t == 0) mma0(mid[n], MINUS_LO, MINUS_HI, MINUS_LO, MINUS_HI, ps[0][n][0], ps[0][n][1]);
                         else mma(mid[n], MINUS_LO, MINUS_HI, MINUS_LO, MINUS_HI, ps[t][n][0], ps[t][n][1]);
                     }
@@ -558,10 +575,12 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const uint32_t w = word(code, i), x = w >> 8;
+                        const uint32_t a0 = w & 0x000F000Fu, a1 = w & 0x00F000F0u, a2 = x & 0x000F000Fu, a3 = x & 0x00F000F0u;
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            if (t == 0) mma(acc[n][i], w & 0x000F000Fu, w & 0x00F000F0u, x & 0x000F000Fu, x & 0x00F000F0u, ps[t][n][0], ps[t][n][1], mid[n]);
-                            else mma(acc[n][i], w & 0x000F000Fu, w & 0x00F000F0u, x & 0x000F000Fu, x & 0x00F000F0u, ps[t][n][0], ps[t][n][1]);
+                            if (t > 0) mma(acc[n][i], a0, a1, a2, a3, ps[t][n][0], ps[t][n][1]);
+                            else if (FINE) mma(acc[n][i], a0, a1, a2, a3, ps[0][n][0], ps[0][n][1], mid[n]);
+                            else mma0(acc[n][i], a0, a1, a2, a3, ps[0][n][0], ps[0][n][1]);
                         }
                     }
                 }
@@ -646,16 +665,21 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) page_attn_merge_kernel(const
             ml = make_float4(m0, ml.y * a0 + y.y * b0, m1, ml.w * a1 + y.w * b1);
         }
     };
-    const int w_end = min(workers, (int)(blockIdx.x + 1) * 8);
-    for (int w = max(1, (int)blockIdx.x * 8); w < w_end; ++w) {
-        const int4 d = p.desc[w];
-        if (d.w == 0) continue;                                 // the same for the whole block
+    const int w0 = blockIdx.x * 8;
+    int4 mine = make_int4(0, 0, 0, 0);
+    if (lane < 8 && w0 + lane < workers) mine = p.desc[w0 + lane];
+    for (uint32_t todo = __ballot_sync(0xFFFFFFFFu, mine.w > 0); todo; todo &= todo - 1) {     // the same for the whole block
+        const int from = __ffs(todo) - 1, w = w0 + from;
+        const int4 d = make_int4(__shfl_sync(0xFFFFFFFFu, mine.x, from), __shfl_sync(0xFFFFFFFFu, mine.y, from),
+                                 __shfl_sync(0xFFFFFFFFu, mine.z, from), __shfl_sync(0xFFFFFFFFu, mine.w, from));
         Acc acc;
 #pragma unroll 4
         for (int i = wid; i < d.w; i += MERGE_WARPS) {
             const float* part = p.part + (size_t)(i == 0 ? 2 * (w - 1) + 1 : 2 * (w + i - 1)) * PF;
             acc.add(reinterpret_cast<const float4*>(part)[(n * CT + ct) * 32 + lane], *reinterpret_cast<const float4*>(part + NT * CT * 128 + 2 * r0));
         }
+        const Seq q = seq_of(p, d.x, ROWS);
+        const int n_rows = q.new_ * p.group, t0 = min(max(p.cu[d.x], 0), p.n_tokens);
         __syncthreads();                                        // the last unit's reads of the shared arrays
         s_o[wid][lane] = acc.o;
         s_ml[wid][lane] = acc.ml;
@@ -663,8 +687,6 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) page_attn_merge_kernel(const
         if (wid != 0) continue;
 #pragma unroll
         for (int i = 1; i < MERGE_WARPS; ++i) acc.add(s_o[i][lane], s_ml[i][lane]);
-        const Seq q = seq_of(p, d.x, ROWS);
-        const int n_rows = q.new_ * p.group, t0 = min(max(p.cu[d.x], 0), p.n_tokens);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const int r = d.z * ROWS + r0 + c;
@@ -680,9 +702,9 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) page_attn_merge_kernel(const
 // ------------------------------------------------------------------ host side
 constexpr size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 
-int grid_of(int head_dim, int nt) {
-    return xsv_sm_count() * (head_dim == 64 ? (nt == 1 ? Shape<64, 1>::BLOCKS : Shape<64, 2>::BLOCKS)
-                                            : (nt == 1 ? Shape<128, 1>::BLOCKS : Shape<128, 2>::BLOCKS));
+template <int D, int NT> int workers_at() { return xsv_sm_count() * Shape<D, NT>::BLOCKS * WARPS; }
+int workers_of(int head_dim, int nt) {
+    return head_dim == 64 ? (nt == 1 ? workers_at<64, 1>() : workers_at<64, 2>()) : (nt == 1 ? workers_at<128, 1>() : workers_at<128, 2>());
 }
 // 8 query rows a tile where a head has no more, else 16
 int tiles_of(int max_new, int group) { return (long long)max_new * group <= 8 ? 1 : 2; }
@@ -695,7 +717,7 @@ bool many_rows(int max_new, int group) { return (long long)max_new * group > FEW
 
 size_t workspace_of(int n_tokens, int n_seqs, int max_new, int group, int head_dim) {
     const int nt = tiles_of(max_new, group);
-    const size_t workers = (size_t)grid_of(head_dim, nt) * WARPS;
+    const size_t workers = (size_t)workers_of(head_dim, nt);
     const size_t pf = (size_t)nt * (head_dim / 16) * 128 + nt * 16;
     const size_t few = align256(workers * sizeof(int4)) + align256(2 * workers * pf * sizeof(float));
     return few + (many_rows(max_new, group) ? xsv_page_tc5_workspace(n_tokens, n_seqs, group, head_dim) : 0);
@@ -711,11 +733,11 @@ template <typename T, int D, int NT> cudaError_t launch(Attn& p, cudaStream_t st
         if (e != cudaSuccess) return e;
         ready.set(dev, 1);
     }
-    const int grid = grid_of(D, NT);
+    const int grid = xsv_sm_count() * Shape<D, NT>::BLOCKS, workers = workers_at<D, NT>();
     cudaError_t e = xsv_launch_dep(kernel, dim3(grid), dim3(THREADS), smem, st, p);
     if (e != cudaSuccess) return e;
     xsv_count_launch(1);
-    e = xsv_launch_dep(page_attn_merge_kernel<T, D, NT>, dim3((grid * WARPS + 7) / 8, NT * (D / 16)), dim3(MERGE_WARPS * 32), 0, st, p, grid * WARPS);
+    e = xsv_launch_dep(page_attn_merge_kernel<T, D, NT>, dim3((workers + 7) / 8, NT * (D / 16)), dim3(MERGE_WARPS * 32), 0, st, p, workers);
     if (e == cudaSuccess) xsv_count_launch(1);
     return e;
 }
@@ -752,7 +774,7 @@ extern "C" xsv_status xsv_page_attention(const xsv_page_pool* pool, const void* 
     if ((long long)max_new * group > 1LL << 30 || (long long)table_width * XSV_PAGE > 1LL << 30) return XSV_ERR_LIMIT;
     if (workspace_bytes < workspace_of(n_tokens, n_seqs, max_new, group, pool->head_dim)) return XSV_ERR_ARG;
     p.Q = Q; p.out = out; p.table = block_table; p.cu = cu_new; p.total = total_len; p.q_stride = q_stride;
-    const size_t workers = (size_t)grid_of(pool->head_dim, nt) * WARPS, pf = (size_t)nt * (pool->head_dim / 16) * 128 + nt * 16;
+    const size_t workers = (size_t)workers_of(pool->head_dim, nt), pf = (size_t)nt * (pool->head_dim / 16) * 128 + nt * 16;
     p.desc = (int4*)workspace;
     p.part = (float*)((char*)workspace + align256(workers * sizeof(int4)));
     void* const more = (char*)p.part + align256(2 * workers * pf * sizeof(float));
