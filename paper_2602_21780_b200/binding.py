@@ -1,5 +1,6 @@
 """ctypes binding of the xsv C-ABI library (include/xsv.h): argument
-marshalling only.  Device tensors are passed as raw pointers; every step of
+marshalling only (for the page operators, whose kernels can be shorter than a
+ctypes call, by a compiled module beside it).  Device tensors are passed as raw pointers; every step of
 the path runs in the library's CUDA kernels.  Loading fails loudly when the
 shared library has not been built (there is no fallback of any kind)."""
 from __future__ import annotations
@@ -12,6 +13,7 @@ import numpy as np
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libxsv.so")
+PAGES_PATH = os.path.join(_HERE, "xsv_pages.so")
 
 XSV_OK = 0
 F16, BF16 = 0, 1
@@ -307,6 +309,7 @@ def kernel_launches():
 # stream; with `stream`, outputs and workspaces are allocated for that stream.  Nothing synchronises.
 
 class _PagePool(C.Structure):
+    """xsv_page_pool, for calls of the C entry points themselves."""
     _fields_ = [("records", C.c_void_p), ("k_tail", C.c_void_p), ("n_pages", C.c_longlong), ("max_seqs", C.c_int),
                 ("kv_heads", C.c_int), ("head_dim", C.c_int), ("dtype", C.c_int)]
 
@@ -315,71 +318,45 @@ PagePlan = collections.namedtuple("PagePlan", "cu_new total_len slot_map token_s
 PagePlan.__doc__ = """What page_plan() says of a step (see xsv_page_plan); ring_state is the next step's."""
 
 
-def _on_device(call, first, stream):
-    """Runs call(stream pointer) with the tensor's device current and, if a stream is given, that stream current."""
+_pages = None
+
+
+def _load_pages():
+    """The module that checks the tensors and makes the calls (csrc/page_binding.cpp); like the library itself it is loaded
+    once and has no fallback."""
+    global _pages
+    if _pages is None:
+        import importlib.machinery
+        import importlib.util
+
+        import torch  # noqa: F401  (the module links to its libraries)
+        lib = load()
+        if not os.path.exists(PAGES_PATH):
+            raise RuntimeError(f"xsv: {PAGES_PATH} is missing -- build it with __graft_entry__.build(); there is no fallback path")
+        spec = importlib.util.spec_from_loader("xsv_pages", importlib.machinery.ExtensionFileLoader("xsv_pages", PAGES_PATH))
+        mod = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(mod)
+        mod.bind(*[C.cast(getattr(lib, "xsv_" + n), C.c_void_p).value for n in
+                   ("qk_norm_rope", "page_plan", "page_append", "page_read", "page_attention", "page_attention_workspace")])
+        _pages = mod
+    return _pages
+
+
+def _on(stream, first):
+    """The context in which `stream` is the current stream of the tensors' device."""
     import torch
-    dev = first.get_device()
-    if dev < 0:
+    if not first.is_cuda:
         raise ValueError("xsv: CUDA tensors are needed")
-    if stream is not None:
-        if stream.device != first.device:
-            raise ValueError("xsv: the stream belongs to another device than the tensors")
-        with torch.cuda.stream(stream):
-            return call(stream.cuda_stream)
-    if dev != torch.cuda.current_device():
-        with torch.cuda.device(dev):
-            return call(torch.cuda.current_stream(dev).cuda_stream)
-    return call(torch._C._cuda_getCurrentRawStream(dev))     # current_stream(dev).cuda_stream without the wrapper object
+    if stream.device != first.device:
+        raise ValueError("xsv: the stream belongs to another device than the tensors")
+    return torch.cuda.stream(stream)
 
 
-# Checks of the arguments.  They cost more host time than a small kernel runs, so each is one pass of plain comparisons.
-def _tensor(t, name, dtype, dev, shape):
-    """The address of a contiguous tensor of this type, device index and shape."""
-    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"xsv: {name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on device {dev}, "
-                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr()
-
-
-def _like(t):
-    """Uninitialised contiguous tensor of t's shape."""
-    import torch
-    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
-
-
-def _list(t, name, dev):
-    """The address of an int32 list, or table, of any length."""
-    import torch
-    if t.dtype is not torch.int32 or t.get_device() != dev or not t.is_contiguous():
-        raise ValueError(f"xsv: {name} must be a contiguous int32 tensor on device {dev}, not {t.dtype} on {t.device}")
-    return t.data_ptr()
-
-
-def _rows(t, name, dtype, dev, shape):
-    """Rows [tokens, heads, head_dim] whose heads are contiguous, at any stride: (address, stride in elements)."""
-    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape or len(shape) != 3:
-        raise ValueError(f"xsv: {name} must be a {dtype} tensor [tokens, heads, head_dim] of shape {tuple(shape)} on device {dev}, "
-                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
-    n, h, d = shape
-    st, sh, sd = t.stride()
-    if n and (sd != 1 or (sh != d and h > 1)):
-        raise ValueError(f"xsv: {name} needs contiguous heads and channels")
-    return t.data_ptr(), st if n > 1 else h * d
-
-
-def _pool(pages, k_tail):
-    import torch
-    if pages.dim() != 3 or k_tail.dim() != 5:
-        raise ValueError("xsv: pages are [pages, kv_heads, 72 * head_dim], k_tail is [sequences, 2, kv_heads, 64, head_dim]")
-    (n, h, b), (seqs, _, _, _, d), dev = pages.shape, k_tail.shape, pages.get_device()
-    return _PagePool(_tensor(pages, "pages", torch.uint8, dev, (n, h, 72 * d)),
-                     _tensor(k_tail, "k_tail", k_tail.dtype, dev, (seqs, 2, h, PAGE_TOKENS, d)), n, seqs, h, d, _dtype_code(k_tail))
-
-
-def _table(t, dev, seqs):
-    if t.dim() != 2 or t.shape[0] != seqs:
-        raise ValueError(f"xsv: block_table has shape {tuple(t.shape)}, expected a row for each of {seqs} sequences")
-    return _list(t, "block_table", dev)
+def _done(result, where):
+    """What a call of the module gave; an int is the status of a call that the library refused."""
+    if result.__class__ is int:
+        _check(result, where)
+    return result
 
 
 def page_pool(n_pages, max_seqs, kv_heads, head_dim, dtype, device="cuda"):
@@ -395,115 +372,50 @@ def qk_norm_rope(q, k, v=None, *, norm=None, q_weight=None, q_bias=None, k_weigh
     normalised, rotated and laid out (q, k, v), [n, heads, d] or, with head_major, [heads, n, d].  norm: None, "rms",
     "layer"; rope: None, "half", "pairs", "2d" with inv_freq float32 [rotary_dim / 2] ([d / 4] for "2d") and positions
     int32 [n] ([n, 2])."""
-    import torch
     if norm not in NORMS or rope not in ROPES:
         raise ValueError(f"xsv: norm {norm!r} or rope {rope!r} is unknown")
-
-    def call(st):
-        dt, dev, (n, hq, d), hk = q.dtype, q.get_device(), q.shape, k.shape[1]
-        qp, qs = _rows(q, "q", dt, dev, (n, hq, d))
-        kp, ks = _rows(k, "k", dt, dev, (n, hk, d))
-        vp, vs = _rows(v, "v", dt, dev, (n, hk, d)) if v is not None else (None, 0)
-        qw, qb, kw, kb = [None if t is None else _tensor(t, "weight", dt, dev, (d,)) for t in (q_weight, q_bias, k_weight, k_bias)]
-        code, rot, fp, pp = ROPES[rope], 0, None, None
-        if code:
-            if inv_freq is None or positions is None:
-                raise ValueError("xsv: rope needs inv_freq and positions")
-            nf = inv_freq.shape[0] if code != 3 else d // 4
-            rot = d if code == 3 else 2 * nf
-            fp = _tensor(inv_freq, "inv_freq", torch.float32, dev, (nf,))
-            pp = _tensor(positions, "positions", torch.int32, dev, (n, 2) if code == 3 else (n,))
-        qo = q.new_empty((hq, n, d)) if head_major else _like(q)
-        ko = q.new_empty((hk, n, d)) if head_major else _like(k)
-        vo = torch.empty_like(ko) if v is not None else None
-        _check(load().xsv_qk_norm_rope(qp, kp, vp, qs, ks, vs, n, hq, hk, d, _dtype_code(q), NORMS[norm], qw, qb, kw, kb, eps,
-                                       code, rot, fp, pp, 1 if head_major else 0, qo.data_ptr(), ko.data_ptr(),
-                                       None if vo is None else vo.data_ptr(), st), "xsv_qk_norm_rope")
-        return (qo, ko) if vo is None else (qo, ko, vo)
-
-    if q.dim() != 3 or k.dim() != 3:
-        raise ValueError("xsv: q and k are [tokens, heads, head_dim]")
-    return _on_device(call, q, stream)
+    args = (q, k, v, NORMS[norm], q_weight, q_bias, k_weight, k_bias, eps, ROPES[rope], inv_freq, positions, head_major)
+    if stream is None:
+        return _done((_pages or _load_pages()).norm_rope(*args), "xsv_qk_norm_rope")
+    with _on(stream, q):
+        return _done(_load_pages().norm_rope(*args), "xsv_qk_norm_rope")
 
 
 def page_plan(cached_len, new_len, block_table, free_ring, ring_state, max_tokens, stream=None):
     """xsv_page_plan: int32 CUDA tensors cached_len, new_len [sequences], block_table [sequences, width] and free_ring
     [pages] (both updated in place), ring_state [2 or more] -> PagePlan."""
-    import torch
-
-    def call(st):
-        i32, dev, n = torch.int32, cached_len.get_device(), cached_len.shape[0]
-        if ring_state.dim() != 1 or ring_state.shape[0] < 2 or free_ring.dim() != 1 or max_tokens < 0:
-            raise ValueError("xsv: ring_state holds head and count, free_ring is a list; max_tokens is not negative")
-        one = cached_len.new_empty(4 + (n + 1) + n + 3 * max_tokens)      # one allocation for all outputs
-        state, cu, total, slot, seq, pos = one.split_with_sizes((4, n + 1, n, max_tokens, max_tokens, max_tokens))
-        at = one.data_ptr()
-        cu_at = at + 16
-        total_at = cu_at + 4 * (n + 1)
-        slot_at = total_at + 4 * n
-        _check(load().xsv_page_plan(_tensor(cached_len, "cached_len", i32, dev, (n,)), _tensor(new_len, "new_len", i32, dev, (n,)), n,
-                                    _table(block_table, dev, n), block_table.shape[1], _list(free_ring, "free_ring", dev),
-                                    free_ring.shape[0], _list(ring_state, "ring_state", dev), at, cu_at, total_at, slot_at,
-                                    slot_at + 4 * max_tokens, slot_at + 8 * max_tokens, max_tokens, st), "xsv_page_plan")
-        return PagePlan(cu, total, slot, seq, pos, state)
-
-    return _on_device(call, cached_len, stream)
+    args = (cached_len, new_len, block_table, free_ring, ring_state, max_tokens)
+    if stream is None:
+        return PagePlan._make(_done((_pages or _load_pages()).plan(*args), "xsv_page_plan"))
+    with _on(stream, cached_len):
+        return PagePlan._make(_done(_load_pages().plan(*args), "xsv_page_plan"))
 
 
 def page_append(pages, k_tail, K, V, slot_map, token_seq, cu_new, total_len, stream=None):
     """xsv_page_append: K, V [n, kv_heads, d] (rows at any stride) into the pool, by the plan's arrays."""
-    import torch
-
-    def call(st):
-        pool, dev, n, seqs = _pool(pages, k_tail), pages.get_device(), K.shape[0], total_len.shape[0]
-        shape = (n, pool.kv_heads, pool.head_dim)
-        kp, ks = _rows(K, "K", k_tail.dtype, dev, shape)
-        vp, vs = _rows(V, "V", k_tail.dtype, dev, shape)
-        if slot_map.shape[0] < n or token_seq.shape[0] < n:
-            raise ValueError("xsv: the plan lists fewer tokens than K and V hold")
-        _check(load().xsv_page_append(C.byref(pool), kp, vp, ks, vs, n, _list(slot_map, "slot_map", dev),
-                                      _list(token_seq, "token_seq", dev), _tensor(cu_new, "cu_new", torch.int32, dev, (seqs + 1,)),
-                                      _tensor(total_len, "total_len", torch.int32, dev, (seqs,)), seqs, st), "xsv_page_append")
-
-    _on_device(call, pages, stream)
+    args = (pages, k_tail, K, V, slot_map, token_seq, cu_new, total_len)
+    if stream is None:
+        _done((_pages or _load_pages()).append(*args), "xsv_page_append")
+        return
+    with _on(stream, pages):
+        _done(_load_pages().append(*args), "xsv_page_append")
 
 
 def page_read(pages, k_tail, block_table, total_len, token_seq, positions, stream=None):
     """xsv_page_read: the tokens (token_seq[i], positions[i]) as values, (K, V) [rows, kv_heads, d]."""
-    import torch
-
-    def call(st):
-        pool, dev, i32, n, seqs = _pool(pages, k_tail), pages.get_device(), torch.int32, token_seq.shape[0], total_len.shape[0]
-        K = k_tail.new_empty((n, pool.kv_heads, pool.head_dim))
-        V = torch.empty_like(K)
-        _check(load().xsv_page_read(C.byref(pool), _table(block_table, dev, seqs), block_table.shape[1],
-                                    _tensor(total_len, "total_len", i32, dev, (seqs,)), seqs,
-                                    _tensor(token_seq, "token_seq", i32, dev, (n,)), _tensor(positions, "positions", i32, dev, (n,)), n,
-                                    K.data_ptr(), V.data_ptr(), st), "xsv_page_read")
-        return K, V
-
-    return _on_device(call, pages, stream)
+    args = (pages, k_tail, block_table, total_len, token_seq, positions)
+    if stream is None:
+        return _done((_pages or _load_pages()).read(*args), "xsv_page_read")
+    with _on(stream, pages):
+        return _done(_load_pages().read(*args), "xsv_page_read")
 
 
 def page_attention(Q, pages, k_tail, block_table, cu_new, total_len, max_new, *, scale=None, window=0, out=None, stream=None):
     """xsv_page_attention: Q [n, q_heads, d] (rows at any stride), new tokens of all sequences in a row -> out
     [n, q_heads, d].  max_new: the most new tokens of a sequence.  Rows behind the last sequence are not written: they
     keep what `out` held, and hold nothing defined if it was not given."""
-    import torch
-
-    def call(st):
-        pool, dev, i32, seqs, lib = _pool(pages, k_tail), pages.get_device(), torch.int32, total_len.shape[0], load()
-        n, heads, hkv, d = *Q.shape[:2], pool.kv_heads, pool.head_dim
-        qp, qs = _rows(Q, "Q", k_tail.dtype, dev, (n, heads, d))
-        to = out if out is not None else _like(Q)
-        need = lib.xsv_page_attention_workspace(n, seqs, max_new, heads, hkv, d)
-        space = pages.new_empty(need)
-        _check(lib.xsv_page_attention(C.byref(pool), qp, qs, n, heads, _table(block_table, dev, seqs), block_table.shape[1],
-                                      _tensor(cu_new, "cu_new", i32, dev, (seqs + 1,)), _tensor(total_len, "total_len", i32, dev, (seqs,)),
-                                      seqs, max_new, d ** -0.5 if scale is None else scale, window,
-                                      _tensor(to, "out", Q.dtype, dev, (n, heads, d)), space.data_ptr(), need, st), "xsv_page_attention")
-        return to
-
-    if Q.dim() != 3:
-        raise ValueError("xsv: Q is [tokens, heads, head_dim]")
-    return _on_device(call, pages, stream)
+    args = (Q, pages, k_tail, block_table, cu_new, total_len, max_new, scale, window, out)
+    if stream is None:
+        return _done((_pages or _load_pages()).attention(*args), "xsv_page_attention")
+    with _on(stream, pages):
+        return _done(_load_pages().attention(*args), "xsv_page_attention")

@@ -413,6 +413,101 @@ def test_pages_behind_four_gigabytes():
         assert np.all(np.abs(host(V[i]) - ref) <= HALF[sv.dt] * np.abs(ref) * 1.001)
 
 
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("d,hq,hkv", [(64, 4, 4), (64, 12, 1), (128, 8, 2), (128, 5, 5)])
+def test_attention_of_a_long_chunk_shared_by_many_blocks(dtype, d, hq, hkv):
+    sv = Server(1, hkv, d, dtype, pages=70, width=64, seed=d + hq)
+    sv.step([3001])
+    for new in (700, 65, 258):
+        plan = sv.step([new])
+        sv.check_attention(plan, [new], hq)
+        sv.check_attention(plan, [new], hq, window=500)
+
+
+def test_attention_of_decoding_and_prompt_sequences_in_one_call():
+    sv = Server(6, 2, 64, "bf16", pages=80, width=24, seed=21)
+    sv.step([500, 3, 64, 1000, 0, 0])
+    for new in ([1, 400, 2, 90, 0, 1], [1, 1, 300, 1, 20, 17], [33, 16, 17, 1, 64, 65]):
+        plan = sv.step(new, pad=5)
+        n = sum(new) + 5
+        out = torch.full((n, 8, 64), 7.0, device="cuda", dtype=sv.dt)
+        q = sv.rnd(n, 8, 64).to(sv.dt)
+        sv.check_attention(plan, new, 8, q=q, out=out, max_new=500)
+        assert bool((out[-5:] == 7).all())
+        again = binding.page_attention(q, sv.pages, sv.tail, sv.table, plan.cu_new, plan.total_len, max(new))
+        assert torch.equal(again[:-5], out[:-5])             # the bound on the new tokens changes nothing
+
+
+def test_long_chunks_of_sequences_that_hold_nothing_or_miss_pages():
+    sv = Server(2, 1, 64, "fp16", pages=8, width=6)
+    plan = sv.step([300, 0])
+    q = sv.rnd(300, 2, 64).to(sv.dt)
+    out = binding.page_attention(q, sv.pages, sv.tail, sv.table, ints([0, 0, 300]), ints([300, 0]), 300)
+    assert not out.any()
+    out = binding.page_attention(q, sv.pages, sv.tail, sv.table, ints([0, 300, 300]), ints([100, 0]), 300)
+    assert not out[:200].any() and out[200:].any()
+    # without its second page, a sequence sees the others; rows before it see the first alone
+    table = sv.table.clone()
+    table[0, 1] = -1
+    out = host(binding.page_attention(q, sv.pages, sv.tail, table, plan.cu_new, plan.total_len, 300))
+    r = sv.ref[0][0]
+    qh, keep = host(q), np.r_[0:64, 128:300]
+    for i in (0, 63, 64, 127, 128, 299):
+        at = keep[keep <= i]
+        w = np.exp(r.k[at] @ qh[i].T / 8 - (r.k[at] @ qh[i].T / 8).max(0))
+        ref = (w / w.sum(0)).T @ r.v[at]
+        assert np.abs(out[i] - ref).max() <= 0.02 * np.abs(ref).max()
+    table[0, :] = 8
+    assert not binding.page_attention(q, sv.pages, sv.tail, table, plan.cu_new, plan.total_len, 300).any()
+
+
+def test_long_chunks_repeat_bit_for_bit_and_from_a_graph():
+    sv = Server(3, 2, 128, "bf16", pages=80, width=40, seed=13)
+    sv.step([2000, 30, 0])
+    new = [300, 200, 90]
+    plan = sv.step(new)
+    q = sv.rnd(590, 8, 128).to(sv.dt)
+    want = sv.check_attention(plan, new, 8, q=q)
+    for _ in range(3):
+        assert torch.equal(want, binding.page_attention(q, sv.pages, sv.tail, sv.table, plan.cu_new, plan.total_len, 300))
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        out = binding.page_attention(q, sv.pages, sv.tail, sv.table, plan.cu_new, plan.total_len, 300)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(want, out)
+
+
+def test_append_of_many_decoding_sequences_beside_a_prompt():
+    n = 41
+    sv = Server(n, 2, 128, "bf16", pages=140, width=40, seed=15)
+    sv.step((np.arange(n) * 7 % 130).tolist())
+    for _ in range(3):
+        sv.step([600 if s == 20 else 1 + s % 9 for s in range(n)], pad=2)
+        sv.check_state()
+    sv.step([1] * n)
+    sv.check_state()
+
+
+def test_append_keeps_a_value_that_is_not_finite_from_its_neighbours():
+    for dtype in ("fp16", "bf16"):
+        for bad in (float("inf"), float("-inf"), float("nan")):
+            dt = DT[dtype]
+            k = torch.randn(64, 1, 64, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).to(dt)
+            ref = orc.Sequence(64)
+            ref.append(host(k[:, 0]), host(k[:, 0]))
+            k[5, 0, 7] = bad
+            plan = binding.page_plan(ints([0]), ints([64]), ints([[-1]]), ints([0]), ints([0, 1]), 64)
+            pages, tail = binding.page_pool(1, 1, 1, 64, dt)
+            binding.page_append(pages, tail, k, k, plan.slot_map, plan.token_seq, plan.cu_new, plan.total_len)
+            got_k, got_v = orc.read_record(pages[0, 0].cpu().numpy(), 64)
+            channels, tokens = np.arange(64) != 7, np.arange(64) != 5
+            assert np.array_equal(got_k[:, channels], ref.k[:, channels]) and np.array_equal(got_v[tokens], ref.v[tokens])
+
+
 # ------------------------------------------------------------------------------------------------ together
 def test_a_serving_step_captured_and_replayed_on_other_streams():
     # norm + rotation -> append -> attention of a decode step, captured; lengths live on the device, so one graph serves
