@@ -42,7 +42,7 @@ template <typename T> __device__ __forceinline__ void unpack4(const uint2& w, fl
 
 constexpr int THREADS = 128, FLIGHT = 2;      // FLIGHT: rows of a lane group in flight
 
-template <typename T, int D, int ROPE, int NORM>
+template <typename T, int D, int ROPE, int NORM, bool BIAS>
 __global__ void __launch_bounds__(THREADS, 8) qk_norm_rope_kernel(const __grid_constant__ NormRope p) {
     constexpr int L = D / 8, GROUPS = THREADS / L;
     __shared__ float2 cs[2][D / 2];
@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(THREADS, 8) qk_norm_rope_kernel(const __grid_c
         f = part * half + 4 * i;
     }
     xsv_dep_sync();
-    uint2 wgt[2][2], bias[2][2];                            // [q, k][piece], 16-bit
+    uint2 wgt[2][2], bias[2][2];                            // [q, k][piece], 16-bit; BIAS: there is one (its registers cost 7 %)
     if (NORM != XSV_NORM_NONE) {
         const uint32_t one = xsv_pack2<T>(1.f, 1.f);
 #pragma unroll
@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(THREADS, 8) qk_norm_rope_kernel(const __grid_c
                 wgt[s][0] = *reinterpret_cast<const uint2*>((const T*)p.w[s] + ca);
                 wgt[s][1] = *reinterpret_cast<const uint2*>((const T*)p.w[s] + cb);
             }
-            if (p.b[s]) {
+            if (BIAS && p.b[s]) {
                 bias[s][0] = *reinterpret_cast<const uint2*>((const T*)p.b[s] + ca);
                 bias[s][1] = *reinterpret_cast<const uint2*>((const T*)p.b[s] + cb);
             }
@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(THREADS, 8) qk_norm_rope_kernel(const __grid_c
             float w[8], b[8];
             if (NORM != XSV_NORM_NONE && part < 2) {
                 unpack4<T>(wgt[part][0], w); unpack4<T>(wgt[part][1], w + 4);
-                unpack4<T>(bias[part][0], b); unpack4<T>(bias[part][1], b + 4);
+                if (BIAS) { unpack4<T>(bias[part][0], b); unpack4<T>(bias[part][1], b + 4); }
             }
             // two rows of the group at a time; every lane of the warp takes part in the shuffles, whatever its row
             for (int base = h0; base < heads; base += FLIGHT * step) {
@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(THREADS, 8) qk_norm_rope_kernel(const __grid_c
                             for (int o = L / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
                             const float inv = rsqrtf(ss * (1.f / D) + p.eps);
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) v[i] = fmaf(v[i] * inv, w[i], b[i]);
+                            for (int i = 0; i < 8; ++i) v[i] = BIAS ? fmaf(v[i] * inv, w[i], b[i]) : v[i] * inv * w[i];
                         }
                         if (ROPE != XSV_ROPE_NONE) {
 #pragma unroll
@@ -187,12 +187,13 @@ cudaError_t launch(const NormRope& p, int norm, int rope, cudaStream_t st) {
     // through its share of them.
     const dim3 grid(std::min(p.n_tokens, full), p.n_tokens >= 2 * xsv_sm_count() ? 1 : (most + groups - 1) / groups);
     auto go = [&](auto kernel) { return xsv_launch_dep(kernel, grid, dim3(THREADS), 0, st, p); };
+    const bool bias = p.b[0] || p.b[1];
     auto with = [&](auto rope_c) {
         constexpr int ROPE = decltype(rope_c)::value;
         switch (norm) {
-            case XSV_NORM_RMS: return go(qk_norm_rope_kernel<T, D, ROPE, XSV_NORM_RMS>);
-            case XSV_NORM_LAYER: return go(qk_norm_rope_kernel<T, D, ROPE, XSV_NORM_LAYER>);
-            default: return go(qk_norm_rope_kernel<T, D, ROPE, XSV_NORM_NONE>);
+            case XSV_NORM_RMS: return bias ? go(qk_norm_rope_kernel<T, D, ROPE, XSV_NORM_RMS, true>) : go(qk_norm_rope_kernel<T, D, ROPE, XSV_NORM_RMS, false>);
+            case XSV_NORM_LAYER: return bias ? go(qk_norm_rope_kernel<T, D, ROPE, XSV_NORM_LAYER, true>) : go(qk_norm_rope_kernel<T, D, ROPE, XSV_NORM_LAYER, false>);
+            default: return go(qk_norm_rope_kernel<T, D, ROPE, XSV_NORM_NONE, false>);
         }
     };
     switch (rope) {
