@@ -11,15 +11,22 @@
 //     channels of O);
 //   - P^T comes out of S^T by one movmatrix per 8 x 8 block, O^T leaves with 8 consecutive channels a lane.
 // q is scaled by a power of two per row so that its largest element lies in [2, 4): with s <= 8734, q s never leaves fp16,
-// and elements below 2^-14 lose at most 2^-25 absolutely.  P s is scaled by a power of two per page, from the page's largest
-// value scale, so that it uses fp16's range whatever the values' magnitude.  Rounding q s, P s and the result
-// to fp16 / the output type are the only roundings below float32; sums, maxima and the output accumulate in float32.
+// and elements below 2^-14 lose at most 2^-25 absolutely.  s is scaled by a power of two per page where that keeps P s inside
+// fp16's range whatever the values' magnitude.  The roundings below float32 are those of q s, P and P s to fp16 (the tensor
+// cores' operands; 2^-12 of a factor on average, for fp16 results taken around the codes' middle) and of the result; sums,
+// maxima and the output accumulate in float32.
 //
 // Work split.  A unit is (sequence, key/value head, tile of 8 NT query rows); its pages are the steps.  All steps of all
 // units are dealt in equal contiguous spans to the warps of the grid, so ragged lengths and few sequences fill the GPU
 // alike; a warp works alone (own ring of page records in shared memory, filled by bulk copies, own softmax state), no
 // block-wide barrier in the loop.  A unit shared by several warps is merged by a second kernel in the order of the
 // warps, so results do not depend on timing.  Each block finds its spans itself by scanning the lengths.
+//
+// Measured.  64 sequences of 900 to 16 000 tokens, one new token each, 32 query and 8 key/value heads of 128, bf16: 127 us,
+// 4.95 TB/s of 6.57 (first version 159).  Without its arithmetic this kernel takes some 110 us, without its loads 115: what is
+// left is instructions, 880 a page for a warp (333 unpack, 80 products, the rest parameters, softmax and bookkeeping).
+// 4 tokens (16 rows) over one sequence of 200 001: 75 us, 3.1 TB/s; its 64 accumulators leave 2 warps a scheduler.
+// One sequence of 261 tokens, 16 heads of 64: 8.8 us with the merge, launch and latency.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -709,18 +716,18 @@ int workers_of(int head_dim, int nt) {
 // 8 query rows a tile where a head has no more, else 16
 int tiles_of(int max_new, int group) { return (long long)max_new * group <= 8 ? 1 : 2; }
 
-// Sequences with more query rows a head go to the tensor-memory kernel.  A step of its 128-row tile costs about as much as
-// 3.4 steps of 16 rows here (frame of 1374 tokens on 21 984, 16 heads of 64: 788 us here), so 64 rows are where the
-// two meet.
-constexpr int FEW_ROWS = 64;
-bool many_rows(int max_new, int group) { return (long long)max_new * group > FEW_ROWS; }
+// Sequences with more query rows a head go to the tensor-memory kernel, whose time does not depend on them up to 128.
+// 8 sequences of 8000 tokens, this kernel against that one: 16 heads of 64, 64 rows 100 against 112 us, 80 rows 122
+// against 113; 8 key/value heads of 128, 32 rows 52 against 71 us, 48 rows 72 against 71, 64 rows 90 against 71.
+int few_rows(int head_dim) { return head_dim == 64 ? 64 : 48; }
+bool many_rows(int max_new, int group, int head_dim) { return (long long)max_new * group > few_rows(head_dim); }
 
 size_t workspace_of(int n_tokens, int n_seqs, int max_new, int group, int head_dim) {
     const int nt = tiles_of(max_new, group);
     const size_t workers = (size_t)workers_of(head_dim, nt);
     const size_t pf = (size_t)nt * (head_dim / 16) * 128 + nt * 16;
     const size_t few = align256(workers * sizeof(int4)) + align256(2 * workers * pf * sizeof(float));
-    return few + (many_rows(max_new, group) ? xsv_page_tc5_workspace(n_tokens, n_seqs, group, head_dim) : 0);
+    return few + (many_rows(max_new, group, head_dim) ? xsv_page_tc5_workspace(n_tokens, n_seqs, group, head_dim) : 0);
 }
 
 template <typename T, int D, int NT> cudaError_t launch(Attn& p, cudaStream_t st) {
@@ -786,8 +793,8 @@ extern "C" xsv_status xsv_page_attention(const xsv_page_pool* pool, const void* 
     cudaStream_t st = (cudaStream_t)stream;
     cudaError_t e = cudaSuccess;
     p.row_limit = 1 << 30;
-    if (many_rows(max_new, group)) {
-        p.row_limit = n_seqs == 1 ? 0 : FEW_ROWS;
+    if (many_rows(max_new, group, pool->head_dim)) {
+        p.row_limit = n_seqs == 1 ? 0 : few_rows(pool->head_dim);
         e = xsv_launch_page_tc5(p, pool->dtype, pool->head_dim, more, st);
     }
     if (e == cudaSuccess && p.row_limit > 0)

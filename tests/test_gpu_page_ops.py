@@ -567,6 +567,28 @@ def test_a_serving_step_captured_and_replayed_on_other_streams():
             assert torch.equal(again, out) and cu[-1] == n
 
 
+def test_norm_and_rotation_feed_a_cache_step():
+    # a frame of 5 special tokens and 6 x 6 patches: layer norm, rotation by row and column, then the streaming step
+    from oracle import xsv_oracle
+    n, h, d, dt = 41, 4, 64, torch.float16
+    g = torch.Generator(device="cuda").manual_seed(3)
+    at = (torch.arange(n, device="cuda") - 5).clamp(min=-1)
+    pos = torch.stack([at // 6 + 1, at % 6 + 1], -1)
+    pos = torch.where(at[:, None] < 0, torch.zeros_like(pos), pos).to(torch.int32).contiguous()
+    inv = 100.0 ** (-torch.arange(d // 4, device="cuda") / (d / 4))
+    cache, ref = binding.Cache(1, h, d, 82, 4), xsv_oracle.LayerCache(h, d, 82, 4)
+    for _ in range(4):
+        q, k, v = (torch.randn(n, h, d, device="cuda", generator=g).to(dt) for _ in range(3))
+        Q, K, V = binding.qk_norm_rope(q, k, v, norm="layer", eps=1e-5, rope="2d", inv_freq=inv, positions=pos, head_major=True)
+        want = orc.norm_rope(host(q), "layer", None, None, 1e-5, "2d", d, host(inv), pos.cpu().numpy()).transpose(1, 0, 2)
+        assert np.all(np.abs(host(Q) - want) <= HALF[dt] * np.abs(want) + 2e-5 * np.abs(want).max())
+        out = torch.empty_like(Q)
+        cache.step(0, Q, K, V, out)
+        o = ref.step(*(t.float().cpu().numpy() for t in (Q, K, V)))
+        assert np.abs(out.float().cpu().numpy() - o).max() <= 1e-2 * np.abs(o).max()      # the step's own tolerance
+    cache.destroy()
+
+
 def test_calls_on_a_given_stream():
     sv = Server(2, 2, 64, "fp16", pages=12, width=6, seed=9)
     plan = sv.step([100, 30])
