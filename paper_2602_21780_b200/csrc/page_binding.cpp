@@ -94,6 +94,14 @@ int small(int64_t n) {
 }
 at::Tensor empty(const at::Tensor& like, at::IntArrayRef shape) { return at::empty(shape, like.options().requires_grad(false).memory_format(c10::MemoryFormat::Contiguous)); }
 
+// Elements [off, off + n) of a list, over the same storage (integers: nothing for autograd to know).
+at::Tensor part_of(const at::Tensor& t, int64_t off, int64_t n) {
+    at::Tensor part = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(t.storage()), t.key_set(), t.dtype());
+    part.unsafeGetTensorImpl()->set_storage_offset(off);
+    part.unsafeGetTensorImpl()->set_sizes_contiguous({n});
+    return part;
+}
+
 xsv_page_pool pool_of(const at::Tensor& pages, const at::Tensor& tail) {
     if (pages.dim() != 3 || tail.dim() != 5) refuse("pages are [pages, kv_heads, 72 * head_dim], k_tail is [sequences, 2, kv_heads, 64, head_dim]");
     const int64_t n = pages.size(0), h = pages.size(1), seqs = tail.size(0), d = tail.size(4);
@@ -163,7 +171,6 @@ PyObject* plan(PyObject* const* a) {
     int *pc = ints(cached, "cached_len", here.dev, {n}), *pf = ints(fresh, "new_len", here.dev, {n}), *pt = ints(table, "block_table", here.dev, {n, -1}),
         *pr = ints(ring, "free_ring", here.dev, {-1}), *ps = ints(state, "ring_state", here.dev, {-1});
     if (state.size(0) < 2 || most < 0) refuse("ring_state holds head and count; max_tokens is not negative");
-    at::AutoDispatchBelowADInplaceOrView plain;              // integers: nothing to record
     const int64_t sizes[6] = {4, n + 1, n, most, most, most};
     const at::Tensor one = empty(cached, {4 + 2 * n + 1 + 3 * (int64_t)most});      // one allocation for all outputs
     int* at0 = one.data_ptr<int>();
@@ -171,7 +178,7 @@ PyObject* plan(PyObject* const* a) {
     int* p[6];
     int64_t off = 0;
     for (int i = 0; i < 6; ++i) {
-        out[i] = one.narrow(0, off, sizes[i]);
+        out[i] = part_of(one, off, sizes[i]);
         p[i] = at0 + off;
         off += sizes[i];
     }
