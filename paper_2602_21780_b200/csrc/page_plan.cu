@@ -2,13 +2,13 @@
 // pages taken from and given back to a ring of free pages, block-table entries of the new pages, and for every new
 // token its slot, sequence and position.
 //
-// Bound by latency: a few bytes per sequence and 12 per token.  Two scans over the sequences (tokens; pages) give
-// every sequence its place among the tokens and in the ring.  Each block repeats the scans for all sequences (they
+// Bound by latency: a few bytes per sequence and 12 per token.  One scan over the sequences (tokens, pages) gives
+// every sequence its place among the tokens and in the ring.  Each block repeats the scan for all sequences (they
 // are at most XSV_PAGE_MAX_SEQS, 16 per thread) instead of waiting for another block's, so that one launch without
 // any communication does it; the blocks then share out the tokens (found in the scanned offsets by bisection, in
 // shared memory) and the table rows.  Nothing that is read is written: ring positions that are pushed never meet
 // those that are popped (free pages plus pages in use are never more than the ring holds), so a call can be repeated.
-// Measured: 7 sequences 4.2 us, 1021 sequences with 52 000 new tokens 7.1 us (9.9 with four tokens a thread).
+// Measured: 7 sequences 3.7 us, 1021 sequences with 52 000 new tokens 7.0 us (9.9 with four tokens a thread and a scan more).
 #include <algorithm>
 
 #include "../../include/xsv.h"
@@ -35,33 +35,37 @@ struct Plan {
     int n_seqs, width, n_pages, max_tokens;
 };
 
-// exclusive scan of one pair per thread over the block; returns the block's totals in `all`
-__device__ __forceinline__ void block_scan2(long long& a, long long& b, long long (&all)[2], long long (*sh)[2]) {
+// exclusive scan of three sums per thread over the block; returns the block's totals in `all`
+__device__ __forceinline__ void block_scan(long long (&v)[3], long long (&all)[3], long long (*sh)[3]) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    long long x = a, y = b;
+    long long x[3];
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long u = __shfl_up_sync(0xFFFFFFFFu, x, o), v = __shfl_up_sync(0xFFFFFFFFu, y, o);
-        if (lane >= o) { x += u; y += v; }
-    }
-    if (lane == 31) { sh[warp][0] = x; sh[warp][1] = y; }
-    __syncthreads();
-    if (warp == 0) {
-        long long u = lane < THREADS / 32 ? sh[lane][0] : 0, v = lane < THREADS / 32 ? sh[lane][1] : 0;
+    for (int k = 0; k < 3; ++k) x[k] = v[k];
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long s = __shfl_up_sync(0xFFFFFFFFu, u, o), t = __shfl_up_sync(0xFFFFFFFFu, v, o);
-            if (lane >= o) { u += s; v += t; }
+    for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            const long long y = __shfl_up_sync(0xFFFFFFFFu, x[k], o);
+            if (lane >= o) x[k] += y;
         }
-        sh[lane][0] = u;
-        sh[lane][1] = v;
+    __syncthreads();                         // the last scan's reads
+    if (lane == 31)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) sh[warp][k] = x[k];
+    __syncthreads();
+    // every warp scans the warps' totals itself
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        long long t = lane < THREADS / 32 ? sh[lane][k] : 0;
+#pragma unroll
+        for (int o = 1; o < THREADS / 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xFFFFFFFFu, t, o);
+            if (lane >= o) t += y;
+        }
+        all[k] = __shfl_sync(0xFFFFFFFFu, t, THREADS / 32 - 1);
+        const long long before = __shfl_sync(0xFFFFFFFFu, t, (warp + 31) & 31);
+        v[k] = x[k] - v[k] + (warp ? before : 0);
     }
-    __syncthreads();
-    a = x - a + (warp ? sh[warp - 1][0] : 0);
-    b = y - b + (warp ? sh[warp - 1][1] : 0);
-    all[0] = sh[31][0];
-    all[1] = sh[31][1];
-    __syncthreads();
 }
 
 __global__ void __launch_bounds__(THREADS) page_plan_kernel(const __grid_constant__ Plan p) {
@@ -69,20 +73,15 @@ __global__ void __launch_bounds__(THREADS) page_plan_kernel(const __grid_constan
     int* s_cu = dyn;                         // [n_seqs + 1] first token of each sequence
     int* s_page = dyn + p.n_seqs + 1;        // [n_seqs] pages popped before it; -1 - that if it was refused
     int* s_free = s_page + p.n_seqs;         // [n_seqs] pages pushed before it
-    __shared__ long long sh[32][2];
-    __shared__ int s_refused;
+    __shared__ long long sh[THREADS / 32][3];
+    __shared__ int s_refused, s_taken;
     xsv_dep_release();
     xsv_dep_sync();
     const int tid = threadIdx.x, per = (p.n_seqs + THREADS - 1) / THREADS;
     const int s0 = min(p.n_seqs, tid * per), s1 = min(p.n_seqs, s0 + per);
-    if (tid == 0) s_refused = 0;
-    const int head = p.n_pages > 0 ? (int)(((long long)p.state_in[0] % p.n_pages + p.n_pages) % p.n_pages) : 0;
+    const int head = (int)(((long long)p.state_in[0] % p.n_pages + p.n_pages) % p.n_pages);
     const int count = max(0, min(p.state_in[1], p.n_pages));
 
-    long long tok = 0, zero = 0, all[2];
-    for (int s = s0; s < s1; ++s) tok += max(0, p.fresh[s]);
-    block_scan2(tok, zero, all, sh);
-    const int n_live = (int)min(all[0], (long long)p.max_tokens);
     // pages each sequence needs or gives back; a sequence that its table row or the token arrays cannot hold needs none
     auto pages_of = [&](int s, long long cu, long long& need, long long& freed, bool& bad) {
         const long long c = max(0, p.cached[s]), n = p.fresh[s];
@@ -94,45 +93,66 @@ __global__ void __launch_bounds__(THREADS) page_plan_kernel(const __grid_constan
         bad = have + need > p.width || (n > 0 && cu + n > p.max_tokens);
         if (bad) need = 0;
     };
-    long long need_sum = 0, freed_sum = 0, cu = tok;
+    // new tokens, pages needed, pages given back, before this thread's sequences: one scan if the token arrays hold all
+    // tokens, else the pages again, now that the tokens before each sequence are known
+    long long sum[3] = {0, 0, 0}, all[3];
     for (int s = s0; s < s1; ++s) {
         long long need, freed;
         bool bad;
-        pages_of(s, cu, need, freed, bad);
-        need_sum += need;
-        freed_sum += freed;
-        s_cu[s] = (int)min(cu, (long long)p.max_tokens);
-        cu += max(0, p.fresh[s]);
+        pages_of(s, -(1LL << 40), need, freed, bad);
+        sum[0] += max(0, p.fresh[s]);
+        sum[1] += need;
+        sum[2] += freed;
     }
-    block_scan2(need_sum, freed_sum, all, sh);
-    cu = tok;
-    int refused = 0;
-    long long taken = 0;
-    for (int s = s0; s < s1; ++s) {
-        long long need, freed;
-        bool bad;
-        pages_of(s, cu, need, freed, bad);
-        cu += max(0, p.fresh[s]);
-        if (need > 0 && need_sum + need > count) bad = true;
-        const int before = (int)min(need_sum, (long long)p.n_pages);
-        s_page[s] = bad ? -1 - before : before;
-        s_free[s] = (int)min(freed_sum, (long long)p.n_pages);
-        refused += bad;
-        if (!bad) taken += need;
-        need_sum += need;
-        freed_sum += freed;
+    block_scan(sum, all, sh);
+    const long long tok = sum[0];
+    const int n_live = (int)min(all[0], (long long)p.max_tokens);
+    if (all[0] > p.max_tokens) {
+        sum[0] = sum[1] = sum[2] = 0;
+        long long cu = tok;
+        for (int s = s0; s < s1; ++s) {
+            long long need, freed;
+            bool bad;
+            pages_of(s, cu, need, freed, bad);
+            cu += max(0, p.fresh[s]);
+            sum[1] += need;
+            sum[2] += freed;
+        }
+        block_scan(sum, all, sh);
+    }
+    const long long freed_all = all[2];
+    if (tid == 0) { s_refused = 0; s_taken = (int)min(all[1], (long long)p.n_pages); }
+    __syncthreads();
+    {
+        long long cu = tok, need_sum = sum[1], freed_sum = sum[2];
+        int refused = 0;
+        for (int s = s0; s < s1; ++s) {
+            long long need, freed;
+            bool bad;
+            pages_of(s, cu, need, freed, bad);
+            s_cu[s] = (int)min(cu, (long long)p.max_tokens);
+            cu += max(0, p.fresh[s]);
+            const int before = (int)min(need_sum, (long long)p.n_pages);
+            if (need > 0 && need_sum + need > count) {           // too few pages: it and all later ones that need any
+                bad = true;
+                atomicMin(&s_taken, before);
+            }
+            s_page[s] = bad ? -1 - before : before;
+            s_free[s] = (int)min(freed_sum, (long long)p.n_pages);
+            refused += bad;
+            need_sum += need;
+            freed_sum += freed;
+        }
+        if (refused) atomicAdd(&s_refused, refused);
     }
     if (tid == 0) s_cu[p.n_seqs] = n_live;
-    if (refused) atomicAdd(&s_refused, refused);
-    const long long freed_all = all[1];
-    zero = 0;
-    block_scan2(taken, zero, all, sh);       // also orders the shared arrays
-    const long long taken_all = all[0];
+    __syncthreads();
+    const long long taken_all = s_taken;
     auto at_ring = [&](long long i) { return (int)(((long long)head + i) % p.n_pages); };
 
     if (blockIdx.x == 0) {
         if (tid == 0) {
-            p.state_out[0] = p.n_pages > 0 ? at_ring(taken_all) : 0;
+            p.state_out[0] = at_ring(taken_all);
             p.state_out[1] = (int)min((long long)count - taken_all + freed_all, (long long)p.n_pages);
             p.state_out[2] = s_refused;
             p.state_out[3] = n_live;
