@@ -535,8 +535,10 @@ xsv_status xsv_page_read(const xsv_page_pool* pool, const int* block_table, int 
  *                  that see no token (of a sequence that the plan refused, for instance) are zero.
  *   workspace    : device, 16-byte aligned, at least xsv_page_attention_workspace() bytes; needs no clearing, holds
  *                  nothing between calls, and serves one call at a time (calls that may overlap take one each).
- * Probabilities and scaled queries are rounded to fp16 before the tensor cores, sums are float32.  Every device-side
- * wait is bounded; a row whose wait ran out is NaN.
+ * Sequences with up to 64 (head_dim 64) or 48 query rows a head (new tokens times q_heads / kv_heads) are attended by a
+ * kernel that multiplies the codes themselves, the others by one that dequantises pages to fp16 first; queries,
+ * probabilities and their products with the scales are fp16 operands, sums are float32.  Results do not depend on
+ * timing.  Every device-side wait is bounded; a row whose wait ran out is NaN.
  */
 xsv_status xsv_page_attention(const xsv_page_pool* pool, const void* Q, long long q_stride, int n_tokens, int q_heads,
                               const int* block_table, int table_width, const int* cu_new, const int* total_len, int n_seqs,

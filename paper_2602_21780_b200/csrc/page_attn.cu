@@ -58,7 +58,7 @@ template <int D, int NT> struct Part { static constexpr int FLOATS = NT * (D / 1
 constexpr int WARPS = 4, THREADS = WARPS * 32;
 template <int D, int NT> struct Shape {
     static constexpr int BLOCKS = D == 64 ? (NT == 1 ? 4 : 3) : (NT == 1 ? 3 : 2);
-    static constexpr int STAGES = D == 64 ? (NT == 1 ? 3 : 3) : (NT == 1 ? 2 : 2);
+    static constexpr int STAGES = D == 64 ? 3 : 2;
     static constexpr bool Q_REGS = NT == 1;
     static constexpr int PER_WARP = STAGES * PageRec<D>::BYTES + (Q_REGS ? 0 : NT * D * 16);
     static constexpr size_t SMEM = (size_t)WARPS * PER_WARP;
@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
             // logits (in log2 units) are s * f + z, f by row half (i / 2) and column (i % 2)
             float s[NT][4][4], f[NT][4], z[NT][2];
             if (!part) {
-                // q . z and, below it, what the rounding of q s leaves out (exact) times the middle code, 8, so that the error
+                // q . z and, FINE only, what the rounding of q s leaves out (exact) times the middle code, 8, so that the error
                 // that stays is that of the codes around their middle
                 float qz[NT][3][4];
 #pragma unroll

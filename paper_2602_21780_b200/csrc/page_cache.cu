@@ -1,9 +1,10 @@
 // Writing the pages of the shared pool, and reading them back as values.
 //
 // xsv_page_append: one block per (new tokens of one page, head), or, where a few tokens do not fill their page
-// (decoding), one warp.  Values are quantised per token over 64 channels as they come and merged into the page's code words (a token is one byte of each word it touches); keys need all 64
-// tokens of a page for their per-channel scale, so a page's keys wait in the sequence's tail, in 16 bits, and are
-// quantised by the call that brings the page's last token.  The tail has two halves, by the page's parity: the page
+// (decoding), one warp.  Values are quantised per token over 64 channels as they come and merged into the page's code
+// words (a token is one byte of each word it touches); keys need all 64 tokens of a page for their per-channel scale,
+// so a page's keys wait in the sequence's tail, in 16 bits, and are quantised by the call that brings the page's last
+// token.  The tail has two halves, by the page's parity: the page
 // that is completed is read from one while the page after it starts in the other.  Bound by HBM for prompts (2 bytes
 // read, 72/128 written per element); the thread layout makes both packings local to a thread -- a thread's 8 rows x
 // 8 channels of keys (rows 8 i + g) are whole code words, and so are 4 tokens x 8 channels of values -- so codes never
