@@ -271,9 +271,13 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
         __syncwarp();
         if (!failed) {
             issue(stage == 0 ? STAGES - 1 : stage - 1);
-            if (!mbar_try(smem_u32(&bars[wid][stage]), parity) && !mbar_wait_bounded(smem_u32(&bars[wid][stage]), parity)) {
+            // The warp gives up as one: what follows needs all of its lanes, and near the limit one lane's clock can have run
+            // out while another's wait succeeds.
+            const uint32_t bar = smem_u32(&bars[wid][stage]);
+            if (!__all_sync(0xFFFFFFFFu, mbar_try(bar, parity)) && !__all_sync(0xFFFFFFFFu, mbar_wait_bounded(bar, parity))) {
                 failed = true;                                 // nothing is issued any more; what is in flight gets its time
                 for (int i = 0; i < STAGES; ++i) mbar_wait_bounded(smem_u32(&bars[wid][(stage + i) % STAGES]), stage + i < STAGES ? parity : parity ^ 1);
+                __syncwarp();
             }
         }
         __syncwarp();
