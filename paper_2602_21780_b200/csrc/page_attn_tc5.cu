@@ -569,11 +569,14 @@ __device__ __noinline__ void mma_loop(const Work& w, const Cta c, Units u, const
     for (; u.valid; next_unit(w, u)) {
         const int n = u.kv1 - u.kv0, ntile = u.en.row0 + BM < u.en.n_rows ? 2 : 1;
         if (x >= ntile) {
-            // no second tile: tile 0's warp releases the stages for both; this one still passes their phases one by one
+            // No second tile: this warp passes the stages' phases one by one and releases its share of each.  The stage is
+            // not filled again before it has, so a parity wait here is never more than one phase late.
             for (int k = 0; k < n; ++k) {
                 const uint32_t step = it + (uint32_t)k, st = step % C::NSTAGE;
                 mbar_wait(BAR(C::KFULL + (int)st), (step / C::NSTAGE) & 1u, c.abort_flag, c.status, XSV_DEV_SITE_K);
                 mbar_wait(BAR(C::VFULL + (int)st), (step / C::NSTAGE) & 1u, c.abort_flag, c.status, XSV_DEV_SITE_K);
+                __syncwarp();
+                if (elect_one()) mbar_arrive(BAR(C::EMPTY + (int)st));
             }
             it += (uint32_t)n;
             continue;
@@ -595,7 +598,6 @@ __device__ __noinline__ void mma_loop(const Work& w, const Cta c, Units u, const
                     mma_ts(tO, tS + buf * 64u + 8u * q, vd + 2u * q, C::IDESC_PV, q > 0 ? 1u : acc);
                 tc_commit(BAR(C::PVDONE + x * C::NBUF + (int)buf));
                 tc_commit(BAR(C::EMPTY + (int)st));
-                if (ntile == 1) tc_commit(BAR(C::EMPTY + (int)st));    // the other tile's share
             }
             __syncwarp();
             if (qk < n) {
@@ -630,7 +632,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) page_attn_tc5_kernel(const __grid
         for (int i = 0; i < C::NSTAGE; ++i) {
             mbar_init(BAR(C::KFULL + i), C::BLK);      // one arrival per slab
             mbar_init(BAR(C::VFULL + i), C::BLK);
-            mbar_init(BAR(C::EMPTY + i), 2);           // one commit per query tile
+            mbar_init(BAR(C::EMPTY + i), 2);           // one per query tile: a commit, or an arrival where there is no second tile
         }
         for (int i = 0; i < 2 * C::NBUF; ++i) {
             mbar_init(BAR(C::SFULL + i), 1);
