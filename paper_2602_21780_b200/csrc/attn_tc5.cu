@@ -799,13 +799,15 @@ __device__ __noinline__ void mma_loop(const Params& p, const Cta c, const int x,
         const int ntile = (mp * 2 * BM + BM < F) ? 2 : 1;
         const int n = sp.kv1 - sp.kv0;
         if (x >= ntile) {
-            // This unit has no second query tile: tile 0's warp releases the stages for both.  This warp still
-            // consumes the stages' barrier phases one by one, so that it never runs more than one phase ahead
-            // of a barrier (a parity wait means nothing beyond that).
+            // This unit has no second query tile.  This warp passes the stages' barrier phases one by one and releases
+            // its share of each stage: not filled again before it has, a stage never gets more than one phase ahead of
+            // it, nor it of a barrier (a parity wait means nothing beyond that).
             for (int i = 0; i < n; ++i) {
                 const uint32_t it = it0 + (uint32_t)i, st = it % NSTAGE;
                 mbar_wait(BAR(B_KFULL + (int)st), (it / NSTAGE) & 1u, abort_flag, status, XSV_DEV_SITE_K);
                 mbar_wait(BAR(B_VFULL + (int)st), (it / NSTAGE) & 1u, abort_flag, status, XSV_DEV_SITE_K);
+                __syncwarp();
+                if (elect_one()) mbar_arrive(BAR(B_EMPTY + (int)st));
             }
             it0 += (uint32_t)n;
             continue;
@@ -836,10 +838,7 @@ __device__ __noinline__ void mma_loop(const Params& p, const Cta c, const int x,
                     for (int k = 0; k < SUB / 16; ++k)     // 16 tokens: 8 columns of P, 2048 bytes of V
                         mma_ts(tO, tS + buf * SUB + 8u * k, vd + 128u * k, IDESC_PV | fmt, k > 0 ? 1u : acc0);
                     tc_commit(BAR(B_PVDONE + x * NBUF + (int)buf));
-                    if (release) {
-                        tc_commit(BAR(B_EMPTY + (int)st));
-                        if (ntile == 1) tc_commit(BAR(B_EMPTY + (int)st));   // the other tile's share
-                    }
+                    if (release) tc_commit(BAR(B_EMPTY + (int)st));
                 }
                 __syncwarp();
                 if (qi < n) {
@@ -882,7 +881,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) attn_tc5_kernel(const __grid_cons
         for (int i = 0; i < NSTAGE; ++i) {
             mbar_init(BAR(B_KFULL + i), bp.use_tma ? 1 : 4);     // one arrival per slab of 32 rows, or the one that announces the copy
             mbar_init(BAR(B_VFULL + i), bp.use_tma ? 1 : 4);
-            mbar_init(BAR(B_EMPTY + i), 2);     // one commit per query tile
+            mbar_init(BAR(B_EMPTY + i), 2);     // one per query tile: a commit, or an arrival where there is no second tile
         }
         for (int x = 0; x < 2; ++x) {
             for (int i = 0; i < NBUF; ++i) {
