@@ -81,7 +81,7 @@ static_assert(smem_bytes<16>() <= 227 * 1024, "shared memory");
 
 // barrier slots (8 bytes each) inside the barrier block
 enum { B_KFULL = 0, B_VFULL = NSTAGE, B_EMPTY = 2 * NSTAGE, B_SFULL = 3 * NSTAGE, B_PREADY = B_SFULL + 2 * NBUF,
-       B_PVDONE = B_PREADY + 2 * NBUF, B_QFULL = B_PVDONE + 2 * NBUF, B_COUNT = B_QFULL + 2 };
+       B_PVDONE = B_PREADY + 2 * NBUF, B_QFULL = B_PVDONE + 2 * NBUF, B_DRAIN = B_QFULL + 2, B_COUNT = B_DRAIN + 2 };
 static_assert(B_COUNT * 8 + 16 <= BAR_BYTES, "barrier block");
 // tensor-memory columns: S sub-tile buffer b of query tile x (its P, as fp16 pairs, overwrites the first half of
 // the S it was computed from), then the two output accumulators
@@ -550,9 +550,11 @@ __device__ __noinline__ void producer_tma_loop(const Params& p, const Cta c, con
     const int n_ct = p.n_ct;
     TileIter cur{c.u_first, 0, 0, 0, false};
     tile_iter_settle(p, c.b, c.u_last, cur);
-    for (uint32_t it = 0; cur.valid; ++it, tile_iter_next(p, c.b, c.u_last, cur)) {
+    uint32_t it = 0;
+    for (; cur.valid; ++it, tile_iter_next(p, c.b, c.u_last, cur)) {
         const uint32_t st = it % NSTAGE;
         if (it >= NSTAGE) mbar_wait(BAR(B_EMPTY + st), ((it / NSTAGE) - 1u) & 1u, abort_flag, p.status, XSV_DEV_SITE_STAGE);
+        if (*abort_flag) break;                       // nothing is issued any more
         const bool cached = cur.kv < n_ct;
         const int row0 = (cached ? cur.kv : cur.kv - n_ct) * BN;
         const uint32_t kdst = c.smem_base + OFF_KV + st * 2 * TILE_BYTES, vdst = kdst + TILE_BYTES;
@@ -560,6 +562,11 @@ __device__ __noinline__ void producer_tma_loop(const Params& p, const Cta c, con
         tma_load_3d(kdst, &maps.m[cached ? 0 : 2], BAR(B_KFULL + (int)st), 0, row0, cur.h);
         mbar_expect_tx(BAR(B_VFULL + (int)st), TILE_BYTES);
         tma_load_3d(vdst, &maps.m[cached ? 1 : 3], BAR(B_VFULL + (int)st), 0, row0, cur.h);
+    }
+    // the copies that may still be in flight land before the block can end, also where no one waits for them any more
+    for (uint32_t i = it > NSTAGE ? it - NSTAGE : 0; i < it; ++i) {
+        mbar_wait_bounded(BAR(B_KFULL + (int)(i % NSTAGE)), (i / NSTAGE) & 1u);
+        mbar_wait_bounded(BAR(B_VFULL + (int)(i % NSTAGE)), (i / NSTAGE) & 1u);
     }
 }
 
@@ -890,6 +897,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) attn_tc5_kernel(const __grid_cons
                 mbar_init(BAR(B_PVDONE + x * NBUF + i), 1);
             }
             mbar_init(BAR(B_QFULL + x), 4);
+            mbar_init(BAR(B_DRAIN + x), 1);
         }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -914,6 +922,14 @@ __global__ void __launch_bounds__(NTHREADS, 1) attn_tc5_kernel(const __grid_cons
     else mma_loop(p, cta, warp - (8 + NPROD), BF ? IDESC_BF16 : 0u);
     tc_fence_before();
     __syncthreads();
+    if (*abort_flag) {                                // a wait ran out (the same for the whole block): MMAs may still be in flight
+        if (warp >= 8 + NPROD) {
+            const uint32_t drain = BAR(B_DRAIN + warp - (8 + NPROD));
+            if (elect_one()) tc_commit(drain);
+            mbar_wait_bounded(drain, 0u);
+        }
+        __syncthreads();
+    }
     // Only now may the next kernel be scheduled: released at the start, its blocks would sit through this whole kernel
     // on whatever multiprocessor the grid leaves free (the one kept for the selection kernel of another stream).
     xsv_dep_release();

@@ -64,13 +64,6 @@ template <int D, int NT> struct Shape {
     static constexpr size_t SMEM = (size_t)WARPS * PER_WARP;
 };
 
-// Bounded: false once the limit has passed.
-__device__ __noinline__ bool mbar_wait_bounded(uint32_t bar, uint32_t parity) {
-    const unsigned long long t0 = globaltimer();
-    while (globaltimer() - t0 < WAIT_LIMIT_NS)
-        if (mbar_try(bar, parity)) return true;
-    return false;
-}
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));

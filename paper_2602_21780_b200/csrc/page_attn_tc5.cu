@@ -48,7 +48,7 @@ template <int D> struct Cfg {
     static constexpr uint32_t OFF_KV = 2 * Q_TILE, OFF_BAR = OFF_KV + NSTAGE * STAGE, SMEM = OFF_BAR + 1024 + 1024;
     // barriers
     static constexpr int KFULL = 0, VFULL = NSTAGE, EMPTY = 2 * NSTAGE, SFULL = 3 * NSTAGE, PREADY = SFULL + 2 * NBUF,
-                         PVDONE = PREADY + 2 * NBUF, QFULL = PVDONE + 2 * NBUF, COUNT = QFULL + 2;
+                         PVDONE = PREADY + 2 * NBUF, QFULL = PVDONE + 2 * NBUF, DRAIN = QFULL + 2, COUNT = DRAIN + 2;
     static_assert(COUNT * 8 + 128 <= 1024 && SMEM <= 227 * 1024, "shared memory");
     __host__ __device__ static constexpr uint32_t tm_s(int x, int b) { return (uint32_t)((x * NBUF + b) * 64); }
     __host__ __device__ static constexpr uint32_t tm_o(int x) { return (uint32_t)(2 * NBUF * 64 + x * D); }
@@ -641,6 +641,8 @@ __global__ void __launch_bounds__(NTHREADS, 1) page_attn_tc5_kernel(const __grid
         }
         mbar_init(BAR(C::QFULL), 4);
         mbar_init(BAR(C::QFULL + 1), 4);
+        mbar_init(BAR(C::DRAIN), 1);
+        mbar_init(BAR(C::DRAIN + 1), 1);
         misc[1] = misc[2] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -697,6 +699,14 @@ __global__ void __launch_bounds__(NTHREADS, 1) page_attn_tc5_kernel(const __grid
     else mma_loop<D>(w, cta, u, warp - (8 + NPROD));
     tc_fence_before();
     __syncthreads();
+    if (*cta.abort_flag) {                             // a wait ran out (the same for the whole block): MMAs may still be in flight
+        if (warp >= 8 + NPROD) {
+            const uint32_t drain = BAR(C::DRAIN + warp - (8 + NPROD));
+            if (elect_one()) tc_commit(drain);
+            mbar_wait_bounded(drain, 0u);
+        }
+        __syncthreads();
+    }
     xsv_dep_release();
     if (warp == 8 + NPROD + 1) {
         tc_fence_after();

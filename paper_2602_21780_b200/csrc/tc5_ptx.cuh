@@ -55,6 +55,13 @@ __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatil
     if (*abort_flag) return;
     mbar_wait_slow(bar, parity, abort_flag, status, site);
 }
+// Bounded, whatever the abort flag says: false once the limit has passed.
+__device__ __noinline__ bool mbar_wait_bounded(uint32_t bar, uint32_t parity) {
+    const unsigned long long t0 = globaltimer();
+    while (globaltimer() - t0 < WAIT_LIMIT_NS)
+        if (mbar_try(bar, parity)) return true;
+    return false;
+}
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }

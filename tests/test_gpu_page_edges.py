@@ -6,7 +6,7 @@ import torch
 
 from oracle import page_oracle as orc
 from paper_2602_21780_b200 import binding
-from test_gpu_page_ops import DT, HALF, PAGE, Server, host, ints
+from tests.test_gpu_page_ops import DT, HALF, PAGE, Server, host, ints
 
 pytestmark = pytest.mark.gpu
 
