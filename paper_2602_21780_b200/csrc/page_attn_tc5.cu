@@ -206,7 +206,9 @@ __device__ __forceinline__ uint32_t pair_at(const uint4& a, const uint4& b, int 
 __host__ __device__ constexpr int place(int m, int b, int j, int h) { return 16 * j + 4 * m + 2 * b + h; }
 __host__ __device__ constexpr int token_at(int pos) { return 16 * (pos >> 2 & 3) + 8 * (pos >> 1 & 1) + 2 * (pos >> 4) + (pos & 1); }
 
-__device__ __forceinline__ uint4 ldg16(const uint8_t* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
+// A plain load: blocks of this kernel can be resident while the append before it still writes the records, and what
+// the wait for it makes visible is not promised to the read-only path.
+__device__ __forceinline__ uint4 ld16(const uint8_t* p) { return *reinterpret_cast<const uint4*>(p); }
 __device__ __forceinline__ void sts16(uint32_t at, const uint4& v) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
@@ -230,7 +232,7 @@ __device__ __noinline__ void producer_loop(const PageAttn& p, const Work& w, con
             if (k - ids_from >= 32) {
                 ids_from = k & ~31;
                 const int pg = u.en.p0 + u.kv0 + ids_from + lane;
-                ids = ids_from + lane < n && pg < p.width && pg * XSV_PAGE < total ? __ldg(row + ids_from + lane) : -1;
+                ids = ids_from + lane < n && pg < p.width && pg * XSV_PAGE < total ? row[ids_from + lane] : -1;
                 if ((unsigned long long)(long long)ids >= (unsigned long long)p.pool.n_pages) ids = -1;
             }
             return __shfl_sync(0xFFFFFFFFu, ids, k & 31);
@@ -244,19 +246,19 @@ __device__ __noinline__ void producer_loop(const PageAttn& p, const Work& w, con
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int kg = 2 * part + (i ^ odd);
-                    r.code[2 * i] = ldg16(rec + R::K_CODES + (2 * kg * 32 + lane) * 16);
-                    r.code[2 * i + 1] = ldg16(rec + R::K_CODES + ((2 * kg + 1) * 32 + lane) * 16);
-                    r.a[i] = ldg16(rec + R::K_SCALE + 64 * kg + 16 * j);
-                    r.b[i] = ldg16(rec + R::K_ZERO + 64 * kg + 16 * j);
+                    r.code[2 * i] = ld16(rec + R::K_CODES + (2 * kg * 32 + lane) * 16);
+                    r.code[2 * i + 1] = ld16(rec + R::K_CODES + ((2 * kg + 1) * 32 + lane) * 16);
+                    r.a[i] = ld16(rec + R::K_SCALE + 64 * kg + 16 * j);
+                    r.b[i] = ld16(rec + R::K_ZERO + 64 * kg + 16 * j);
                 }
             } else {
                 const int v = part - C::BLK;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) r.code[t] = ldg16(rec + R::V_CODES + ((t * C::BLK + v) * 32 + lane) * 16);
+                for (int t = 0; t < 4; ++t) r.code[t] = ld16(rec + R::V_CODES + ((t * C::BLK + v) * 32 + lane) * 16);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    r.a[i] = ldg16(rec + R::V_SCALE + 128 * v + 32 * j + 16 * i);
-                    r.b[i] = ldg16(rec + R::V_ZERO + 128 * v + 32 * j + 16 * i);
+                    r.a[i] = ld16(rec + R::V_SCALE + 128 * v + 32 * j + 16 * i);
+                    r.b[i] = ld16(rec + R::V_ZERO + 128 * v + 32 * j + 16 * i);
                 }
             }
         };
