@@ -419,8 +419,9 @@ int xsv_plan_batch_groups(int n, const int* cache_tokens, const int* frame_token
  * A page holds 64 tokens -- one quantisation group -- of every key/value head of one layer, quantised at the paper's
  * granularities (Eq. 11: keys per channel over the page's 64 tokens, values per token over 64 channels) with fp16
  * parameters rounded outwards: offset z = the group's minimum rounded down to fp16, scale s = (maximum - z) / 15
- * rounded up to fp16 (1 where that is 0), code = nearest-even of (x - z) / s, value = code * s + z, off by at most
- * s / 2.  Inputs are finite; magnitudes beyond 65504 are stored as 65504.  A sequence is a row of a block table (page
+ * rounded up to fp16 (down where code 15 would otherwise stand for more than 65504; 1 where that is 0), code =
+ * nearest-even of (x - z) / s, value = code * s + z, off by at most s / 2 and at most 65504 in magnitude.  Inputs are
+ * finite; magnitudes beyond 65504 are stored as 65504.  A sequence is a row of a block table (page
  * indices in order) and a length; sequences take pages from a ring of free pages.  A sequence's last, unfilled page
  * keeps its keys as they came, 16 bits, in the sequence's tail (per-channel scales need all 64 tokens); its values are
  * in the page.  A step of a model: xsv_page_plan once, then per layer xsv_qk_norm_rope, xsv_page_append,

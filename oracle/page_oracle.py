@@ -23,6 +23,7 @@ def quantise(x, axis):
     x = np.clip(np.asarray(x, np.float64), -65504, 65504)
     z = half_down(x.min(axis, keepdims=True))
     s = half_up((x.max(axis, keepdims=True) - z) / 15)
+    s = np.where(15 * s + z > 65504, _HALVES[np.searchsorted(_HALVES, s) - 1], s)      # no code stands for more than 65504
     s = np.where(s == 0, 1.0, s)
     return np.clip(np.rint((x - z) / s), 0, 15).astype(np.int64), s, z
 

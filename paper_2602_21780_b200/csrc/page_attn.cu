@@ -626,8 +626,8 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
 #pragma unroll
                         for (int v = 0; v < VG; ++v)
                             *reinterpret_cast<uint4*>(dst + 64 * v) = make_uint4(
-                                xsv_pack2<T>(o[n][4 * v][c] * inv, o[n][4 * v][c + 2] * inv), xsv_pack2<T>(o[n][4 * v + 1][c] * inv, o[n][4 * v + 1][c + 2] * inv),
-                                xsv_pack2<T>(o[n][4 * v + 2][c] * inv, o[n][4 * v + 2][c + 2] * inv), xsv_pack2<T>(o[n][4 * v + 3][c] * inv, o[n][4 * v + 3][c + 2] * inv));
+                                page_result2<T>(o[n][4 * v][c] * inv, o[n][4 * v][c + 2] * inv), page_result2<T>(o[n][4 * v + 1][c] * inv, o[n][4 * v + 1][c + 2] * inv),
+                                page_result2<T>(o[n][4 * v + 2][c] * inv, o[n][4 * v + 2][c + 2] * inv), page_result2<T>(o[n][4 * v + 3][c] * inv, o[n][4 * v + 3][c + 2] * inv));
                     }
             } else {
                 float* dst = p.part + (size_t)(2 * worker + (whole ? 1 : 0)) * Part<D, NT>::FLOATS;
@@ -698,7 +698,7 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) page_attn_merge_kernel(const
             const int i = r / p.group, h = r - i * p.group;
             const float l = c ? acc.ml.w : acc.ml.y, inv = l == 0.f ? 0.f : 1.f / l;
             T* dst = (T*)p.out + ((size_t)(t0 + i) * p.q_heads + d.y * p.group + h) * D + 64 * (ct / 4) + 8 * g + 2 * (ct % 4);
-            *reinterpret_cast<uint32_t*>(dst) = xsv_pack2<T>((c ? acc.o.y : acc.o.x) * inv, (c ? acc.o.w : acc.o.z) * inv);
+            *reinterpret_cast<uint32_t*>(dst) = page_result2<T>((c ? acc.o.y : acc.o.x) * inv, (c ? acc.o.w : acc.o.z) * inv);
         }
     }
 }

@@ -26,6 +26,17 @@ __device__ __forceinline__ PageSeq page_seq(const PageAttn& p, int s) {
     q.first = q.total - q.new_;
     return q;
 }
+// Two results -> 16 bits.  Results are means of values of at most 65504, but the rounding of the weights may carry one
+// past the largest fp16.  A NaN stays.
+template <typename T> __device__ __forceinline__ uint32_t page_result2(float a, float b) { return xsv_pack2<T>(a, b); }
+template <> __device__ __forceinline__ uint32_t page_result2<__half>(float a, float b) {
+    auto in = [](float x) {
+        asm("min.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(65504.f));
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(-65504.f));
+        return x;
+    };
+    return xsv_pack2<__half>(in(a), in(b));
+}
 // query row of a key/value head -> new token and query head of the group
 __device__ __forceinline__ void page_row(const PageAttn& p, int r, int& i, int& h) {
     i = p.group_shift >= 0 ? r >> p.group_shift : r / p.group;

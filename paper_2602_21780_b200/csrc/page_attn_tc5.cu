@@ -529,7 +529,7 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
                 if (r < u.en.n_rows) {
                     uint32_t y[8];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) y[k] = xsv_pack2<T>(__uint_as_float(o[2 * k]) * inv, __uint_as_float(o[2 * k + 1]) * inv);
+                    for (int k = 0; k < 8; ++k) y[k] = page_result2<T>(__uint_as_float(o[2 * k]) * inv, __uint_as_float(o[2 * k + 1]) * inv);
                     reinterpret_cast<uint4*>(dst + 16 * q)[0] = make_uint4(y[0], y[1], y[2], y[3]);
                     reinterpret_cast<uint4*>(dst + 16 * q)[1] = make_uint4(y[4], y[5], y[6], y[7]);
                 }
@@ -752,7 +752,7 @@ __global__ void __launch_bounds__(256) page_attn_tc5_merge_kernel(const __grid_c
     T* dst = (T*)p.out + ((size_t)(en.t0 + i) * p.q_heads + d.y * p.group + h) * D;
 #pragma unroll
     for (int k = 0; k < D / 64; ++k)
-        *reinterpret_cast<uint2*>(dst + 64 * k + 4 * c) = make_uint2(xsv_pack2<T>(o[k].x * inv, o[k].y * inv), xsv_pack2<T>(o[k].z * inv, o[k].w * inv));
+        *reinterpret_cast<uint2*>(dst + 64 * k + 4 * c) = make_uint2(page_result2<T>(o[k].x * inv, o[k].y * inv), page_result2<T>(o[k].z * inv, o[k].w * inv));
 }
 
 // ------------------------------------------------------------------ host side

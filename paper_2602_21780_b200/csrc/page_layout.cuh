@@ -17,7 +17,8 @@
 //   values: column r of step k is token 16 k + r; row g of word m is channel 64 c + 8 g + 2 m, row g + 8 the one after
 //           it: a lane's output channels are 8 consecutive ones.
 // Scales and offsets are fp16, rounded outwards (offset down, scale up), so that no value leaves the code range and a
-// value is off by at most half a scale.
+// value is off by at most half a scale.  Where the last code would stand for more than 65504 the scale is rounded down
+// instead, so that every value is a finite fp16: the maximum is then off by at most 15 steps of s, 2^-10 s each.
 #pragma once
 #include "../../include/xsv.h"
 #include "xsv_common.cuh"
@@ -58,13 +59,15 @@ template <> __device__ __forceinline__ float2 xsv_unpack2<__nv_bfloat16>(uint32_
 
 // Scale and offset of a group from its minimum and maximum (already inside +-65504).  The offset is the minimum rounded
 // down to fp16; the scale is the smallest fp16 whose 15-fold (exact in float32) reaches the maximum minus the offset: the
-// nearest fp16 to a fifteenth of that difference (rounded up), or the next one.
+// nearest fp16 to a fifteenth of that difference (rounded up), or the next one; and the one below where that 15-fold is
+// beyond 65504 minus the offset (which the one below never is: it does not reach the maximum).
 __device__ __forceinline__ void page_params(float mn, float mx, __half& s, __half& z) {
     z = __float2half_rd(mn);
     const float d = __fsub_ru(mx, __half2float(z));
     s = __float2half_rn(d * 0.066666670f);
     unsigned short bits = __half_as_ushort(s);
     if (__half2float(s) * 15.f < d) ++bits;
+    if (__half2float(__ushort_as_half(bits)) * 15.f > __fsub_rd(65504.f, __half2float(z))) --bits;
     s = __ushort_as_half(bits ? bits : (unsigned short)0x3C00);       // 1 for a group of one value
 }
 __device__ __forceinline__ float page_inverse(float s) {            // within 2^-23
@@ -72,8 +75,8 @@ __device__ __forceinline__ float page_inverse(float s) {            // within 2^
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
     return r;
 }
-// Codes of 8 values with the same parameters: nearest-even of the quotients (x - z) / s.  Outward rounding keeps a quotient
-// inside [0, 15 + 2^-19]; (x - z) * inv is within 2^-18 of it.  Where that is nowhere within 2e-5 of a half-integer its
+// Codes of 8 values with the same parameters: nearest-even of the quotients (x - z) / s.  A quotient is inside
+// [0, 15 + 2^-6] (outward rounding: 15 + 2^-19); (x - z) * inv is within 2^-18 of it.  Where that is nowhere within 2e-5 of a half-integer its
 // rounding (1.5 * 2^23 added: the integer is in the low bits) is the quotient's; else the remainders of all eight decide, which
 // are exact next to a half-integer.  The mask keeps an infinite or NaN value from its neighbours in a code word.
 __device__ __forceinline__ void page_codes(const float (&x)[8], float s, float inv, float z, uint32_t (&c)[8]) {

@@ -20,3 +20,58 @@ def test_long_units_without_a_second_query_tile(d, hq, hkv, new):
     for step in ([new, 0, 0], [new, 400, new + 1], [0, new, 300]):
         plan = sv.step(step)
         sv.check_attention(plan, step, hq)
+
+
+def top_rows(n, hkv, d, dt, g):
+    """Keys and values whose groups span to the largest finite values: 0, 65504 and both ends, where outward rounding alone
+    would let the last code stand for more than float16 holds."""
+    top = torch.finfo(torch.float16).max
+    k = torch.randn(n, hkv, d, device="cuda", generator=g)
+    k[::2, :, 3], k[1::2, :, 3] = 0, top
+    k[::2, :, 9], k[1::2, :, 9] = top, -top
+    v = torch.rand(n, hkv, d, device="cuda", generator=g)
+    low = torch.tensor([0.0, -top, -60000.0, 0.5 * top], device="cuda")[torch.arange(n, device="cuda") % 4]
+    v = low[:, None, None] + (top - low[:, None, None]) * v
+    v[:, :, ::64], v[:, :, 1::64] = low[:, None, None], top
+    return k.to(dt), v.clamp(-top, top).to(dt)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_values_at_the_top_of_the_range_stay_finite(dtype, d):
+    # 200 tokens by 2 heads: few rows a head (1 new token) and many (90); queries so small that the logits stay near 1
+    sv = Server(1, 2, d, dtype, pages=6, width=4, seed=d)
+    k, v = top_rows(200, 2, d, sv.dt, sv.g)
+    plan = binding.page_plan(sv.len, ints([200]), sv.table, sv.ring, sv.state, 200)
+    binding.page_append(sv.pages, sv.tail, k, v, plan.slot_map, plan.token_seq, plan.cu_new, plan.total_len)
+    sv.len = plan.total_len
+    for h in range(2):
+        sv.ref[0][h].append(host(k[:, h]), host(v[:, h]))
+    sv.check_state()
+    K, V = binding.page_read(sv.pages, sv.tail, sv.table, sv.len, ints([0] * 200), ints(np.arange(200)))
+    for got, which in ((host(K), "k"), (host(V), "v")):
+        ref = np.stack([getattr(r, which) for r in sv.ref[0]], 1)
+        assert np.all(np.abs(got - ref) <= HALF[sv.dt] * np.abs(ref) * 1.001 + 2.0 ** -25)
+    q = (sv.rnd(90, 4, d) * 1e-5).to(sv.dt)
+    for new in (1, 90):
+        fake = plan._replace(cu_new=ints([0, new]))
+        sv.check_attention(fake, [new], 4, q=q[:new].contiguous(), scale=1.0)
+
+
+@pytest.mark.parametrize("new", [1, 6])
+def test_a_mean_of_the_largest_values_stays_finite(new):
+    # 60 values of 65504; one token's weight is 1, the others' lie just above the middle between two float16 numbers next to
+    # 1/2, so that all of them are rounded up by nearly 2^-11: the mean leaves float16 unless it is brought back.  12 query
+    # heads by 6 tokens go to the kernel for many rows, 12 rows to the one for few.
+    sv = Server(1, 1, 64, "fp16", pages=2, width=1)
+    top = 65504.0
+    k = torch.zeros(60, 1, 64, device="cuda", dtype=sv.dt)
+    k[0, 0, 0] = 1
+    v = torch.full((60, 1, 64), top, device="cuda", dtype=sv.dt)
+    plan = binding.page_plan(sv.len, ints([60]), sv.table, sv.ring, sv.state, 60)
+    binding.page_append(sv.pages, sv.tail, k, v, plan.slot_map, plan.token_seq, plan.cu_new, plan.total_len)
+    q = torch.zeros(new, 12, 64, device="cuda", dtype=sv.dt)
+    q[:, :, 0] = 1
+    scale = (1 - np.log2(1 + 1.05 * 2.0 ** -11)) / np.log2(np.e)
+    out = host(binding.page_attention(q, sv.pages, sv.tail, sv.table, ints([0, new]), plan.total_len, new, scale=float(scale)))
+    assert np.all(np.abs(out - top) <= 2.0 ** -11 * top)        # exactly 65504 in real arithmetic

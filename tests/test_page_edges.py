@@ -2,6 +2,10 @@
 import glob
 import os
 
+import numpy as np
+
+from oracle import page_oracle as orc
+
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CSRC = os.path.join(ROOT, "paper_2602_21780_b200", "csrc")
 
@@ -12,3 +16,17 @@ def test_kernels_read_memory_through_the_coherent_path():
     for path in glob.glob(os.path.join(CSRC, "*.cu*")):
         src = open(path).read()
         assert "__ldg(" not in src and "ld.global.nc" not in src, path
+
+
+def test_no_code_stands_for_more_than_the_largest_half():
+    rng = np.random.default_rng(5)
+    top, ulp = 65504.0, 32.0
+    x = [np.r_[lo, top, rng.uniform(lo, top, 62)] for lo in (0.0, -65504.0, -60000.0, 65472.0, 65000.0, 1e-7, -1e-7, 40000.0)]
+    x += [np.r_[-top, rng.uniform(-top, 60000, 63)], np.full(64, top), np.full(64, -top), np.r_[top - ulp * np.arange(64)]]
+    x = np.stack(x + [np.r_[lo, rng.uniform(lo, top, 63)].astype(np.float16).astype(np.float64) for lo in rng.uniform(-top, top, 300)])
+    c, s, z = orc.quantise(x, 1)
+    assert c.min() >= 0 and c.max() <= 15
+    value = c * s + z
+    assert np.all(np.abs(value) <= top) and np.all(np.isfinite(value.astype(np.float16)))
+    assert np.all((15 * s + z)[s[:, 0] != 1] <= top)
+    assert np.all(np.abs(value - x) <= s / 2 * (1 + 1e-12))
