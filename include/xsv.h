@@ -530,16 +530,18 @@ xsv_status xsv_page_read(const xsv_page_pool* pool, const int* block_table, int 
  *               of scale * q[t][h] . k[j][h / (q_heads / kv_heads)], times v[j].
  *   Q            : device, n_tokens rows of [q_heads][head_dim] at q_stride elements (a multiple of 8); magnitudes
  *                  below 2^64.
- *   max_new      : at least the largest number of new tokens of a sequence (a host number; larger costs time only).
+ *   max_new      : the largest number of new tokens of a sequence, a host number by which the call chooses its kernels (0:
+ *                  none has any, nothing is written).  Another one than the largest, above or below it, costs time
+ *                  and can change how results are rounded, nothing else.
  *   scale        : positive, usually 1 / sqrt(head_dim).
  *   out          : [n_tokens][q_heads][head_dim], contiguous.  Rows behind cu_new[n_seqs] are left as they were; rows
  *                  that see no token (of a sequence that the plan refused, for instance) are zero.
  *   workspace    : device, 16-byte aligned, at least xsv_page_attention_workspace() bytes; needs no clearing, holds
  *                  nothing between calls, and serves one call at a time (calls that may overlap take one each).
- * Sequences with up to 64 (head_dim 64) or 48 query rows a head (new tokens times q_heads / kv_heads) are attended by a
- * kernel that multiplies the codes themselves, the others by one that dequantises pages to fp16 first; queries,
- * probabilities and their products with the scales are fp16 operands, sums are float32.  Results do not depend on
- * timing.  Every device-side wait is bounded; a row whose wait ran out is NaN.
+ * Rows a head are new tokens times q_heads / kv_heads.  If max_new allows more than 64 (head_dim 64) or 48, sequences with
+ * more, or a sequence that is the only one, are attended by a kernel that dequantises pages to fp16 first; all others by one
+ * that multiplies the codes themselves, in tiles of 8 rows if max_new allows no more, else of 16.  Queries, probabilities
+ * and their products with the scales are fp16 operands, sums are float32.  Results do not depend on timing.  Every device-side wait is bounded; a row whose wait ran out is NaN.
  */
 xsv_status xsv_page_attention(const xsv_page_pool* pool, const void* Q, long long q_stride, int n_tokens, int q_heads,
                               const int* block_table, int table_width, const int* cu_new, const int* total_len, int n_seqs,

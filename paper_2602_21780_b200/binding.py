@@ -412,7 +412,7 @@ def page_read(pages, k_tail, block_table, total_len, token_seq, positions, strea
 
 def page_attention(Q, pages, k_tail, block_table, cu_new, total_len, max_new, *, scale=None, window=0, out=None, stream=None):
     """xsv_page_attention: Q [n, q_heads, d] (rows at any stride), new tokens of all sequences in a row -> out
-    [n, q_heads, d].  max_new: the most new tokens of a sequence.  Rows behind the last sequence are not written: they
+    [n, q_heads, d].  max_new: the most new tokens of a sequence, by which the kernels are chosen.  Rows behind the last sequence are not written: they
     keep what `out` held, and hold nothing defined if it was not given."""
     args = (Q, pages, k_tail, block_table, cu_new, total_len, max_new, scale, window, out)
     if stream is None:

@@ -775,7 +775,8 @@ extern "C" xsv_status xsv_page_attention(const xsv_page_pool* pool, const void* 
     if (n_tokens > 1 && q_stride < (long long)q_heads * pool->head_dim) return XSV_ERR_ARG;
     if (((uintptr_t)Q | (uintptr_t)out | (uintptr_t)workspace) & 15 || q_stride & 7) return XSV_ERR_SHAPE;
     const int group = q_heads / pool->kv_heads, nt = tiles_of(max_new, group);
-    if ((long long)max_new * group > 1LL << 30 || (long long)table_width * XSV_PAGE > 1LL << 30) return XSV_ERR_LIMIT;
+    // rows of a sequence and its tokens are 32-bit numbers
+    if ((long long)n_tokens * group > 1LL << 30 || (long long)table_width * XSV_PAGE > 1LL << 30) return XSV_ERR_LIMIT;
     if (workspace_bytes < workspace_of(n_tokens, n_seqs, max_new, group, pool->head_dim)) return XSV_ERR_ARG;
     p.Q = Q; p.out = out; p.table = block_table; p.cu = cu_new; p.total = total_len; p.q_stride = q_stride;
     const size_t workers = (size_t)workers_of(pool->head_dim, nt), pf = (size_t)nt * (pool->head_dim / 16) * 128 + nt * 16;
@@ -783,7 +784,7 @@ extern "C" xsv_status xsv_page_attention(const xsv_page_pool* pool, const void* 
     p.part = (float*)((char*)workspace + align256(workers * sizeof(int4)));
     void* const more = (char*)p.part + align256(2 * workers * pf * sizeof(float));
     p.scale = scale * 1.4426950408889634f;
-    p.width = table_width; p.n_seqs = n_seqs; p.n_tokens = n_tokens; p.q_heads = q_heads; p.group = group; p.max_new = max_new;
+    p.width = table_width; p.n_seqs = n_seqs; p.n_tokens = n_tokens; p.q_heads = q_heads; p.group = group;
     p.window = window;
     p.group_shift = -1;
     for (int b = 0; b < 16; ++b) if (group == 1 << b) p.group_shift = b;

@@ -11,7 +11,7 @@ struct PageAttn {
     const int* total;
     long long q_stride;
     float scale;         // times log2 e
-    int width, n_seqs, n_tokens, q_heads, group, max_new, window;
+    int width, n_seqs, n_tokens, q_heads, group, window;
     int group_shift;     // log2 of group where it is a power of two, else -1
     int row_limit;       // sequences of at most so many query rows a head go to the kernel for few rows, the others to
                          // the one for many
@@ -21,7 +21,7 @@ struct PageSeq { int new_, total, first; };     // first: position of the first 
 __device__ __forceinline__ PageSeq page_seq(const PageAttn& p, int s) {
     PageSeq q;
     const int a = min(max(p.cu[s], 0), p.n_tokens), b = min(max(p.cu[s + 1], a), p.n_tokens);
-    q.new_ = min(b - a, p.max_new);
+    q.new_ = b - a;
     q.total = (int)min((long long)max(p.total[s], 0), (long long)p.width * XSV_PAGE);
     q.first = q.total - q.new_;
     return q;

@@ -75,3 +75,23 @@ def test_a_mean_of_the_largest_values_stays_finite(new):
     scale = (1 - np.log2(1 + 1.05 * 2.0 ** -11)) / np.log2(np.e)
     out = host(binding.page_attention(q, sv.pages, sv.tail, sv.table, ints([0, new]), plan.total_len, new, scale=float(scale)))
     assert np.all(np.abs(out - top) <= 2.0 ** -11 * top)        # exactly 65504 in real arithmetic
+
+
+@pytest.mark.parametrize("d,hq,hkv", [(64, 4, 4), (128, 8, 2)])
+def test_any_bound_on_the_new_tokens_gives_the_same_rows(d, hq, hkv):
+    # it chooses kernels and tiles; the rows attended and their positions come from the lengths
+    sv = Server(4, hkv, d, "bf16", pages=60, width=14, seed=31)
+    sv.step([70, 0, 300, 5])
+    new = [3, 150, 1, 70]
+    plan = sv.step(new)
+    for bound in (1, 2, 20, 149, 224, 1 << 30):
+        sv.check_attention(plan, new, hq, max_new=bound)
+    sv.check_attention(plan, new, hq, max_new=1, window=40)
+    one = Server(1, hkv, d, "bf16", pages=20, width=14, seed=32)          # a single sequence, whose kernel a loose bound changes
+    one.step([200])
+    plan = one.step([2])
+    q = one.rnd(90, hq, d).to(one.dt)
+    for bound in (1, 2, 90):
+        out = torch.full((90, hq, d), 7.0, device="cuda", dtype=one.dt)
+        one.check_attention(plan, [2], hq, max_new=bound, q=q, out=out)
+        assert bool((out[2:] == 7).all())
