@@ -813,7 +813,6 @@ __device__ __noinline__ void mma_loop(const Params& p, const Cta c, const int x,
                 const uint32_t it = it0 + (uint32_t)i, st = it % NSTAGE;
                 mbar_wait(BAR(B_KFULL + (int)st), (it / NSTAGE) & 1u, abort_flag, status, XSV_DEV_SITE_K);
                 mbar_wait(BAR(B_VFULL + (int)st), (it / NSTAGE) & 1u, abort_flag, status, XSV_DEV_SITE_K);
-                __syncwarp();
                 if (elect_one()) mbar_arrive(BAR(B_EMPTY + (int)st));
             }
             it0 += (uint32_t)n;
@@ -859,6 +858,9 @@ __device__ __noinline__ void mma_loop(const Params& p, const Cta c, const int x,
         cT += (uint32_t)pj;
         ++uT;
     }
+    // nothing of this warp's is in flight when the block ends, also where a wait ran out and no one else waits for it
+    if (elect_one()) tc_commit(BAR(B_DRAIN + x));
+    mbar_wait_bounded(BAR(B_DRAIN + x), 0u);
 }
 
 // ------------------------------------------------------------------ the kernel
@@ -922,14 +924,6 @@ __global__ void __launch_bounds__(NTHREADS, 1) attn_tc5_kernel(const __grid_cons
     else mma_loop(p, cta, warp - (8 + NPROD), BF ? IDESC_BF16 : 0u);
     tc_fence_before();
     __syncthreads();
-    if (*abort_flag) {                                // a wait ran out (the same for the whole block): MMAs may still be in flight
-        if (warp >= 8 + NPROD) {
-            const uint32_t drain = BAR(B_DRAIN + warp - (8 + NPROD));
-            if (elect_one()) tc_commit(drain);
-            mbar_wait_bounded(drain, 0u);
-        }
-        __syncthreads();
-    }
     // Only now may the next kernel be scheduled: released at the start, its blocks would sit through this whole kernel
     // on whatever multiprocessor the grid leaves free (the one kept for the selection kernel of another stream).
     xsv_dep_release();

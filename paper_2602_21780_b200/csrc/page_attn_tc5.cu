@@ -577,7 +577,6 @@ __device__ __noinline__ void mma_loop(const Work& w, const Cta c, Units u, const
                 const uint32_t step = it + (uint32_t)k, st = step % C::NSTAGE;
                 mbar_wait(BAR(C::KFULL + (int)st), (step / C::NSTAGE) & 1u, c.abort_flag, c.status, XSV_DEV_SITE_K);
                 mbar_wait(BAR(C::VFULL + (int)st), (step / C::NSTAGE) & 1u, c.abort_flag, c.status, XSV_DEV_SITE_K);
-                __syncwarp();
                 if (elect_one()) mbar_arrive(BAR(C::EMPTY + (int)st));
             }
             it += (uint32_t)n;
@@ -611,6 +610,9 @@ __device__ __noinline__ void mma_loop(const Work& w, const Cta c, Units u, const
         cT += (uint32_t)n;
         ++uT;
     }
+    // nothing of this warp's is in flight when the block ends, also where a wait ran out and no one else waits for it
+    if (elect_one()) tc_commit(BAR(C::DRAIN + x));
+    mbar_wait_bounded(BAR(C::DRAIN + x), 0u);
 }
 
 // ------------------------------------------------------------------ the kernel
@@ -701,14 +703,6 @@ __global__ void __launch_bounds__(NTHREADS, 1) page_attn_tc5_kernel(const __grid
     else mma_loop<D>(w, cta, u, warp - (8 + NPROD));
     tc_fence_before();
     __syncthreads();
-    if (*cta.abort_flag) {                             // a wait ran out (the same for the whole block): MMAs may still be in flight
-        if (warp >= 8 + NPROD) {
-            const uint32_t drain = BAR(C::DRAIN + warp - (8 + NPROD));
-            if (elect_one()) tc_commit(drain);
-            mbar_wait_bounded(drain, 0u);
-        }
-        __syncthreads();
-    }
     xsv_dep_release();
     if (warp == 8 + NPROD + 1) {
         tc_fence_after();
