@@ -61,6 +61,7 @@ SYMBOLS = {
     "xsv_page_append": (_i, [_vp, _vp, _vp, _ll, _ll, _i, _vp, _vp, _vp, _vp, _i, _vp]),
     "xsv_page_read": (_i, [_vp, _vp, _i, _vp, _i, _vp, _vp, _i, _vp, _vp, _vp]),
     "xsv_page_attention": (_i, [_vp, _vp, _ll, _i, _i, _vp, _i, _vp, _vp, _i, _i, C.c_float, _i, _vp, _vp, C.c_size_t, _vp]),
+    "xsv_page_attention_planned": (_i, [_vp, _vp, _ll, _i, _i, _vp, _i, _vp, _vp, _vp, _i, _i, C.c_float, _i, _vp, _vp, C.c_size_t, _vp]),
     "xsv_page_attention_workspace": (C.c_size_t, [_i, _i, _i, _i, _i, _i]),
     "xsv_kernel_launches": (_ll, []),
     "xsv_strerror": (C.c_char_p, [_i]),
@@ -337,7 +338,7 @@ def _load_pages():
         mod = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(mod)
         mod.bind(*[C.cast(getattr(lib, "xsv_" + n), C.c_void_p).value for n in
-                   ("qk_norm_rope", "page_plan", "page_append", "page_read", "page_attention", "page_attention_workspace")])
+                   ("qk_norm_rope", "page_plan", "page_append", "page_read", "page_attention_planned", "page_attention_workspace")])
         _pages = mod
     return _pages
 
@@ -410,11 +411,12 @@ def page_read(pages, k_tail, block_table, total_len, token_seq, positions, strea
         return _done(_load_pages().read(*args), "xsv_page_read")
 
 
-def page_attention(Q, pages, k_tail, block_table, cu_new, total_len, max_new, *, scale=None, window=0, out=None, stream=None):
-    """xsv_page_attention: Q [n, q_heads, d] (rows at any stride), new tokens of all sequences in a row -> out
+def page_attention(Q, pages, k_tail, block_table, cu_new, total_len, max_new, *, scale=None, window=0, out=None, slot_map=None, stream=None):
+    """xsv_page_attention_planned: Q [n, q_heads, d] (rows at any stride), new tokens of all sequences in a row -> out
     [n, q_heads, d].  max_new: the most new tokens of a sequence, by which the kernels are chosen.  Rows behind the last sequence are not written: they
-    keep what `out` held, and hold nothing defined if it was not given."""
-    args = (Q, pages, k_tail, block_table, cu_new, total_len, max_new, scale, window, out)
+    keep what `out` held, and hold nothing defined if it was not given.  slot_map: the plan's, needed where it may have refused
+    sequences: their rows are then zero (without it they see the last of what the sequence held)."""
+    args = (Q, pages, k_tail, block_table, cu_new, total_len, max_new, scale, window, out, slot_map)
     if stream is None:
         return _done((_pages or _load_pages()).attention(*args), "xsv_page_attention")
     with _on(stream, pages):

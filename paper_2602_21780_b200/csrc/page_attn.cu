@@ -763,6 +763,14 @@ extern "C" xsv_status xsv_page_attention(const xsv_page_pool* pool, const void* 
                                          const int* block_table, int table_width, const int* cu_new, const int* total_len,
                                          int n_seqs, int max_new, float scale, int window, void* out, void* workspace,
                                          size_t workspace_bytes, void* stream) {
+    return xsv_page_attention_planned(pool, Q, q_stride, n_tokens, q_heads, block_table, table_width, cu_new, total_len, nullptr, n_seqs, max_new, scale,
+                                      window, out, workspace, workspace_bytes, stream);
+}
+
+extern "C" xsv_status xsv_page_attention_planned(const xsv_page_pool* pool, const void* Q, long long q_stride, int n_tokens, int q_heads,
+                                                 const int* block_table, int table_width, const int* cu_new, const int* total_len,
+                                                 const int* slot_map, int n_seqs, int max_new, float scale, int window, void* out,
+                                                 void* workspace, size_t workspace_bytes, void* stream) {
     Attn p{};
     xsv_status s = xsv_pool_view(pool, &p.pool);
     if (s != XSV_OK) return s;
@@ -778,7 +786,7 @@ extern "C" xsv_status xsv_page_attention(const xsv_page_pool* pool, const void* 
     // rows of a sequence and its tokens are 32-bit numbers
     if ((long long)n_tokens * group > 1LL << 30 || (long long)table_width * XSV_PAGE > 1LL << 30) return XSV_ERR_LIMIT;
     if (workspace_bytes < workspace_of(n_tokens, n_seqs, max_new, group, pool->head_dim)) return XSV_ERR_ARG;
-    p.Q = Q; p.out = out; p.table = block_table; p.cu = cu_new; p.total = total_len; p.q_stride = q_stride;
+    p.Q = Q; p.out = out; p.table = block_table; p.cu = cu_new; p.total = total_len; p.slot = slot_map; p.q_stride = q_stride;
     const size_t workers = (size_t)workers_of(pool->head_dim, nt), pf = (size_t)nt * (pool->head_dim / 16) * 128 + nt * 16;
     p.desc = (int4*)workspace;
     p.part = (float*)((char*)workspace + align256(workers * sizeof(int4)));

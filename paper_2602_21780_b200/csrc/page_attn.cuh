@@ -9,6 +9,7 @@ struct PageAttn {
     const int* table;
     const int* cu;
     const int* total;
+    const int* slot;     // the plan's, or null: says which sequences it refused
     long long q_stride;
     float scale;         // times log2 e
     int width, n_seqs, n_tokens, q_heads, group, window;
@@ -23,6 +24,8 @@ __device__ __forceinline__ PageSeq page_seq(const PageAttn& p, int s) {
     const int a = min(max(p.cu[s], 0), p.n_tokens), b = min(max(p.cu[s + 1], a), p.n_tokens);
     q.new_ = b - a;
     q.total = (int)min((long long)max(p.total[s], 0), (long long)p.width * XSV_PAGE);
+    // A refused sequence still holds what it held, but its new tokens are not among it: they see nothing.
+    if (p.slot && b > a && p.slot[a] < 0) q.total = 0;
     q.first = q.total - q.new_;
     return q;
 }

@@ -22,7 +22,7 @@ decltype(&xsv_qk_norm_rope) f_norm;
 decltype(&xsv_page_plan) f_plan;
 decltype(&xsv_page_append) f_append;
 decltype(&xsv_page_read) f_read;
-decltype(&xsv_page_attention) f_attention;
+decltype(&xsv_page_attention_planned) f_attention;
 decltype(&xsv_page_attention_workspace) f_workspace;
 
 [[noreturn]] void refuse(const std::string& what) { throw std::invalid_argument("xsv: " + what); }
@@ -218,7 +218,7 @@ PyObject* read(PyObject* const* a) {
 PyObject* attention(PyObject* const* a) {
     const at::Tensor &Q = tensor(a[0], "Q"), &pages = tensor(a[1], "pages"), &tail = tensor(a[2], "k_tail"), &table = tensor(a[3], "block_table"), &cu = tensor(a[4], "cu_new"),
                      &total = tensor(a[5], "total_len");
-    const at::Tensor* out = maybe(a[9], "out");
+    const at::Tensor *out = maybe(a[9], "out"), *slot = maybe(a[10], "slot_map");
     Here here(pages);
     const xsv_page_pool pool = pool_of(pages, tail);
     if (Q.dim() != 3 || total.dim() != 1) refuse("Q is [tokens, heads, head_dim], total_len a list");
@@ -227,11 +227,13 @@ PyObject* attention(PyObject* const* a) {
     const float scale = a[7] == Py_None ? 1.f / std::sqrt((float)pool.head_dim) : float_of(a[7]);
     const Rows rq = rows(Q, "Q", tail.scalar_type(), here.dev, n, heads, pool.head_dim);
     const int *pt = ints(table, "block_table", here.dev, {seqs, -1}), *pc = ints(cu, "cu_new", here.dev, {seqs + 1}), *pl = ints(total, "total_len", here.dev, {seqs});
+    const int* ps = slot ? ints(*slot, "slot_map", here.dev, {-1}) : nullptr;
+    if (slot && slot->size(0) < n) refuse("slot_map lists fewer tokens than Q holds");
     const at::Tensor to = out ? *out : empty(Q, Q.sizes());
     void* po = flat(to, "out", Q.scalar_type(), here.dev, {n, heads, pool.head_dim});
     const size_t need = f_workspace(small(n), small(seqs), max_new, small(heads), pool.kv_heads, pool.head_dim);
     const at::Tensor space = empty(pages, {(int64_t)need});
-    const xsv_status s = f_attention(&pool, rq.p, rq.stride, small(n), small(heads), pt, small(table.size(1)), pc, pl, small(seqs), max_new, scale, window, po, space.data_ptr(), need, here.stream);
+    const xsv_status s = f_attention(&pool, rq.p, rq.stride, small(n), small(heads), pt, small(table.size(1)), pc, pl, ps, small(seqs), max_new, scale, window, po, space.data_ptr(), need, here.stream);
     if (s != XSV_OK) return status(s);
     if (out) { Py_INCREF(a[9]); return a[9]; }
     return THPVariable_Wrap(to);
@@ -277,7 +279,7 @@ PyMethodDef methods[] = {{"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCA
                          {"plan", (PyCFunction)(void (*)(void))entry<plan, 6>, METH_FASTCALL, nullptr},
                          {"append", (PyCFunction)(void (*)(void))entry<append, 8>, METH_FASTCALL, nullptr},
                          {"read", (PyCFunction)(void (*)(void))entry<read, 6>, METH_FASTCALL, nullptr},
-                         {"attention", (PyCFunction)(void (*)(void))entry<attention, 10>, METH_FASTCALL, nullptr},
+                         {"attention", (PyCFunction)(void (*)(void))entry<attention, 11>, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "xsv_pages", "Argument checks and calls of the page operators; used by binding.py.", -1, methods};
 

@@ -6,7 +6,7 @@ import torch
 
 from oracle import page_oracle as orc
 from paper_2602_21780_b200 import binding
-from tests.test_gpu_page_ops import DT, HALF, PAGE, Server, host, ints
+from tests.test_gpu_page_ops import ATTN, DT, HALF, PAGE, Server, host, ints
 
 pytestmark = pytest.mark.gpu
 
@@ -95,3 +95,48 @@ def test_any_bound_on_the_new_tokens_gives_the_same_rows(d, hq, hkv):
         out = torch.full((90, hq, d), 7.0, device="cuda", dtype=one.dt)
         one.check_attention(plan, [2], hq, max_new=bound, q=q, out=out)
         assert bool((out[2:] == 7).all())
+
+
+@pytest.mark.parametrize("d,hq,hkv", [(64, 4, 2), (128, 8, 1)])
+def test_rows_of_refused_sequences_that_hold_tokens_are_zero(d, hq, hkv):
+    # refused for each of the three reasons, with few rows a head and with many, beside sequences that are served
+    held = [60, 128, 250, 64, 190]
+    for new, pages_left, width, room in (([3, 1, 2, 1, 1], 1, 5, 99),               # 1 takes the page; 3 needs one and is refused
+                                         ([100, 90, 130, 300, 2], 4, 9, 999),       # 0, 1 take two each; 2, 3 refused
+                                         ([1, 70, 1, 200, 2], 9, 4, 999),           # 3's row of the table is full, 2 and 4 fit
+                                         ([1, 5, 90, 80, 20], 9, 9, 150)):          # 3 and 4 are cut by max_tokens
+        sv = Server(5, hkv, d, "bf16", pages=40, width=width, seed=sum(new))
+        sv.step(held)
+        state = sv.state.clone()
+        state[1] = pages_left
+        plan = binding.page_plan(sv.len, ints(new), sv.table, sv.ring, state, room)
+        cu, total = plan.cu_new.cpu().numpy(), plan.total_len.cpu().numpy()
+        slot = plan.slot_map.cpu().numpy()
+        n = int(cu[-1])
+        refused = [s for s in range(5) if total[s] == held[s]]
+        assert refused == {1: [3], 4: [2, 3], 9: [3] if width == 4 else [3, 4]}[pages_left] and int(plan.ring_state[2]) == len(refused)
+        k, v = (sv.rnd(n, hkv, d).to(sv.dt) for _ in range(2))
+        binding.page_append(sv.pages, sv.tail, k, v, plan.slot_map, plan.token_seq, plan.cu_new, plan.total_len)
+        for s in range(5):
+            if s not in refused:
+                for h in range(hkv):
+                    sv.ref[s][h].append(host(k[cu[s]:cu[s + 1], h]), host(v[cu[s]:cu[s + 1], h]))
+        q = sv.rnd(n, hq, d).to(sv.dt)
+        out = host(binding.page_attention(q, sv.pages, sv.tail, sv.table, plan.cu_new, plan.total_len, max(new), slot_map=plan.slot_map))
+        for s in range(5):
+            rows = slice(cu[s], cu[s + 1])
+            if s in refused:
+                assert np.all(slot[rows] == -1) and not out[rows].any()
+                continue
+            for h in range(hq):
+                r = sv.ref[s][h // (hq // hkv)]
+                ref = orc.attention(host(q[rows, h]), r.k, r.v, d ** -0.5)
+                assert np.linalg.norm(out[rows, h] - ref) <= 3 * ATTN[sv.dt] * np.linalg.norm(ref)
+        # a plan that refused nothing: the slots change nothing, bit for bit
+    sv = Server(3, hkv, d, "fp16", pages=40, width=9, seed=1)
+    plan = sv.step([100, 2, 70])
+    q = sv.rnd(172, hq, d).to(sv.dt)
+    a = sv.check_attention(plan, [100, 2, 70], hq, q=q)
+    assert torch.equal(a, sv.check_attention(plan, [100, 2, 70], hq, q=q, slot_map=plan.slot_map))
+    with pytest.raises(ValueError, match="fewer tokens"):
+        binding.page_attention(q, sv.pages, sv.tail, sv.table, plan.cu_new, plan.total_len, 100, slot_map=plan.slot_map[:171])
