@@ -334,7 +334,7 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     const int er = __shfl_sync(0xFFFFFFFFu, e, 4 * (2 * j + c));
-                    fac[n][c] = p.scale * pow2i(er);
+                    fac[n][c] = fmaxf(p.scale * pow2i(er), MIN_FACTOR);
                     const int row = tile * ROWS + 8 * n + 2 * j + c;
                     int i, h;
                     page_row(p, row, i, h);

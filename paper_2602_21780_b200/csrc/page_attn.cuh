@@ -29,6 +29,8 @@ __device__ __forceinline__ PageSeq page_seq(const PageAttn& p, int s) {
     q.first = q.total - q.new_;
     return q;
 }
+constexpr float MIN_FACTOR = 1.17549435e-38f;     // a logit factor does not underflow: times a masked place's -infinity, 0 would be NaN
+
 // Two results -> 16 bits.  Results are means of values of at most 65504, but the rounding of the weights may carry one
 // past the largest fp16.  A NaN stays.
 template <typename T> __device__ __forceinline__ uint32_t page_result2(float a, float b) { return xsv_pack2<T>(a, b); }

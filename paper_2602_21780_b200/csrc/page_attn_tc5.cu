@@ -406,7 +406,7 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
             }
             const int e = mx > 0.f ? max((__float_as_int(mx) >> 23) - 127, -126) : 0;
             const float s1 = __int_as_float((127 - e / 2) << 23), s2 = __int_as_float((127 - (e - e / 2)) << 23);
-            sc = p.scale * __int_as_float((127 + min(e, 127)) << 23);
+            sc = fmaxf(p.scale * __int_as_float((127 + min(e, 127)) << 23), MIN_FACTOR);
 #pragma unroll
             for (int k = 0; k < D / 8; ++k) {
                 uint4 x = make_uint4(0u, 0u, 0u, 0u);

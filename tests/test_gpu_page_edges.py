@@ -140,3 +140,15 @@ def test_rows_of_refused_sequences_that_hold_tokens_are_zero(d, hq, hkv):
     assert torch.equal(a, sv.check_attention(plan, [100, 2, 70], hq, q=q, slot_map=plan.slot_map))
     with pytest.raises(ValueError, match="fewer tokens"):
         binding.page_attention(q, sv.pages, sv.tail, sv.table, plan.cu_new, plan.total_len, 100, slot_map=plan.slot_map[:171])
+
+
+@pytest.mark.parametrize("new", [1, 100])
+def test_logits_too_small_for_float32_weigh_all_tokens_alike(new):
+    # scale * |q| below the smallest float32: the factor of a masked place's -infinity must not become 0
+    sv = Server(2, 1, 64, "bf16", pages=20, width=8, seed=new)
+    sv.step([90, 30])
+    plan = sv.step([new, new])
+    q = (sv.rnd(2 * new, 2, 64) * 1e-20).to(sv.dt)
+    sv.check_attention(plan, [new, new], 2, q=q, scale=1e-30)
+    sv.check_attention(plan, [new, new], 2, q=q, scale=1e-30, window=33)
+    sv.check_attention(plan, [new, new], 2, q=(q.float() * 1e-18).to(sv.dt))          # the smallest normal queries
