@@ -548,8 +548,9 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
 // Tile x: S_k = Q K_k^T into buffer k % NBUF, then, once the softmax warps have turned it into P_k in place, O += P_k V_k.
 // The pipe executes one thread's MMAs in order, so the QK of step k + NBUF goes out right behind the PV of step k into
 // the buffer that this PV reads.
+// Inlined: called, it cost 9 % of a frame's time (1374 tokens on 21 984: 235 us against 215).
 template <int D>
-__device__ __noinline__ void mma_loop(const Work& w, const Cta c, Units u, const int x) {
+__device__ __forceinline__ void mma_loop(const Work& w, const Cta c, Units u, const int x) {
     using C = Cfg<D>;
     auto BAR = [&](int i) { return c.bars + 8u * (uint32_t)i; };
     const uint32_t tS = c.tmem + C::tm_s(0, 0) + (uint32_t)x * (C::NBUF * 64), tO = c.tmem + C::tm_o(0) + (uint32_t)(x * D);
