@@ -307,7 +307,8 @@ def kernel_launches():
 
 # ------------------------------------------------------------------ many sequences over a shared pool of 4-bit pages
 # Tensors in, tensors out: the calls run on the device of their tensors and, unless `stream` is given, on its current
-# stream; with `stream`, outputs and workspaces are allocated for that stream.  Nothing synchronises.
+# stream; with `stream`, outputs and workspaces are allocated for that stream.  Nothing synchronises.  There is no
+# backward: a result of inputs that need a gradient raises when one is asked for.
 
 class _PagePool(C.Structure):
     """xsv_page_pool, for calls of the C entry points themselves."""

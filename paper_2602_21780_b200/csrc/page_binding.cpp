@@ -5,14 +5,18 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/core/grad_mode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
+#include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
 #include <initializer_list>
 #include <stdexcept>
 #include <string>
+#include <vector>
 
 #include "../../include/xsv.h"
 
@@ -116,6 +120,18 @@ xsv_page_pool pool_of(const at::Tensor& pages, const at::Tensor& tail) {
     return p;
 }
 
+// There is no backward: results of inputs that need a gradient say so when one is asked for, instead of passing for constants.
+void no_backward(const char* call, std::initializer_list<const at::Tensor*> from, std::initializer_list<at::Tensor> to) {
+    if (!at::GradMode::is_enabled()) return;
+    std::vector<at::Tensor> need;
+    for (const at::Tensor* t : from)
+        if (t && t->requires_grad()) need.push_back(*t);
+    if (need.empty()) return;
+    const std::shared_ptr<torch::autograd::Node> node(new torch::autograd::NotImplemented(call, torch::autograd::collect_next_edges(need)), torch::autograd::deleteNode);
+    for (const at::Tensor& t : to)
+        if (t.defined()) torch::autograd::set_history(t, node);
+}
+
 PyObject* wrap(std::initializer_list<at::Tensor> ts) {
     PyObject* tuple = PyTuple_New((Py_ssize_t)ts.size());
     Py_ssize_t i = 0;
@@ -159,6 +175,7 @@ PyObject* norm_rope(PyObject* const* a) {
                                 float_of(a[8]), (xsv_rope)rope, rotary, freq, pos, head_major ? XSV_HEAD_MAJOR : XSV_TOKEN_MAJOR, qo.data_ptr(), ko.data_ptr(),
                                 v ? vo.data_ptr() : nullptr, here.stream);
     if (s != XSV_OK) return status(s);
+    no_backward("qk_norm_rope", {&q, &k, v, maybe(a[4], ""), maybe(a[5], ""), maybe(a[6], ""), maybe(a[7], "")}, {qo, ko, vo});
     return v ? wrap({qo, ko, vo}) : wrap({qo, ko});
 }
 
@@ -236,6 +253,7 @@ PyObject* attention(PyObject* const* a) {
     const xsv_status s = f_attention(&pool, rq.p, rq.stride, small(n), small(heads), pt, small(table.size(1)), pc, pl, ps, small(seqs), max_new, scale, window, po, space.data_ptr(), need, here.stream);
     if (s != XSV_OK) return status(s);
     if (out) { Py_INCREF(a[9]); return a[9]; }
+    no_backward("page_attention", {&Q}, {to});
     return THPVariable_Wrap(to);
 }
 

@@ -152,3 +152,28 @@ def test_logits_too_small_for_float32_weigh_all_tokens_alike(new):
     sv.check_attention(plan, [new, new], 2, q=q, scale=1e-30)
     sv.check_attention(plan, [new, new], 2, q=q, scale=1e-30, window=33)
     sv.check_attention(plan, [new, new], 2, q=(q.float() * 1e-18).to(sv.dt))          # the smallest normal queries
+
+
+def test_a_backward_pass_is_refused_and_not_silently_empty():
+    sv = Server(1, 2, 64, "bf16", pages=4, width=2)
+    plan = sv.step([5])
+    q, k, v = (sv.rnd(5, h, 64).to(sv.dt) for h in (4, 2, 2))
+    w = torch.nn.Parameter(torch.ones(64, device="cuda", dtype=sv.dt))
+    att = (sv.pages, sv.tail, sv.table, plan.cu_new, plan.total_len, 5)
+    with torch.no_grad():
+        plain = binding.qk_norm_rope(q, k, v, norm="rms", q_weight=w, k_weight=w)
+    assert not any(t.requires_grad for t in plain)
+    out = binding.qk_norm_rope(q, k, v, norm="rms", q_weight=w, k_weight=w)
+    assert all(torch.equal(a, b) for a, b in zip(plain, out))
+    with pytest.raises(RuntimeError, match="qk_norm_rope is not implemented"):
+        out[0].float().sum().backward()
+    assert w.grad is None
+    q.requires_grad_()
+    out = binding.page_attention(q, *att)
+    with pytest.raises(RuntimeError, match="page_attention is not implemented"):
+        out.float().sum().backward()
+    with torch.inference_mode():
+        assert torch.equal(binding.page_attention(q, *att), out)
+    k.requires_grad_()
+    binding.page_append(sv.pages, sv.tail, k, v, plan.slot_map, plan.token_seq, plan.cu_new, plan.total_len)      # stores numbers
+    assert not binding.page_attention(q.detach(), *att).requires_grad
