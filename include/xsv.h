@@ -508,8 +508,10 @@ xsv_status xsv_page_plan(const int* cached_len, const int* new_len, int n_seqs, 
 /*
  * New keys and values into the pages.  K, V: device, [n_tokens] rows of [kv_heads][head_dim] at k_stride / v_stride
  * elements (multiples of 8), the tokens of a sequence together and in order, as the plan lists them.  slot_map,
- * token_seq, cu_new, total_len: the plan's.  Tokens with slot -1 are skipped.  Keys of a page that the call fills are
- * quantised, those of the last unfilled page kept in the tail.  A call can be repeated as long as no sequence's new
+ * token_seq, cu_new, total_len: the plan's.  Slots are read once a page: the new tokens of a sequence that fall into one
+ * page go, in order, where the first of them has its slot, and are skipped together if that is -1 (so are all tokens of a
+ * refused sequence) or contradicts the lengths.  Keys of a page that the call fills are quantised, those of the last
+ * unfilled page kept in the tail.  A call can be repeated as long as no sequence's new
  * tokens span three pages after starting inside one.  A page must belong to one sequence while it is not full.
  */
 xsv_status xsv_page_append(const xsv_page_pool* pool, const void* K, const void* V, long long k_stride, long long v_stride,

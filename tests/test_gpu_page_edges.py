@@ -177,3 +177,29 @@ def test_a_backward_pass_is_refused_and_not_silently_empty():
     k.requires_grad_()
     binding.page_append(sv.pages, sv.tail, k, v, plan.slot_map, plan.token_seq, plan.cu_new, plan.total_len)      # stores numbers
     assert not binding.page_attention(q.detach(), *att).requires_grad
+
+
+@pytest.mark.parametrize("new", [6, 30])
+def test_append_reads_one_slot_a_page(new):
+    # the first new token's slot in each page decides for all of the sequence's tokens there (few of them: a warp; more: a block)
+    def grown(change):
+        sv = Server(1, 2, 64, "bf16", pages=4, width=3, seed=new)
+        sv.step([64 - new // 2])
+        plan = binding.page_plan(sv.len, ints([new]), sv.table, sv.ring, sv.state, new)
+        slots = plan.slot_map.clone()
+        for i in change:
+            slots[i] = -1
+        k, v = (torch.randn(new, 2, 64, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).to(sv.dt) for _ in range(2))
+        before = sv.pages.clone(), sv.tail.clone()
+        binding.page_append(sv.pages, sv.tail, k, v, slots, plan.token_seq, plan.cu_new, plan.total_len)
+        old, fresh = (int(x) for x in sv.table[0, :2])
+        same = [torch.equal(sv.pages[p], before[0][p]) for p in (old, fresh)]
+        return sv.pages, sv.tail.view(torch.int16), same
+
+    whole = grown([])
+    assert whole[2] == [False, False]
+    inside = grown([1, new // 2 + 1])                       # inside both pages' tokens: nothing changes
+    assert torch.equal(whole[0], inside[0]) and torch.equal(whole[1], inside[1])
+    assert grown([0])[2] == [True, False]                   # the first page's tokens are skipped, the second's are not
+    assert grown([new // 2])[2] == [False, True]
+    assert grown([0, new // 2])[2] == [True, True]
