@@ -488,7 +488,7 @@ typedef struct {
  *   cached_len   : [n_seqs], tokens that each sequence holds.
  *   new_len      : [n_seqs], tokens that it gets now (0: none); negative: the sequence ends, its pages are given back.
  *   block_table  : [n_seqs][table_width], entries of new pages are written, all others left as they are (a sequence
- *                  that ended too: its length says that it holds nothing).
+ *                  that ended too: its length says that it holds nothing).  table_width: at most 2^24.
  *   free_ring    : [n_pages], room for every page that these sequences may hold; the free pages are the ring_state[1]
  *                  entries from ring_state[0] on, cyclically.
  *   ring_state   : [2 or more], head and count; ring_state_out: [4], head, count, sequences refused, new tokens.

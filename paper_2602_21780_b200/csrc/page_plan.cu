@@ -213,7 +213,8 @@ extern "C" xsv_status xsv_page_plan(const int* cached_len, const int* new_len, i
     if (!cached_len || !new_len || !block_table || !free_ring || !ring_state || !ring_state_out || !cu_new || !total_len) return XSV_ERR_ARG;
     if (n_seqs <= 0 || table_width <= 0 || n_pages <= 0 || max_tokens < 0) return XSV_ERR_ARG;
     if (max_tokens > 0 && (!slot_map || !token_seq || !positions)) return XSV_ERR_ARG;
-    if (n_pages > XSV_PAGE_MAX_PAGES || n_seqs > XSV_PAGE_MAX_SEQS) return XSV_ERR_LIMIT;
+    // lengths are 32-bit numbers: no row holds more tokens than the attention takes
+    if (n_pages > XSV_PAGE_MAX_PAGES || n_seqs > XSV_PAGE_MAX_SEQS || (long long)table_width * XSV_PAGE > 1LL << 30) return XSV_ERR_LIMIT;
     // blocks read the inputs while others write the outputs
     if (ring_state == ring_state_out || cached_len == total_len || new_len == total_len || cached_len == cu_new || new_len == cu_new) return XSV_ERR_ARG;
     Plan p{cached_len, new_len, block_table, free_ring, ring_state, ring_state_out, cu_new, total_len, slot_map, token_seq, positions,

@@ -5,6 +5,7 @@ import os
 import numpy as np
 
 from oracle import page_oracle as orc
+from paper_2602_21780_b200 import binding
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CSRC = os.path.join(ROOT, "paper_2602_21780_b200", "csrc")
@@ -30,3 +31,9 @@ def test_no_code_stands_for_more_than_the_largest_half():
     assert np.all(np.abs(value) <= top) and np.all(np.isfinite(value.astype(np.float16)))
     assert np.all((15 * s + z)[s[:, 0] != 1] <= top)
     assert np.all(np.abs(value - x) <= s / 2 * (1 + 1e-12))
+
+
+def test_plan_refuses_rows_of_more_tokens_than_32_bits_count():
+    a = 1 << 20
+    args = [a, a + 64, 2, a, (1 << 24) + 1, a, 9, a, a + 64, a + 128, a + 256, a, a, a, 5, None]
+    assert binding.load().xsv_page_plan(*args) == 9
