@@ -168,7 +168,9 @@ PyObject* norm_rope(PyObject* const* a) {
         freq = static_cast<const float*>(flat(*f, "inv_freq", at::kFloat, here.dev, {nf}));
         pos = rope == XSV_ROPE_2D ? ints(*p, "positions", here.dev, {n, 2}) : ints(*p, "positions", here.dev, {n});
     }
-    const bool head_major = PyObject_IsTrue(a[12]) == 1;
+    const int truth = PyObject_IsTrue(a[12]);
+    if (truth < 0) { PyErr_Clear(); refuse("head_major must be true or false"); }
+    const bool head_major = truth == 1;
     const at::Tensor qo = head_major ? empty(q, {hq, n, d}) : empty(q, {n, hq, d}), ko = head_major ? empty(q, {hk, n, d}) : empty(q, {n, hk, d});
     const at::Tensor vo = v ? empty(ko, ko.sizes()) : at::Tensor();
     const xsv_status s = f_norm(rq.p, rk.p, rv.p, rq.stride, rk.stride, rv.stride, small(n), small(hq), small(hk), (int)d, dt, (xsv_norm)norm, w[0], w[1], w[2], w[3],

@@ -203,3 +203,9 @@ def test_append_reads_one_slot_a_page(new):
     assert grown([0])[2] == [True, False]                   # the first page's tokens are skipped, the second's are not
     assert grown([new // 2])[2] == [False, True]
     assert grown([0, new // 2])[2] == [True, True]
+
+
+def test_an_argument_without_a_truth_value_is_refused():
+    q = torch.zeros(3, 2, 64, device="cuda", dtype=torch.float16)
+    with pytest.raises(ValueError, match="true or false"):
+        binding.qk_norm_rope(q, q, head_major=np.zeros(2))
