@@ -536,7 +536,7 @@ xsv_status xsv_page_read(const xsv_page_pool* pool, const int* block_table, int 
  *                  none has any, nothing is written).  Another one than the largest, above or below it, costs time
  *                  and can change how results are rounded, nothing else.
  *   scale        : positive, usually 1 / sqrt(head_dim).
- *   out          : [n_tokens][q_heads][head_dim], contiguous.  Rows behind cu_new[n_seqs] are left as they were; rows
+ *   out          : [n_tokens][q_heads][head_dim], contiguous; may be Q, if that is.  Rows behind cu_new[n_seqs] are left as they were; rows
  *                  that see no token are zero.
  *   workspace    : device, 16-byte aligned, at least xsv_page_attention_workspace() bytes; needs no clearing, holds
  *                  nothing between calls, and serves one call at a time (calls that may overlap take one each).

@@ -6,14 +6,15 @@
 // lanes, 8 channels each as two 8-byte pieces that are partners in the rotation (for half-split and 2-D rotation the
 // pieces lie half a rotated span apart), so the rotation needs no exchange between lanes; the norm's sum takes
 // log2(d / 8) shuffles.  A block walks through tokens: its first threads compute a token's cosines and sines once, in
-// shared memory, for all its heads; each lane group has two rows in flight.  With few tokens a token's heads are
-// spread over several blocks (a row per lane group), which trades repeated sines for latency.
+// shared memory, for all its heads; q, k and v of a token follow one another, with up to two rows of a lane group in
+// flight (one where a part has no more heads than the block has lane groups: 8 of 128 channels, 16 of 64).  With few
+// tokens a token's heads are spread over several blocks (a row per lane group), which trades repeated sines for latency.
 //
 // Angles: position * inv_freq in turns as a float64 product, its fraction in float32: a float32 angle of a position
 // near 10^6 would be off by 0.03 rad.  Norms are float32, the layer norm's variance from differences to the mean (two
 // passes over registers); results are rounded once, to the output type.
 // Measured: 8191 tokens, 32 + 8 + 8 heads of 128, fp16: 43.6 us, 4.6 TB/s; 1374 tokens, 3 x 16 heads of 64: 6.2 us; one token: 2.5 us.
-// What is left to the copy rate is loads in flight: 8 blocks of 4 warps with two rows each; four rows a lane group or fewer
+// What is left to the copy rate is loads in flight: 8 blocks of 4 warps with one or two rows each; four rows a lane group or fewer
 // blocks were slower (48-52 us), and packed float32 arithmetic changed nothing.
 #include <algorithm>
 #include <type_traits>

@@ -209,3 +209,42 @@ def test_an_argument_without_a_truth_value_is_refused():
     q = torch.zeros(3, 2, 64, device="cuda", dtype=torch.float16)
     with pytest.raises(ValueError, match="true or false"):
         binding.qk_norm_rope(q, q, head_major=np.zeros(2))
+
+
+def served(d, hq, hkv, held, new, seed):
+    """A step over random tokens; the oracle is not grown."""
+    sv = Server(len(held), hkv, d, "bf16", pages=sum(held + new) // 64 + 3 * len(held), width=80, seed=seed)
+    for m in (held, new):
+        n = sum(m)
+        plan = binding.page_plan(sv.len, ints(m), sv.table, sv.ring, sv.state, n)
+        sv.len, sv.state = plan.total_len, plan.ring_state
+        binding.page_append(sv.pages, sv.tail, sv.rnd(n, hkv, d).to(sv.dt), sv.rnd(n, hkv, d).to(sv.dt), plan.slot_map, plan.token_seq,
+                            plan.cu_new, plan.total_len)
+    q = sv.rnd(sum(new), hq, d).to(sv.dt)
+
+    def attend(**kw):
+        return binding.page_attention(kw.pop("q", q), sv.pages, sv.tail, sv.table, plan.cu_new, plan.total_len, max(new), **kw)
+    return q, attend
+
+
+JOBS = [(64, 16, 16, [3000], [1374]), (128, 32, 8, [2000] * 4, [1] * 4), (128, 8, 2, [1500, 100, 900], [300, 1, 65]), (64, 8, 2, [700, 1], [2, 90])]
+
+
+def test_calls_on_several_streams_at_once():
+    jobs = [served(*job, seed=i)[1] for i, job in enumerate(JOBS)]
+    want = [attend() for attend in jobs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    for _ in range(10):
+        got = [attend(stream=s) for _ in range(2) for attend, s in zip(jobs, streams)]
+        torch.cuda.synchronize()
+        for a, b in zip(got, want + want):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("job", JOBS)
+def test_results_in_the_place_of_the_queries(job):
+    q, attend = served(*job, seed=7)
+    want = attend()
+    own = q.clone()
+    assert attend(q=own, out=own) is own and torch.equal(own, want)
