@@ -23,9 +23,11 @@
 // warps, so results do not depend on timing.  Each block finds its spans itself by scanning the lengths.
 //
 // Measured.  64 sequences of 900 to 16 000 tokens, one new token each, 32 query and 8 key/value heads of 128, bf16: 127 us,
-// 4.95 TB/s of 6.57 (first version 159).  Without its arithmetic this kernel takes some 110 us, without its loads 115: what is
-// left is instructions, 880 a page for a warp (333 unpack, 80 products, the rest parameters, softmax and bookkeeping).
-// 4 tokens (16 rows) over one sequence of 200 001: 75 us, 3.1 TB/s; its 64 accumulators leave 2 warps a scheduler.
+// 4.95 TB/s of 6.57 (first version 159).  Without its arithmetic this kernel takes some 110 us, without its loads 115.  No
+// unit is saturated (DRAM 81 %, ALU 55 %, issue slots 54 %): with 11 warps a multiprocessor, 880 instructions a page each
+// (333 unpack, 80 products, the rest parameters, softmax and bookkeeping), the latencies of both are not hidden.
+// 4 tokens (16 rows) over one sequence of 200 001: 75 us, 3.1 TB/s; its 64 accumulators leave 2 warps a scheduler, and
+// issue slots 41 %, tensor pipe 45 % busy.
 // One sequence of 261 tokens, 16 heads of 64: 8.8 us with the merge, launch and latency.
 #include <algorithm>
 #include <cmath>

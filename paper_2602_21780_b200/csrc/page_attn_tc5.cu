@@ -20,8 +20,9 @@
 // that bf16 of any size fits; P is fp16, sums and accumulators are float32.  Every wait is bounded; when one runs out the
 // kernel runs to its end and the rows it touched become NaN.
 //
-// Measured.  1374 tokens on 21 984, 16 heads of 64: 222 us, 575 TFLOP/s (0.41 of the sustained bf16 peak; the kernel for few
-// rows took 788); 6 chunks of 300 to 2047 tokens on up to 9000, 32 / 8 heads of 128: 440 us, 790 TFLOP/s (0.57; 2545).
+// Measured.  1374 tokens on 21 984, 16 heads of 64: 215 to 228 us, 560 to 590 TFLOP/s (0.40 to 0.42 of the sustained bf16
+// peak; the kernel for few rows took 788); 6 chunks of 300 to 2047 tokens on up to 9000, 32 / 8 heads of 128: 418 us,
+// 830 TFLOP/s (0.59; 2545).  At head_dim 64 the exponentials alone, 16 a clock and multiprocessor, take about 115 us of the former.
 // The softmax warps are busy 90 % of the time, the producers wait 55 % of it for free stages.  Storing the tiles
 // through generic addresses cost 20 %; the second half of the logits arriving under the first half's exponentials and the
 // range of unmasked pages known per unit gave 5 %; a share of 1/8 of the exponentials as polynomials cost 10 %.
@@ -34,8 +35,8 @@
 namespace {
 
 constexpr int BM = 128, NPROD = 6, NTHREADS = (8 + NPROD + 2) * 32;
-// Cost of a step with two query tiles, with one, and of entering a unit, in ticks (the ratios of the attention over
-// the contiguous cache, whose steps are two pages).
+// Cost of a step with two query tiles, with one, and of entering a unit, in ticks: the ratios of the attention over
+// the contiguous cache, whose steps are two pages, taken over as they are and not fitted to this kernel.
 constexpr int COST_PAIR = 16, COST_SINGLE = 13, COST_UNIT = 144, MIN_SPAN = 320;
 constexpr float SUM_LIMIT = 256.f;             // a row sum that reaches 2^8: look for the maximum again
 constexpr float NO_MAX = -1e30f;
