@@ -813,6 +813,7 @@ __device__ __noinline__ void mma_loop(const Params& p, const Cta c, const int x,
                 const uint32_t it = it0 + (uint32_t)i, st = it % NSTAGE;
                 mbar_wait(BAR(B_KFULL + (int)st), (it / NSTAGE) & 1u, abort_flag, status, XSV_DEV_SITE_K);
                 mbar_wait(BAR(B_VFULL + (int)st), (it / NSTAGE) & 1u, abort_flag, status, XSV_DEV_SITE_K);
+                __syncwarp();                              // every lane has passed
                 if ((threadIdx.x & 31) == 0) mbar_arrive(BAR(B_EMPTY + (int)st));
             }
             it0 += (uint32_t)n;

@@ -579,7 +579,7 @@ __device__ __forceinline__ void mma_loop(const Work& w, const Cta c, Units u, co
                 const uint32_t step = it + (uint32_t)k, st = step % C::NSTAGE;
                 mbar_wait(BAR(C::KFULL + (int)st), (step / C::NSTAGE) & 1u, c.abort_flag, c.status, XSV_DEV_SITE_K);
                 mbar_wait(BAR(C::VFULL + (int)st), (step / C::NSTAGE) & 1u, c.abort_flag, c.status, XSV_DEV_SITE_K);
-                if (elect_one()) mbar_arrive(BAR(C::EMPTY + (int)st));
+                if (elect_one()) mbar_arrive(BAR(C::EMPTY + (int)st));      // (once every lane has passed)
             }
             it += (uint32_t)n;
             continue;
