@@ -497,8 +497,8 @@ typedef struct {
  *   slot_map     : [max_tokens], page * 64 + place of each new token; -1 behind the last one and for a refused sequence.
  *   token_seq    : [max_tokens], its sequence; -1 behind the last one.   positions: [max_tokens]; 0 behind the last one.
  * Pages are taken in the order of the sequences, and given back behind the free ones (they are not taken by the same
- * call).  A sequence is refused (total_len = cached_len, its new tokens counted in cu_new, no page, slots -1) if its table row is too short, its
- * tokens do not fit max_tokens, or too few pages are free for it and those before it.  Outputs must not be inputs;
+ * call).  A sequence is refused (total_len = cached_len, its new tokens counted in cu_new, no page, slots -1) if its
+ * table row is too short, its tokens do not fit max_tokens, or too few pages are free for it and those before it.  Outputs must not be inputs;
  * what is written is not read, so a repeated call does the same.  Sum of new tokens below 2^31.
  */
 xsv_status xsv_page_plan(const int* cached_len, const int* new_len, int n_seqs, int* block_table, int table_width,
@@ -536,14 +536,15 @@ xsv_status xsv_page_read(const xsv_page_pool* pool, const int* block_table, int 
  *                  none has any, nothing is written).  Another one than the largest, above or below it, costs time
  *                  and can change how results are rounded, nothing else.
  *   scale        : positive, usually 1 / sqrt(head_dim).
- *   out          : [n_tokens][q_heads][head_dim], contiguous; may be Q, if that is.  Rows behind cu_new[n_seqs] are left as they were; rows
- *                  that see no token are zero.
+ *   out          : [n_tokens][q_heads][head_dim], contiguous; may be Q, if that is.  Rows behind cu_new[n_seqs] are
+ *                  left as they were; rows that see no token are zero.
  *   workspace    : device, 16-byte aligned, at least xsv_page_attention_workspace() bytes; needs no clearing, holds
  *                  nothing between calls, and serves one call at a time (calls that may overlap take one each).
  * Rows a head are new tokens times q_heads / kv_heads.  If max_new allows more than 64 (head_dim 64) or 48, sequences with
  * more, or a sequence that is the only one, are attended by a kernel that dequantises pages to fp16 first; all others by one
  * that multiplies the codes themselves, in tiles of 8 rows if max_new allows no more, else of 16.  Queries, probabilities
- * and their products with the scales are fp16 operands, sums are float32.  Results do not depend on timing.  Every device-side wait is bounded; a row whose wait ran out is NaN.
+ * and their products with the scales are fp16 operands, sums are float32.  Results do not depend on timing.  Every
+ * device-side wait is bounded; a row whose wait ran out is NaN.
  */
 xsv_status xsv_page_attention(const xsv_page_pool* pool, const void* Q, long long q_stride, int n_tokens, int q_heads,
                               const int* block_table, int table_width, const int* cu_new, const int* total_len, int n_seqs,
@@ -561,7 +562,8 @@ xsv_status xsv_page_attention_planned(const xsv_page_pool* pool, const void* Q, 
                                       const int* slot_map, int n_seqs, int max_new, float scale, int window, void* out,
                                       void* workspace, size_t workspace_bytes, void* stream);
 
-/* Bytes of workspace that xsv_page_attention and xsv_page_attention_planned need on the current device; 0 for arguments that it would refuse. */
+/* Bytes of workspace that xsv_page_attention and xsv_page_attention_planned need on the current device; 0 for arguments
+ * that they would refuse. */
 size_t xsv_page_attention_workspace(int n_tokens, int n_seqs, int max_new, int q_heads, int kv_heads, int head_dim);
 
 /* Kernels launched by this library in the calling process since load (the paper has no counterpart). */
