@@ -286,7 +286,9 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page_attn_kerne
         if (at == 0 || cur.pg == 0) {
             // ---- a unit begins: its query rows
             whole = cur.pg == 0;
-            const int n_rows = cur.q.new_ * p.group, t0 = min(max(p.cu[cur.s], 0), p.n_tokens), first = cur.q.total - cur.q.new_;
+            const int n_rows = cur.q.new_ * p.group, t0 = min(max(p.cu[cur.s], 0), p.n_tokens);
+            int first = cur.q.total - cur.q.new_;
+            if (cur.q.total == p.width * XSV_PAGE) first = page_seq(p, cur.s).first;      // the sequence may go on beyond its table row
             {
                 int i, h;
                 page_row(p, tile * ROWS, i, h);

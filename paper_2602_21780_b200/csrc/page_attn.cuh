@@ -18,15 +18,17 @@ struct PageAttn {
                          // the one for many
 };
 
-struct PageSeq { int new_, total, first; };     // first: position of the first new token
+// total: tokens that the table row has pages for; first: position of the first new token, which may lie beyond them
+struct PageSeq { int new_, total, first; };
 __device__ __forceinline__ PageSeq page_seq(const PageAttn& p, int s) {
     PageSeq q;
     const int a = min(max(p.cu[s], 0), p.n_tokens), b = min(max(p.cu[s + 1], a), p.n_tokens);
     q.new_ = b - a;
-    q.total = (int)min((long long)max(p.total[s], 0), (long long)p.width * XSV_PAGE);
+    int held = max(p.total[s], 0);
     // A refused sequence still holds what it held, but its new tokens are not among it: they see nothing.
-    if (p.slot && b > a && p.slot[a] < 0) q.total = 0;
-    q.first = q.total - q.new_;
+    if (p.slot && b > a && p.slot[a] < 0) held = 0;
+    q.total = min(held, p.width * XSV_PAGE);
+    q.first = held - q.new_;
     return q;
 }
 constexpr float MIN_FACTOR = 1.17549435e-38f;     // a logit factor does not underflow: times a masked place's -infinity, 0 would be NaN

@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(1024) page_list_kernel(const __grid_constant__
             page_row(p, e.row0 + here - 1, hi, h);
             const int last = q.first + hi;                    // position of the last row
             e.p0 = p.window > 0 ? max(0, q.first + lo - p.window + 1) / XSV_PAGE : 0;
-            e.pages = max(1, (last < 0 ? 0 : last / XSV_PAGE + 1) - e.p0);
+            e.pages = max(1, (last < 0 ? 0 : min(last / XSV_PAGE + 1, p.width)) - e.p0);
             e.ticks = COST_UNIT + e.pages * (here > BM ? COST_PAIR : COST_SINGLE);
             int4* dst = reinterpret_cast<int4*>(w.entry + s_base[s] + m);
             dst[0] = make_int4(e.seq, e.row0, e.p0, e.pages);
@@ -226,7 +226,7 @@ __device__ __noinline__ void producer_loop(const PageAttn& p, const Work& w, con
     uint32_t it = 0;                                           // steps of the CTA before the unit
     int slab = pw;                                             // this warp's next slab, counted from the unit's first
     for (; u.valid; next_unit(w, u)) {
-        const int n = u.kv1 - u.kv0, total = u.en.first + u.en.n_rows / p.group;
+        const int n = u.kv1 - u.kv0, total = min(u.en.first + u.en.n_rows / p.group, p.width * XSV_PAGE);
         const int* row = p.table + (size_t)u.en.seq * p.width + u.en.p0 + u.kv0;
         int ids = -1, ids_from = -32;                          // page indices of 32 steps, one a lane
         auto page_of = [&](int k) {
@@ -388,7 +388,7 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
         if (u.en.row0 + X * BM >= u.en.n_rows) { it += (uint32_t)n; continue; }     // no second tile
         int i, h;
         page_row(p, min(r, u.en.n_rows - 1), i, h);
-        const int qpos = u.en.first + i, total = u.en.first + u.en.n_rows / p.group;
+        const int qpos = u.en.first + i, total = min(u.en.first + u.en.n_rows / p.group, p.width * XSV_PAGE);
         // ---- the query row -> fp16, its largest element in [1, 2)
         float sc;
         {

@@ -248,3 +248,28 @@ def test_results_in_the_place_of_the_queries(job):
     want = attend()
     own = q.clone()
     assert attend(q=own, out=own) is own and torch.equal(own, want)
+
+
+@pytest.mark.parametrize("window", [0, 150])
+@pytest.mark.parametrize("d,hq,hkv", [(64, 4, 2), (128, 8, 1)])
+def test_tokens_beyond_a_table_row_are_masked(d, hq, hkv, window):
+    # the lengths say more than the row has pages for: positions stay, the tokens behind the row are not seen
+    sv = Server(3, hkv, d, "bf16", pages=40, width=12, seed=3)
+    sv.step([500, 320, 100])
+    for new in ([1, 3, 1], [120, 2, 60]):
+        plan = sv.step(new)
+        q = sv.rnd(sum(new), hq, d).to(sv.dt)
+        total, cu = plan.total_len.cpu().numpy(), plan.cu_new.cpu().numpy()
+        for width in (5, 2):
+            out = host(binding.page_attention(q, sv.pages, sv.tail, sv.table[:, :width].contiguous(), plan.cu_new, plan.total_len, max(new), window=window))
+            for s in range(3):
+                seen = min(int(total[s]), width * PAGE)
+                for h in range(hq):
+                    r = sv.ref[s][h // (hq // hkv)]
+                    for i in range(0, new[s], 7):
+                        at = int(total[s]) - new[s] + i
+                        lo, hi = max(0, at - window + 1) if window else 0, min(at + 1, seen)
+                        ref = np.zeros(d)
+                        if lo < hi:
+                            ref = orc.attention(host(q[cu[s] + i, h])[None], r.k[lo:hi], r.v[lo:hi], d ** -0.5)[0]
+                        assert np.linalg.norm(out[cu[s] + i, h] - ref) <= 3 * ATTN[sv.dt] * np.linalg.norm(ref)
