@@ -466,6 +466,23 @@ xsv_status xsv_qk_norm_rope(const void* q, const void* k, const void* v, long lo
                             const void* k_bias, float eps, xsv_rope rope, int rotary_dim, const float* inv_freq,
                             const int* positions, xsv_layout layout, void* q_out, void* k_out, void* v_out, void* stream);
 
+#define XSV_ROPE_MAX_AXES 8
+
+/*
+ * The same with several positions a token (time, height, width of a video's patches): frequency i turns by position axes[i].
+ *   rope          : XSV_ROPE_HALF or XSV_ROPE_PAIRS.
+ *   positions     : device, int [n_tokens][n_axes].
+ *   axes          : device, int [rotary_dim / 2], each from 0 to n_axes - 1 (in any order: runs of one axis, or the axes in turn);
+ *                   a channel pair whose entry is none of these is not rotated.
+ *   n_axes        : 1 to XSV_ROPE_MAX_AXES.
+ */
+xsv_status xsv_qk_norm_rope_axes(const void* q, const void* k, const void* v, long long q_stride, long long k_stride,
+                                 long long v_stride, int n_tokens, int q_heads, int kv_heads, int head_dim, xsv_dtype dtype,
+                                 xsv_norm norm, const void* q_weight, const void* q_bias, const void* k_weight,
+                                 const void* k_bias, float eps, xsv_rope rope, int rotary_dim, const float* inv_freq,
+                                 const int* positions, const int* axes, int n_axes, xsv_layout layout, void* q_out,
+                                 void* k_out, void* v_out, void* stream);
+
 #define XSV_PAGE_TOKENS 64
 #define XSV_PAGE_MAX_SEQS 8192           /* sequences (rows of a block table, tails of a pool) */
 #define XSV_PAGE_MAX_PAGES (1 << 25)     /* pages of a pool: slots are 32-bit                 */
@@ -565,6 +582,97 @@ xsv_status xsv_page_attention_planned(const xsv_page_pool* pool, const void* Q, 
 /* Bytes of workspace that xsv_page_attention and xsv_page_attention_planned need on the current device; 0 for arguments
  * that they would refuse. */
 size_t xsv_page_attention_workspace(int n_tokens, int n_seqs, int max_new, int q_heads, int kv_heads, int head_dim);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * The same pool at 8 bits, and attention over selected pages (no counterpart in the paper; its selection, Eq. 3 to 8, prunes a
+ * stream's cache for good, this one picks what each new token reads and keeps all).
+ *
+ * A page holds 64 tokens of every key/value head of one layer as e4m3 codes, with one scale for the block's keys and one for
+ * its values, per head: s = 2^e with the smallest e from -80 to 8 for which 448 s reaches the largest magnitude that the
+ * page has been given; code = nearest-even e4m3 of x / s, value = code * s: off by at most 2^-4 of x, or by 2^-10 s where |x| is
+ * below 2^-6 s.  Codes are written as their tokens come (there is no 16-bit tail); when a later token of an unfilled page
+ * needs a larger scale, the codes that stand there are brought to it, which rounds only those that become smaller than
+ * 2^-6 s.  Inputs are finite; magnitudes beyond 65504 count as 65504, whose code stands for 65536 (read back as 65504 in
+ * fp16).  A full page also has its mean key, in whole numbers of 8 bits with a factor, for xsv_page8_select.
+ *
+ * Block tables, lengths and slots are those of xsv_page_plan.  A step of a model: xsv_page_plan once, then per layer
+ * xsv_qk_norm_rope, xsv_page8_append, and xsv_page8_attention, or xsv_page8_select and xsv_page8_attention_selected.
+ * What stands above about state, memory, devices, capture and index values holds for these entry points too.
+ */
+#define XSV_PAGE8_MAX_TOP 1024           /* pages that a token selects                    */
+#define XSV_PAGE8_MAX_WIDTH 32768        /* pages of a block table's row in a selection   */
+#define XSV_PAGE8_MAX_GROUP 128          /* query heads of a key/value head in a selection */
+
+/* The pool of one layer: n_pages * kv_heads records of 130 * head_dim bytes (csrc/page8_layout.cuh).  Needs no clearing. */
+typedef struct {
+    void* records;      /* device, 16-byte aligned */
+    long long n_pages;
+    int kv_heads;
+    int head_dim;       /* 64 or 128 */
+    xsv_dtype dtype;    /* of keys, values, queries and results */
+} xsv_page8_pool;
+
+/*
+ * New keys and values into the pages: arguments as for xsv_page_append.  A call can be repeated.  The tokens of a page
+ * that was begun before must still stand in it.
+ */
+xsv_status xsv_page8_append(const xsv_page8_pool* pool, const void* K, const void* V, long long k_stride, long long v_stride,
+                            int n_tokens, const int* slot_map, const int* token_seq, const int* cu_new, const int* total_len,
+                            int n_seqs, void* stream);
+
+/* What the pages hold, as values: as xsv_page_read. */
+xsv_status xsv_page8_read(const xsv_page8_pool* pool, const int* block_table, int table_width, const int* total_len,
+                          int n_seqs, const int* token_seq, const int* positions, int n_rows, void* K_out, void* V_out,
+                          void* stream);
+
+/*
+ * Causal attention of the new tokens over all that their sequences hold: as xsv_page_attention_planned (slot_map may be
+ * NULL).  Queries, codes and probabilities are fp16 operands, sums are float32.
+ */
+xsv_status xsv_page8_attention(const xsv_page8_pool* pool, const void* Q, long long q_stride, int n_tokens, int q_heads,
+                               const int* block_table, int table_width, const int* cu_new, const int* total_len,
+                               const int* slot_map, int n_seqs, int max_new, float scale, int window, void* out,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that xsv_page8_attention needs on the current device; 0 for arguments that it would refuse. */
+size_t xsv_page8_attention_workspace(int n_tokens, int n_seqs, int max_new, int q_heads, int kv_heads, int head_dim);
+
+/*
+ * The pages that each new token attends to, for every key/value head: of the pages up to the token's own, the `first` first
+ * ones and the `recent` last ones (its own among them), and of those between the best by their score, `top` pages in all.
+ *   score        : the largest over the group's query heads of (dot * factor) * a, products in float32, where dot is the
+ *                  whole number sum of q8 * mean, a = max(max |q|, 2^-60) and q8 = nearest-even of q * (127 / a), and
+ *                  mean = nearest-even of S * (127 / A), factor = A * s / 64 with S the sum of a channel's 64 key codes and A the
+ *                  largest |S| (0 where that is 0): a logit against the page's mean key, but for a constant.  Equal scores:
+ *                  the lower page first.  A page that the table does not have is not taken.
+ *   Q            : device, n_tokens rows of [q_heads][head_dim] at q_stride elements (a multiple of 8).
+ *   token_seq, positions : the plan's, [n_tokens]; a token of sequence -1 selects nothing.  All pages before the token's own
+ *                  must have been filled by appends.
+ *   slot_map     : the plan's, or NULL; a token without a slot (of a refused sequence) selects nothing.
+ *   top, first, recent : first + recent <= top, recent at least 1.
+ *   selected     : [n_tokens][kv_heads][top], numbers of pages in the sequence, ascending, then -1.
+ * Limits: top, the table's width and the query heads of a key/value head as above.
+ */
+xsv_status xsv_page8_select(const xsv_page8_pool* pool, const void* Q, long long q_stride, int n_tokens, int q_heads,
+                            const int* block_table, int table_width, int n_seqs, const int* token_seq, const int* positions,
+                            const int* slot_map, int top, int first, int recent, int* selected, void* stream);
+
+/*
+ * Attention of every new token over the pages that `selected` lists for it, up to its own position:
+ *   out[t][h] = softmax over the positions j <= positions[t] of these pages of scale * q[t][h] . k[j], times v[j].
+ *   selected     : [n_tokens][kv_heads][top], ascending; an entry that is not above the one before it, negative, or not a
+ *                  page that the token's sequence has at its position is passed over.
+ *   token_seq, positions : the plan's.  Rows of tokens of sequence -1 are left as they were, rows that see no page are zero.
+ *   The others   : as for xsv_page_attention; the workspace has xsv_page8_attention_selected_workspace() bytes.
+ */
+xsv_status xsv_page8_attention_selected(const xsv_page8_pool* pool, const void* Q, long long q_stride, int n_tokens,
+                                        int q_heads, const int* block_table, int table_width, int n_seqs,
+                                        const int* token_seq, const int* positions, const int* selected, int top, float scale,
+                                        void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that xsv_page8_attention_selected needs on the current device, whatever the number of tokens; 0 for
+ * arguments that it would refuse. */
+size_t xsv_page8_attention_selected_workspace(int q_heads, int kv_heads, int head_dim);
 
 /* Kernels launched by this library in the calling process since load (the paper has no counterpart). */
 long long xsv_kernel_launches(void);

@@ -57,6 +57,15 @@ SYMBOLS = {
     "xsv_plan_batch_groups": (_i, [_i, C.POINTER(_i), C.POINTER(_i), _i, _i]),
     "xsv_qk_norm_rope": (_i, [_vp, _vp, _vp, _ll, _ll, _ll, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, C.c_float, _i, _i,
                               _vp, _vp, _i, _vp, _vp, _vp, _vp]),
+    "xsv_qk_norm_rope_axes": (_i, [_vp, _vp, _vp, _ll, _ll, _ll, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, C.c_float, _i, _i,
+                                   _vp, _vp, _vp, _i, _i, _vp, _vp, _vp, _vp]),
+    "xsv_page8_append": (_i, [_vp, _vp, _vp, _ll, _ll, _i, _vp, _vp, _vp, _vp, _i, _vp]),
+    "xsv_page8_read": (_i, [_vp, _vp, _i, _vp, _i, _vp, _vp, _i, _vp, _vp, _vp]),
+    "xsv_page8_attention": (_i, [_vp, _vp, _ll, _i, _i, _vp, _i, _vp, _vp, _vp, _i, _i, C.c_float, _i, _vp, _vp, C.c_size_t, _vp]),
+    "xsv_page8_attention_workspace": (C.c_size_t, [_i, _i, _i, _i, _i, _i]),
+    "xsv_page8_select": (_i, [_vp, _vp, _ll, _i, _i, _vp, _i, _i, _vp, _vp, _vp, _i, _i, _i, _vp, _vp]),
+    "xsv_page8_attention_selected": (_i, [_vp, _vp, _ll, _i, _i, _vp, _i, _i, _vp, _vp, _vp, _i, C.c_float, _vp, _vp, C.c_size_t, _vp]),
+    "xsv_page8_attention_selected_workspace": (C.c_size_t, [_i, _i, _i]),
     "xsv_page_plan": (_i, [_vp, _vp, _i, _vp, _i, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp]),
     "xsv_page_append": (_i, [_vp, _vp, _vp, _ll, _ll, _i, _vp, _vp, _vp, _vp, _i, _vp]),
     "xsv_page_read": (_i, [_vp, _vp, _i, _vp, _i, _vp, _vp, _i, _vp, _vp, _vp]),
@@ -316,6 +325,11 @@ class _PagePool(C.Structure):
                 ("kv_heads", C.c_int), ("head_dim", C.c_int), ("dtype", C.c_int)]
 
 
+class _Page8Pool(C.Structure):
+    """xsv_page8_pool, for calls of the C entry points themselves."""
+    _fields_ = [("records", C.c_void_p), ("n_pages", C.c_longlong), ("kv_heads", C.c_int), ("head_dim", C.c_int), ("dtype", C.c_int)]
+
+
 PagePlan = collections.namedtuple("PagePlan", "cu_new total_len slot_map token_seq positions ring_state")
 PagePlan.__doc__ = """What page_plan() says of a step (see xsv_page_plan); ring_state is the next step's."""
 
@@ -339,7 +353,9 @@ def _load_pages():
         mod = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(mod)
         mod.bind(*[C.cast(getattr(lib, "xsv_" + n), C.c_void_p).value for n in
-                   ("qk_norm_rope", "page_plan", "page_append", "page_read", "page_attention_planned", "page_attention_workspace")])
+                   ("qk_norm_rope", "page_plan", "page_append", "page_read", "page_attention_planned", "page_attention_workspace",
+                    "qk_norm_rope_axes", "page8_append", "page8_read", "page8_attention", "page8_attention_workspace", "page8_select",
+                    "page8_attention_selected", "page8_attention_selected_workspace")])
         _pages = mod
     return _pages
 
@@ -369,14 +385,15 @@ def page_pool(n_pages, max_seqs, kv_heads, head_dim, dtype, device="cuda"):
 
 
 def qk_norm_rope(q, k, v=None, *, norm=None, q_weight=None, q_bias=None, k_weight=None, k_bias=None, eps=1e-6, rope=None,
-                 inv_freq=None, positions=None, head_major=False, stream=None):
+                 inv_freq=None, positions=None, axes=None, head_major=False, stream=None):
     """xsv_qk_norm_rope: q [n, q_heads, d], k and v [n, kv_heads, d] (rows may be views into a projection's output) ->
     normalised, rotated and laid out (q, k, v), [n, heads, d] or, with head_major, [heads, n, d].  norm: None, "rms",
     "layer"; rope: None, "half", "pairs", "2d" with inv_freq float32 [rotary_dim / 2] ([d / 4] for "2d") and positions
-    int32 [n] ([n, 2])."""
+    int32 [n] ([n, 2]).  axes (xsv_qk_norm_rope_axes; "half" and "pairs"): int32 [rotary_dim / 2], which of a token's several
+    positions, int32 [n, axes], each frequency turns by."""
     if norm not in NORMS or rope not in ROPES:
         raise ValueError(f"xsv: norm {norm!r} or rope {rope!r} is unknown")
-    args = (q, k, v, NORMS[norm], q_weight, q_bias, k_weight, k_bias, eps, ROPES[rope], inv_freq, positions, head_major)
+    args = (q, k, v, NORMS[norm], q_weight, q_bias, k_weight, k_bias, eps, ROPES[rope], inv_freq, positions, axes, head_major)
     if stream is None:
         return _done((_pages or _load_pages()).norm_rope(*args), "xsv_qk_norm_rope")
     with _on(stream, q):
@@ -422,3 +439,60 @@ def page_attention(Q, pages, k_tail, block_table, cu_new, total_len, max_new, *,
         return _done((_pages or _load_pages()).attention(*args), "xsv_page_attention")
     with _on(stream, pages):
         return _done(_load_pages().attention(*args), "xsv_page_attention")
+
+
+# ------------------------------------------------------------------ the same pool at 8 bits; attention over selected pages
+def page8_pool(n_pages, kv_heads, head_dim, device="cuda"):
+    """Uninitialised storage of one layer's pool of 8-bit pages, as the page8_* calls take it."""
+    import torch
+    return torch.empty(n_pages, kv_heads, 130 * head_dim, dtype=torch.uint8, device=device)
+
+
+def page8_append(pages, K, V, slot_map, token_seq, cu_new, total_len, stream=None):
+    """xsv_page8_append: K, V [n, kv_heads, d] (rows at any stride) into the pool, by the plan's arrays."""
+    args = (pages, K, V, slot_map, token_seq, cu_new, total_len)
+    if stream is None:
+        _done((_pages or _load_pages()).append8(*args), "xsv_page8_append")
+        return
+    with _on(stream, pages):
+        _done(_load_pages().append8(*args), "xsv_page8_append")
+
+
+def page8_read(pages, block_table, total_len, token_seq, positions, dtype, stream=None):
+    """xsv_page8_read: the tokens (token_seq[i], positions[i]) as values of `dtype` (torch.float16 or torch.bfloat16),
+    (K, V) [rows, kv_heads, d]."""
+    args = (pages, block_table, total_len, token_seq, positions, dtype)
+    if stream is None:
+        return _done((_pages or _load_pages()).read8(*args), "xsv_page8_read")
+    with _on(stream, pages):
+        return _done(_load_pages().read8(*args), "xsv_page8_read")
+
+
+def page8_attention(Q, pages, block_table, cu_new, total_len, max_new, *, scale=None, window=0, out=None, slot_map=None, stream=None):
+    """xsv_page8_attention: as page_attention, over 8-bit pages."""
+    args = (Q, pages, block_table, cu_new, total_len, max_new, scale, window, out, slot_map)
+    if stream is None:
+        return _done((_pages or _load_pages()).attention8(*args), "xsv_page8_attention")
+    with _on(stream, pages):
+        return _done(_load_pages().attention8(*args), "xsv_page8_attention")
+
+
+def page8_select(Q, pages, block_table, token_seq, positions, top, *, first=1, recent=2, slot_map=None, stream=None):
+    """xsv_page8_select: Q [n, q_heads, d] (rows at any stride), the plan's token_seq and positions -> int32 [n, kv_heads, top],
+    the pages that each token attends to: the `first` first ones, the `recent` last ones, and the best-scored of those between,
+    ascending, then -1.  slot_map: the plan's, needed where it may have refused sequences: their tokens select nothing."""
+    args = (Q, pages, block_table, token_seq, positions, top, first, recent, slot_map)
+    if stream is None:
+        return _done((_pages or _load_pages()).select8(*args), "xsv_page8_select")
+    with _on(stream, pages):
+        return _done(_load_pages().select8(*args), "xsv_page8_select")
+
+
+def page8_attention_selected(Q, pages, block_table, token_seq, positions, selected, *, scale=None, out=None, stream=None):
+    """xsv_page8_attention_selected: attention of each token over its selected pages, int32 [n, kv_heads, top], up to its own
+    position -> out [n, q_heads, d].  Rows of tokens of sequence -1 are not written, rows that see no page are zero."""
+    args = (Q, pages, block_table, token_seq, positions, selected, scale, out)
+    if stream is None:
+        return _done((_pages or _load_pages()).attention8_selected(*args), "xsv_page8_attention_selected")
+    with _on(stream, pages):
+        return _done(_load_pages().attention8_selected(*args), "xsv_page8_attention_selected")

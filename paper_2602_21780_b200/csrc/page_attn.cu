@@ -66,46 +66,12 @@ template <int D, int NT> struct Shape {
     static constexpr size_t SMEM = (size_t)WARPS * PER_WARP;
 };
 
-__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-// c = a b
-__device__ __forceinline__ void mma0(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
-}
-// d = a b + c
-__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, const float (&c)[4]) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
-                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1),
-                   "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
-}
-__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
-    uint32_t y;
-    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t hmul2_u(uint32_t a, uint32_t b) {
-    uint32_t d;
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
 __device__ __forceinline__ uint32_t hfnma2_u(uint32_t a, uint32_t b, uint32_t c) {      // c - a b
     const __half2 r = __hfma2(__hneg2(*reinterpret_cast<__half2*>(&a)), *reinterpret_cast<__half2*>(&b), *reinterpret_cast<__half2*>(&c));
     return *reinterpret_cast<const uint32_t*>(&r);
 }
 constexpr uint32_t ONES = 0x3C003C00u, EIGHTS = 0x48004800u, MINUS_EIGHTS = 0xC800C800u;   // pairs of fp16
 constexpr uint32_t MINUS_LO = 0x80088008u, MINUS_HI = 0x80808080u;   // -8 in the codes' units: rows g, rows g + 8
-__device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
-// halves i of two 8-half vectors as a pair
-__device__ __forceinline__ uint32_t pair_at(const uint4& a, const uint4& b, int i) {
-    return __byte_perm(word(a, i >> 1), word(b, i >> 1), i & 1 ? 0x7632 : 0x5410);
-}
-__device__ __forceinline__ float pow2i(int e) {            // 2^e, clamped to what float32 holds as a normal number
-    return __int_as_float((min(max(e, -126), 127) + 127) << 23);
-}
-
 // A sequence as the split sees it.
 struct Seq { int new_, total, p0, pages, tiles; };
 __device__ __forceinline__ Seq seq_of(const Attn& p, int s, int rows) {
@@ -708,7 +674,6 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) page_attn_merge_kernel(const
 }
 
 // ------------------------------------------------------------------ host side
-constexpr size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 
 template <int D, int NT> int workers_at() { return xsv_sm_count() * Shape<D, NT>::BLOCKS * WARPS; }
 int workers_of(int head_dim, int nt) {

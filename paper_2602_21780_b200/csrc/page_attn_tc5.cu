@@ -28,6 +28,7 @@
 // range of unmasked pages known per unit gave 5 %; a share of 1/8 of the exponentials as polynomials cost 10 %.
 #include <algorithm>
 
+#include "page8_layout.cuh"
 #include "page_attn.cuh"
 #include "tc5_ptx.cuh"
 #include "xsv_kernels.h"
@@ -199,10 +200,6 @@ struct Cta {
 // then code * s + z is rounded once.
 __device__ __forceinline__ uint32_t dq_lo(uint32_t w, uint32_t s, uint32_t z) { return hfma2_u(hsub2_u((w & 0x000F000Fu) | 0x64006400u, 0x64006400u), s, z); }
 __device__ __forceinline__ uint32_t dq_hi(uint32_t w, uint32_t s, uint32_t z) { return hfma2_u(hsub2_u((w & 0x00F000F0u) | 0x54005400u, 0x54005400u), s, z); }
-__device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
-__device__ __forceinline__ uint32_t pair_at(const uint4& a, const uint4& b, int i) {
-    return __byte_perm(word(a, i >> 1), word(b, i >> 1), i & 1 ? 0x7632 : 0x5410);
-}
 // the row of the key tile, and the column of S and the value tile, of token 16 m + 8 b + 2 j + h
 __host__ __device__ constexpr int place(int m, int b, int j, int h) { return 16 * j + 4 * m + 2 * b + h; }
 __host__ __device__ constexpr int token_at(int pos) { return 16 * (pos >> 2 & 3) + 8 * (pos >> 1 & 1) + 2 * (pos >> 4) + (pos & 1); }
@@ -358,6 +355,151 @@ __device__ __noinline__ void producer_loop(const PageAttn& p, const Work& w, con
     }
 }
 
+// 8-bit pages: the codes as fp16, without their scale, which the softmax warps take in; a stage's scales beside its page.
+// A slab is 64 tokens x 64 channels of keys, or half the values: at head_dim 128 all channels of 32 tokens (a lane's 8 tokens are
+// 8 consecutive columns of the tile), at 64 all 64 tokens.
+template <typename T, int D>
+__device__ __noinline__ void producer8_loop(const PageAttn& p, const Work& w, const Cta c, Units u) {
+    using C = Cfg<D>;
+    using R = Page8Rec<D>;
+    constexpr int SLABS = 2 * C::BLK;
+    const int lane = threadIdx.x & 31, pw = (threadIdx.x >> 5) - 8, g = lane >> 2, j = lane & 3, odd = g & 1;
+    auto BAR = [&](int i) { return c.bars + 8u * (uint32_t)i; };
+    struct Regs { uint4 code[8]; float2 scale; };
+    uint32_t it = 0;                                           // steps of the CTA before the unit
+    int slab = pw;                                             // this warp's next slab, counted from the unit's first
+    for (; u.valid; next_unit(w, u)) {
+        const int n = u.kv1 - u.kv0, total = min(u.en.first + u.en.n_rows / p.group, p.width * XSV_PAGE);
+        const int* row = p.table + (size_t)u.en.seq * p.width + u.en.p0 + u.kv0;
+        int ids = -1, ids_from = -32;                          // page indices of 32 steps, one a lane
+        auto page_of = [&](int k) {
+            if (k - ids_from >= 32) {
+                ids_from = k & ~31;
+                const int pg = u.en.p0 + u.kv0 + ids_from + lane;
+                ids = ids_from + lane < n && pg < p.width && pg * XSV_PAGE < total ? row[ids_from + lane] : -1;
+                if ((unsigned long long)(long long)ids >= (unsigned long long)p.pool.n_pages) ids = -1;
+            }
+            return __shfl_sync(0xFFFFFFFFu, ids, k & 31);
+        };
+        auto fetch = [&](int sl, int page, Regs& r) {
+            if (page < 0) return;
+            const uint8_t* rec = page8_rec<D>(p.pool, page, u.h);
+            const int part = sl % SLABS;
+            if (part < C::BLK) {
+#pragma unroll
+                for (int a = 0; a < 8; ++a) r.code[a] = ld16(rec + R::K_CODES + ((a * C::BLK + part) * 32 + lane) * 16);
+                if (part == 0) r.scale = *reinterpret_cast<const float2*>(rec + R::PARAMS);
+            } else if (D == 128) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) r.code[i] = ld16(rec + R::V_CODES + ((8 * (part - C::BLK) + i) * 32 + lane) * 16);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint2 x = *reinterpret_cast<const uint2*>(rec + R::V_CODES + (2 * i * 32 + lane) * 8);
+                    const uint2 y = *reinterpret_cast<const uint2*>(rec + R::V_CODES + ((2 * i + 1) * 32 + lane) * 8);
+                    r.code[i] = make_uint4(x.x, x.y, y.x, y.y);
+                }
+            }
+        };
+        Regs cur{}, nxt{};
+        int page = -1, page_n = -1;
+        if (slab < n * SLABS) {
+            page = page_of(slab / SLABS);
+            fetch(slab, page, cur);
+        }
+        while (slab < n * SLABS) {
+            const int k = slab / SLABS, part = slab % SLABS, next = slab + NPROD;
+            if (next < n * SLABS) {
+                page_n = page_of(next / SLABS);
+                fetch(next, page_n, nxt);
+            }
+            const uint32_t step = it + (uint32_t)k, st = step % C::NSTAGE;
+            if (step >= (uint32_t)C::NSTAGE) mbar_wait(BAR(C::EMPTY + (int)st), (step / C::NSTAGE - 1u) & 1u, c.abort_flag, c.status, XSV_DEV_SITE_STAGE);
+            const int held = page < 0 ? 0 : total - (u.en.p0 + u.kv0 + k) * XSV_PAGE;      // tokens of the page
+            const uint32_t stage = c.base + C::OFF_KV + st * C::STAGE;
+            if (part < C::BLK) {
+                const uint32_t tile = stage + part * 8192;
+                if (part == 0 && lane == 0) {
+                    asm volatile("st.shared.b32 [%0], %1;" ::"r"(c.page_ok + 4u * st), "r"(page >= 0 ? 1 : 0) : "memory");
+                    // keys' scale, and the values' as the exponent that the logits are moved by
+                    asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(c.page_ok + 4u * C::NSTAGE + 8u * st), "f"(page >= 0 ? cur.scale.x : 1.f),
+                                 "f"(page >= 0 ? (float)p8_exponent_of(cur.scale.y) : 0.f) : "memory");
+                }
+                // 16 channels of a token: two chunks of its row (keys of places without a token are masked, whatever they are)
+#pragma unroll
+                for (int a = 0; a < 8; ++a) {
+                    uint32_t h[8];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p8_halves(word(cur.code[a], i), h[2 * i], h[2 * i + 1]);
+                    const int r = place(a >> 1, a & 1, g >> 1, odd);
+                    sts16(tile + swz(r, 2 * j), make_uint4(h[0], h[1], h[2], h[3]));
+                    sts16(tile + swz(r, 2 * j + 1), make_uint4(h[4], h[5], h[6], h[7]));
+                }
+            } else {
+                const int v = part - C::BLK;
+                const uint32_t tile = stage + C::K_TILE;
+                if (held < XSV_PAGE) {                         // places without a token: zeros, whatever the record holds there
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        if (D == 128) {                        // i = 4 (t % 2) + 2 b + h
+                            if (16 * (2 * v + (i >> 2)) + 8 * (i >> 1 & 1) + 2 * j + (i & 1) >= held) cur.code[i] = make_uint4(0u, 0u, 0u, 0u);
+                        } else {                               // i = 2 t + b, two tokens
+                            const int tok = 8 * i + 2 * j;
+                            if (tok >= held) cur.code[i].x = cur.code[i].y = 0u;
+                            if (tok + 1 >= held) cur.code[i].z = cur.code[i].w = 0u;
+                        }
+                    }
+                }
+                if (D == 128) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {              // channels 16 g + 4 i to + 3: pairs of tokens h = 0, 1 of four (t, b)
+                        uint32_t e[4][4];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const uint32_t x = word(cur.code[2 * q], i), y = word(cur.code[2 * q + 1], i);
+                            p8_halves(__byte_perm(x, y, 0x5140), e[0][q], e[1][q]);
+                            p8_halves(__byte_perm(x, y, 0x7362), e[2][q], e[3][q]);
+                        }
+#pragma unroll
+                        for (int q = 0; q < 4; q += 2) {       // lanes of odd g in another order, so that a store's lanes touch different banks
+                            const uint4 a = make_uint4(e[q][0], e[q][1], e[q][2], e[q][3]), b = make_uint4(e[q + 1][0], e[q + 1][1], e[q + 1][2], e[q + 1][3]);
+                            const int r = 16 * g + 4 * i + q;
+                            sts16(tile + swz(r + odd, 2 * j + v), odd ? b : a);
+                            sts16(tile + swz(r + (odd ^ 1), 2 * j + v), odd ? a : b);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {              // channels 8 g + 4 i to + 3, 16 tokens
+                        uint32_t e[4][8];
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) {
+                            const uint32_t x = word(cur.code[q], i), y = word(cur.code[q], i + 2);
+                            p8_halves(__byte_perm(x, y, 0x5140), e[0][q], e[1][q]);
+                            p8_halves(__byte_perm(x, y, 0x7362), e[2][q], e[3][q]);
+                        }
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const uint4 a = make_uint4(e[q][0], e[q][1], e[q][2], e[q][3]), b = make_uint4(e[q][4], e[q][5], e[q][6], e[q][7]);
+                            const int r = 8 * g + 4 * i + q;
+                            sts16(tile + swz(r, 2 * j + odd), odd ? b : a);
+                            sts16(tile + swz(r, 2 * j + (odd ^ 1)), odd ? a : b);
+                        }
+                    }
+                }
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(BAR((part < C::BLK ? C::KFULL : C::VFULL) + (int)st));
+            cur = nxt;
+            page = page_n;
+            slab = next;
+        }
+        it += (uint32_t)n;
+        slab -= n * SLABS;
+    }
+}
+
 // ------------------------------------------------------------------ softmax and epilogue
 __device__ __forceinline__ void softmax32(const uint32_t (&v)[32], unsigned long long sc2, unsigned long long nm2, unsigned long long& ls2,
                                           uint32_t (&pk)[16]) {
@@ -371,7 +513,9 @@ __device__ __forceinline__ void softmax32(const uint32_t (&v)[32], unsigned long
     }
 }
 
-template <typename T, int D>
+// BITS 8: a page's keys have a scale, which goes into the factor of its logits, and its values one, 2^ev, by which the weights are
+// multiplied; so the logits are moved by ev, the maximum is that of the moved ones, and the sum takes ev back.
+template <typename T, int D, int BITS>
 __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, const Cta c, Units u) {
     using C = Cfg<D>;
     auto BAR = [&](int i) { return c.bars + 8u * (uint32_t)i; };
@@ -439,13 +583,19 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
             tmem_ld32(tSb, va);
             int ok;
             asm volatile("ld.shared.b32 %0, [%1];" : "=r"(ok) : "r"(c.page_ok + 4u * ((it + (uint32_t)k) % C::NSTAGE)) : "memory");
+            float sp = sc, ev = 0.f;
+            if (BITS == 8) {
+                float ks;
+                asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(ks), "=f"(ev) : "r"(c.page_ok + 4u * C::NSTAGE + 8u * ((it + (uint32_t)k) % C::NSTAGE)) : "memory");
+                sp = fmaxf(sc * ks, MIN_FACTOR);
+            }
             tc_wait_ld();
             tmem_ld32(tSb + 32u, vb);              // arrives under the first half's exponentials
             const bool mask = !(tok0 >= tok_lo && tok0 <= tok_hi && ok);     // uniform
             float ls = 0.f;
             bool careful = first || mask;
             if (!careful) {
-                const unsigned long long sc2 = f2_pack(sc, sc), nm2 = f2_pack(-m_used, -m_used);
+                const unsigned long long sc2 = f2_pack(sp, sp), nm2 = f2_pack(BITS == 8 ? ev - m_used : -m_used, BITS == 8 ? ev - m_used : -m_used);
                 unsigned long long ls2 = f2_pack(0.f, 0.f);
                 softmax32(va, sc2, nm2, ls2, pk);
                 tmem_st16(tSb, pk);
@@ -471,7 +621,7 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
                 float mx = -INFINITY;
 #pragma unroll
                 for (int q = 0; q < 32; ++q) mx = fmax3(mx, __uint_as_float(va[q]), __uint_as_float(vb[q]));
-                const float m_new = mx * sc;
+                const float m_new = BITS == 8 ? fmaf(mx, sp, ev) : mx * sc;
                 const bool need = m_new > m_used;
                 if (__any_sync(0xFFFFFFFFu, need)) {
                     if (!first) {
@@ -493,7 +643,7 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
                         }
                     }
                 }
-                const unsigned long long sc2 = f2_pack(sc, sc), nm2 = f2_pack(-m_used, -m_used);
+                const unsigned long long sc2 = f2_pack(sp, sp), nm2 = f2_pack(BITS == 8 ? ev - m_used : -m_used, BITS == 8 ? ev - m_used : -m_used);
                 unsigned long long ls2 = f2_pack(0.f, 0.f);
                 softmax32(va, sc2, nm2, ls2, pk);
                 tmem_st16(tSb, pk);
@@ -503,7 +653,7 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
                 f2_unpack(ls2, l0, l1);
                 ls = l0 + l1;
             }
-            l += ls;
+            l = BITS == 8 ? fmaf(ls, p8_pow2(-(int)ev), l) : l + ls;
             tc_wait_st();
             tc_fence_before();
             __syncwarp();
@@ -625,7 +775,7 @@ __device__ __forceinline__ int owner(long long tick, long long total, int G) {  
     return b;
 }
 
-template <typename T, int D>
+template <typename T, int D, int BITS>
 __global__ void __launch_bounds__(NTHREADS, 1) page_attn_tc5_kernel(const __grid_constant__ PageAttn p, const __grid_constant__ Work w) {
     using C = Cfg<D>;
     extern __shared__ uint8_t smem_raw[];
@@ -700,9 +850,15 @@ __global__ void __launch_bounds__(NTHREADS, 1) page_attn_tc5_kernel(const __grid
         w.desc[b] = d;
     }
     const Cta cta{smem, base, bars, tmem, misc + 1, misc + 2, smem_u32(misc + 4)};
-    if (warp < 8) softmax_loop<T, D>(p, w, cta, u);
-    else if (warp < 8 + NPROD) producer_loop<T, D>(p, w, cta, u);
-    else mma_loop<D>(w, cta, u, warp - (8 + NPROD));
+    if (warp < 8) {
+        softmax_loop<T, D, BITS>(p, w, cta, u);
+    } else if (warp < 8 + NPROD) {
+        if (BITS == 8) producer8_loop<T, D>(p, w, cta, u);
+        else producer_loop<T, D>(p, w, cta, u);
+    }
+    else {
+        mma_loop<D>(w, cta, u, warp - (8 + NPROD));
+    }
     tc_fence_before();
     __syncthreads();
     xsv_dep_release();
@@ -752,21 +908,20 @@ __global__ void __launch_bounds__(256) page_attn_tc5_merge_kernel(const __grid_c
 }
 
 // ------------------------------------------------------------------ host side
-constexpr size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 size_t max_entries(int n_tokens, int n_seqs, int group) { return (size_t)((long long)n_tokens * group / 256) + n_seqs + 1; }
 
-template <typename T, int D> cudaError_t launch(const PageAttn& p, const Work& w, cudaStream_t st) {
+template <typename T, int D, int BITS> cudaError_t launch(const PageAttn& p, const Work& w, cudaStream_t st) {
     static XsvPerDeviceInt ready;
     const int dev = xsv_current_device();
     if (!ready.get(dev)) {
-        cudaError_t e = cudaFuncSetAttribute(page_attn_tc5_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<D>::SMEM);
+        cudaError_t e = cudaFuncSetAttribute(page_attn_tc5_kernel<T, D, BITS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<D>::SMEM);
         if (e != cudaSuccess) return e;
         ready.set(dev, 1);
     }
     cudaError_t e = xsv_launch_dep(page_list_kernel, dim3(1), dim3(1024), 0, st, p, w);
     if (e != cudaSuccess) return e;
     xsv_count_launch(1);
-    e = xsv_launch_dep(page_attn_tc5_kernel<T, D>, dim3(w.G), dim3(NTHREADS), Cfg<D>::SMEM, st, p, w);
+    e = xsv_launch_dep(page_attn_tc5_kernel<T, D, BITS>, dim3(w.G), dim3(NTHREADS), Cfg<D>::SMEM, st, p, w);
     if (e != cudaSuccess) return e;
     xsv_count_launch(1);
     e = xsv_launch_dep(page_attn_tc5_merge_kernel<T, D>, dim3(w.G, 16), dim3(256), 0, st, p, w);
@@ -781,7 +936,8 @@ size_t xsv_page_tc5_workspace(int n_tokens, int n_seqs, int group, int head_dim)
     return 256 + align256(G * sizeof(int4)) + align256((E + 1) * sizeof(long long)) + align256(E * sizeof(Entry)) + G * 2 * 256 * (head_dim + 2) * sizeof(float);
 }
 
-cudaError_t xsv_launch_page_tc5(const PageAttn& p, xsv_dtype dtype, int head_dim, void* workspace, cudaStream_t st) {
+namespace {
+template <int BITS> cudaError_t launch_any(const PageAttn& p, xsv_dtype dtype, int head_dim, void* workspace, cudaStream_t st) {
     Work w{};
     w.G = xsv_sm_count();
     const size_t E = max_entries(p.n_tokens, p.n_seqs, p.group);
@@ -792,6 +948,14 @@ cudaError_t xsv_launch_page_tc5(const PageAttn& p, xsv_dtype dtype, int head_dim
     w.pre = (long long*)at; at += align256((E + 1) * sizeof(long long));
     w.entry = (Entry*)at; at += align256(E * sizeof(Entry));
     w.part = (float*)at;
-    if (dtype == XSV_F16) return head_dim == 64 ? launch<__half, 64>(p, w, st) : launch<__half, 128>(p, w, st);
-    return head_dim == 64 ? launch<__nv_bfloat16, 64>(p, w, st) : launch<__nv_bfloat16, 128>(p, w, st);
+    if (dtype == XSV_F16) return head_dim == 64 ? launch<__half, 64, BITS>(p, w, st) : launch<__half, 128, BITS>(p, w, st);
+    return head_dim == 64 ? launch<__nv_bfloat16, 64, BITS>(p, w, st) : launch<__nv_bfloat16, 128, BITS>(p, w, st);
+}
+}  // namespace
+
+cudaError_t xsv_launch_page_tc5(const PageAttn& p, xsv_dtype dtype, int head_dim, void* workspace, cudaStream_t st) {
+    return launch_any<4>(p, dtype, head_dim, workspace, st);
+}
+cudaError_t xsv_launch_page8_tc5(const PageAttn& p, xsv_dtype dtype, int head_dim, void* workspace, cudaStream_t st) {
+    return launch_any<8>(p, dtype, head_dim, workspace, st);
 }

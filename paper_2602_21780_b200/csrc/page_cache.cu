@@ -41,19 +41,9 @@ template <typename T> __device__ __forceinline__ void unpack8(const uint4& w, fl
     o[0] = a.x; o[1] = a.y; o[2] = b.x; o[3] = b.y; o[4] = c.x; o[5] = c.y; o[6] = d.x; o[7] = d.y;
 }
 
-// Where new token t lands.  False for a token without a place, or with one that contradicts the lengths.
-struct Place { int seq, begin, end, page, off, pos; };
+using Place = PagePlace;
 __device__ __forceinline__ bool place_of(const Append& p, int t, Place& q) {
-    const int slot = p.slot[t];
-    q.seq = p.seq[t];
-    if (slot < 0 || q.seq < 0 || q.seq >= p.n_seqs || q.seq >= p.pool.max_seqs) return false;
-    q.begin = p.cu[q.seq];
-    q.end = p.cu[q.seq + 1];
-    q.page = slot / XSV_PAGE;
-    q.off = slot % XSV_PAGE;
-    if (q.begin < 0 || q.begin > t || q.end <= t || q.end > p.n_tokens || q.page >= p.pool.n_pages) return false;
-    q.pos = p.total[q.seq] - (q.end - t);
-    return q.pos >= q.off && q.pos - (t - q.begin) >= 0 && q.pos % XSV_PAGE == q.off;
+    return page_place(p.slot, p.seq, p.cu, p.total, p.n_tokens, min(p.n_seqs, p.pool.max_seqs), p.pool.n_pages, t, q);
 }
 
 // What codes are computed from: bf16 values beyond fp16 are brought to +-65504, fp16 ones have no such values.

@@ -106,3 +106,19 @@ template <> __device__ __forceinline__ uint32_t max2<__half>(uint32_t a, uint32_
 template <> __device__ __forceinline__ uint32_t min2<__nv_bfloat16>(uint32_t a, uint32_t b) { uint32_t d; asm("min.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b)); return d; }
 template <> __device__ __forceinline__ uint32_t max2<__nv_bfloat16>(uint32_t a, uint32_t b) { uint32_t d; asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b)); return d; }
 __device__ __forceinline__ float clamp_half(float x) { return fminf(fmaxf(x, -65504.f), 65504.f); }
+
+// Where new token t of an append lands.  False for a token without a place, or with one that contradicts the lengths.
+struct PagePlace { int seq, begin, end, page, off, pos; };
+__device__ __forceinline__ bool page_place(const int* slot_map, const int* token_seq, const int* cu, const int* total, int n_tokens, int n_seqs,
+                                           long long n_pages, int t, PagePlace& q) {
+    const int slot = slot_map[t];
+    q.seq = token_seq[t];
+    if (slot < 0 || q.seq < 0 || q.seq >= n_seqs) return false;
+    q.begin = cu[q.seq];
+    q.end = cu[q.seq + 1];
+    q.page = slot / XSV_PAGE;
+    q.off = slot % XSV_PAGE;
+    if (q.begin < 0 || q.begin > t || q.end <= t || q.end > n_tokens || q.page >= n_pages) return false;
+    q.pos = total[q.seq] - (q.end - t);
+    return q.pos >= q.off && q.pos - (t - q.begin) >= 0 && q.pos % XSV_PAGE == q.off;
+}

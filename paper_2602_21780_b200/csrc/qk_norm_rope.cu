@@ -11,7 +11,8 @@
 // tokens a token's heads are spread over several blocks (a row per lane group), which trades repeated sines for latency.
 //
 // Angles: position * inv_freq in turns as a float64 product, its fraction in float32: a float32 angle of a position
-// near 10^6 would be off by 0.03 rad.  Norms are float32, the layer norm's variance from differences to the mean (two
+// near 10^6 would be off by 0.03 rad.  With several positions a token (time, height, width) the thread that serves a frequency
+// looks up once which of them it turns by.  Norms are float32, the layer norm's variance from differences to the mean (two
 // passes over registers); results are rounded once, to the output type.
 // Measured: 8191 tokens, 32 + 8 + 8 heads of 128, fp16: 43.6 us, 4.6 TB/s; 1374 tokens, 3 x 16 heads of 64: 6.2 us; one token: 2.5 us.
 // What is left to the copy rate is loads in flight: 8 blocks of 4 warps with one or two rows each; four rows a lane group or fewer
@@ -35,8 +36,10 @@ struct NormRope {
     const void* b[2];
     const float* inv_freq;
     const int* pos;
+    const int* axes;         // the position that each frequency turns by, or null
     float eps;
     int n_tokens, n_rot;     // n_rot: channels rotated (0: none)
+    int n_pos;               // positions of a token
 };
 
 template <typename T> __device__ __forceinline__ void unpack4(const uint2& w, float* o) {
@@ -92,7 +95,11 @@ __global__ void __launch_bounds__(THREADS, 8) qk_norm_rope_kernel(const __grid_c
         const int per = ROPE == XSV_ROPE_2D ? n_freq / 2 : n_freq;
         coord = threadIdx.x / per;
         freq = (double)p.inv_freq[threadIdx.x - coord * per];
-        at = ROPE == XSV_ROPE_2D ? p.pos[2 * (size_t)blockIdx.x + coord] : p.pos[blockIdx.x];
+        if (ROPE != XSV_ROPE_2D && p.axes) {
+            coord = p.axes[threadIdx.x];
+            if (coord < 0 || coord >= p.n_pos) { coord = 0; freq = 0.0; }       // no such position: not rotated
+        }
+        at = p.pos[(size_t)blockIdx.x * p.n_pos + coord];
     }
     int buf = 0;
     for (int t = blockIdx.x; t < p.n_tokens; t += gridDim.x, buf ^= 1) {
@@ -105,7 +112,7 @@ __global__ void __launch_bounds__(THREADS, 8) qk_norm_rope_kernel(const __grid_c
                 sincospif(2.f * (float)turns, &s, &c);
                 cs[buf][threadIdx.x] = make_float2(c, s);
                 const int next = t + gridDim.x;
-                if (next < p.n_tokens) at = ROPE == XSV_ROPE_2D ? p.pos[2 * (size_t)next + coord] : p.pos[next];
+                if (next < p.n_tokens) at = p.pos[(size_t)next * p.n_pos + coord];
             }
             __syncthreads();                                // two buffers: the last token's are read before this one
 #pragma unroll
@@ -212,12 +219,11 @@ cudaError_t launch(const NormRope& p, int norm, int rope, cudaStream_t st) {
 }  // namespace
 
 
-extern "C" xsv_status xsv_qk_norm_rope(const void* q, const void* k, const void* v, long long q_stride, long long k_stride,
-                                       long long v_stride, int n_tokens, int q_heads, int kv_heads, int head_dim,
-                                       xsv_dtype dtype, xsv_norm norm, const void* q_weight, const void* q_bias,
-                                       const void* k_weight, const void* k_bias, float eps, xsv_rope rope, int rotary_dim,
-                                       const float* inv_freq, const int* positions, xsv_layout layout, void* q_out,
-                                       void* k_out, void* v_out, void* stream) {
+static xsv_status norm_rope(const void* q, const void* k, const void* v, long long q_stride, long long k_stride, long long v_stride, int n_tokens,
+                            int q_heads, int kv_heads, int head_dim, xsv_dtype dtype, xsv_norm norm, const void* q_weight, const void* q_bias,
+                            const void* k_weight, const void* k_bias, float eps, xsv_rope rope, int rotary_dim, const float* inv_freq,
+                            const int* positions, const int* axes, int n_axes, xsv_layout layout, void* q_out, void* k_out, void* v_out,
+                            void* stream) {
     if (n_tokens < 0 || q_heads < 0 || kv_heads < 0 || q_heads > 1 << 16 || kv_heads > 1 << 16) return XSV_ERR_ARG;
     if (head_dim != 64 && head_dim != 128) return XSV_ERR_ARG;
     if (dtype != XSV_F16 && dtype != XSV_BF16) return XSV_ERR_ARG;
@@ -250,7 +256,8 @@ extern "C" xsv_status xsv_qk_norm_rope(const void* q, const void* k, const void*
     if (norm != XSV_NORM_NONE) bits |= (uintptr_t)q_weight | (uintptr_t)q_bias | (uintptr_t)k_weight | (uintptr_t)k_bias;
     if (bits & 15) return XSV_ERR_SHAPE;
     p.w[0] = q_weight; p.w[1] = k_weight; p.b[0] = q_bias; p.b[1] = k_bias;
-    p.inv_freq = inv_freq; p.pos = positions; p.eps = eps; p.n_tokens = n_tokens;
+    p.inv_freq = inv_freq; p.pos = positions; p.axes = axes; p.eps = eps; p.n_tokens = n_tokens;
+    p.n_pos = axes ? n_axes : rope == XSV_ROPE_2D ? 2 : 1;
     p.n_rot = rope == XSV_ROPE_NONE ? 0 : rotary_dim;
     cudaStream_t st = (cudaStream_t)stream;
     cudaError_t e;
@@ -259,4 +266,26 @@ extern "C" xsv_status xsv_qk_norm_rope(const void* q, const void* k, const void*
     if (e != cudaSuccess) return xsv_cuda_status(e);
     xsv_count_launch(1);
     return XSV_OK;
+}
+
+extern "C" xsv_status xsv_qk_norm_rope(const void* q, const void* k, const void* v, long long q_stride, long long k_stride,
+                                       long long v_stride, int n_tokens, int q_heads, int kv_heads, int head_dim,
+                                       xsv_dtype dtype, xsv_norm norm, const void* q_weight, const void* q_bias,
+                                       const void* k_weight, const void* k_bias, float eps, xsv_rope rope, int rotary_dim,
+                                       const float* inv_freq, const int* positions, xsv_layout layout, void* q_out,
+                                       void* k_out, void* v_out, void* stream) {
+    return norm_rope(q, k, v, q_stride, k_stride, v_stride, n_tokens, q_heads, kv_heads, head_dim, dtype, norm, q_weight, q_bias, k_weight, k_bias, eps, rope,
+                     rotary_dim, inv_freq, positions, nullptr, 0, layout, q_out, k_out, v_out, stream);
+}
+
+extern "C" xsv_status xsv_qk_norm_rope_axes(const void* q, const void* k, const void* v, long long q_stride, long long k_stride, long long v_stride,
+                                            int n_tokens, int q_heads, int kv_heads, int head_dim, xsv_dtype dtype, xsv_norm norm,
+                                            const void* q_weight, const void* q_bias, const void* k_weight, const void* k_bias, float eps,
+                                            xsv_rope rope, int rotary_dim, const float* inv_freq, const int* positions, const int* axes, int n_axes,
+                                            xsv_layout layout, void* q_out, void* k_out, void* v_out, void* stream) {
+    if ((rope != XSV_ROPE_HALF && rope != XSV_ROPE_PAIRS) || n_axes <= 0 || n_axes > XSV_ROPE_MAX_AXES) return XSV_ERR_ARG;
+    if (n_tokens > 0 && !axes) return XSV_ERR_ARG;
+    if ((uintptr_t)axes & 3) return XSV_ERR_SHAPE;
+    return norm_rope(q, k, v, q_stride, k_stride, v_stride, n_tokens, q_heads, kv_heads, head_dim, dtype, norm, q_weight, q_bias, k_weight, k_bias, eps, rope,
+                     rotary_dim, inv_freq, positions, axes, n_axes, layout, q_out, k_out, v_out, stream);
 }
