@@ -540,10 +540,10 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page8_attn_kern
     }
 }
 
-// Units that several warps share.  A block looks at 8 workers' descriptions and merges 16 channels of the units that
-// begin to be shared there: its 8 warps take the parts in turn, each lane 4 values (2 rows x 2 channels) of its parts,
-// and are merged in the order of the warps.
-constexpr int MERGE_WARPS = 8;
+// Units that several warps share.  A block of 8 warps looks at the descriptions of 16 workers and merges 16 channels of the units that
+// begin to be shared there: as many warps a unit as there are for it, which take its parts in turn and are merged in their order; a lane has
+// 4 values (2 rows x 2 channels).  (The whole block for one unit after the other: 15 us instead of 5 where most units have two parts.)
+constexpr int MERGE_UNITS = 16, MERGE_WARPS = 8;
 template <typename T, int D, int NT, bool SEL>
 __global__ void __launch_bounds__(MERGE_WARPS * 32) page8_attn_merge_kernel(const __grid_constant__ Attn8 p, int workers) {
     constexpr int ROWS = 8 * NT, CT = D / 16, PF = Part<D, NT>::FLOATS;
@@ -562,39 +562,53 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) page8_attn_merge_kernel(cons
             ml = make_float4(m0, ml.y * a0 + y.y * b0, m1, ml.w * a1 + y.w * b1);
         }
     };
-    const int w0 = blockIdx.x * 8;
+    const int w0 = blockIdx.x * MERGE_UNITS;
     int4 mine = make_int4(0, 0, 0, 0);
-    if (lane < 8 && w0 + lane < workers) mine = p.desc[w0 + lane];
-    for (uint32_t todo = __ballot_sync(0xFFFFFFFFu, mine.w > 0); todo; todo &= todo - 1) {     // the same for the whole block
-        const int from = __ffs(todo) - 1, w = w0 + from;
-        const int4 d = make_int4(__shfl_sync(0xFFFFFFFFu, mine.x, from), __shfl_sync(0xFFFFFFFFu, mine.y, from),
-                                 __shfl_sync(0xFFFFFFFFu, mine.z, from), __shfl_sync(0xFFFFFFFFu, mine.w, from));
-        Acc acc;
+    if (lane < MERGE_UNITS && w0 + lane < workers) mine = p.desc[w0 + lane];
+    auto unit = [&](int from) { return make_int4(__shfl_sync(0xFFFFFFFFu, mine.x, from), __shfl_sync(0xFFFFFFFFu, mine.y, from), __shfl_sync(0xFFFFFFFFu, mine.z, from), __shfl_sync(0xFFFFFFFFu, mine.w, from)); };
+    auto sum = [&](Acc& acc, int w, int parts, int i0, int step) {
 #pragma unroll 4
-        for (int i = wid; i < d.w; i += MERGE_WARPS) {
+        for (int i = i0; i < parts; i += step) {
             const float* part = p.part + (size_t)(i == 0 ? 2 * (w - 1) + 1 : 2 * (w + i - 1)) * PF;
             acc.add(reinterpret_cast<const float4*>(part)[(n * CT + ct) * 32 + lane], *reinterpret_cast<const float4*>(part + NT * CT * 128 + 2 * r0));
         }
+    };
+    auto write = [&](const Acc& acc, const int4& d) {
         const Unit8 q = unit_of<SEL>(p, d.x, ROWS);
         const int n_rows = q.new_ * p.group, t0 = first_token<SEL>(p, d.x);
-        const bool write = !SEL || q.total > 0 || (p.seq[d.x] >= 0 && p.seq[d.x] < p.n_seqs);
-        __syncthreads();                                        // the last unit's reads of the shared arrays
-        s_o[wid][lane] = acc.o;
-        s_ml[wid][lane] = acc.ml;
-        __syncthreads();
-        if (wid != 0) continue;
-#pragma unroll
-        for (int i = 1; i < MERGE_WARPS; ++i) acc.add(s_o[i][lane], s_ml[i][lane]);
+        if (SEL && q.total == 0 && !(p.seq[d.x] >= 0 && p.seq[d.x] < p.n_seqs)) return;
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const int r = d.z * ROWS + r0 + c;
-            if (r >= n_rows || !write) continue;
+            if (r >= n_rows) continue;
             int i, h;
             page_row(p, r, i, h);
             const float l = c ? acc.ml.w : acc.ml.y, inv = l == 0.f ? 0.f : 1.f / l;
             T* dst = (T*)p.out + ((size_t)(t0 + i) * p.q_heads + d.y * p.group + h) * D + (D / 8) * g + 2 * ct;
             *reinterpret_cast<uint32_t*>(dst) = page_result2<T>((c ? acc.o.y : acc.o.x) * inv, (c ? acc.o.w : acc.o.z) * inv);
         }
+    };
+    const uint32_t todo = __ballot_sync(0xFFFFFFFFu, mine.w > 0);                // the same for the whole block
+    const int units = __popc(todo), per = units <= 1 ? 8 : units == 2 ? 4 : units <= 4 ? 2 : 1;      // warps of a unit
+    for (int at = wid / per; at < (per == 1 ? units : MERGE_WARPS / per); at += MERGE_WARPS / per) {
+        Acc acc;
+        int from = 0;
+        int4 d = make_int4(0, 0, 0, 0);
+        if (at < units) {
+            uint32_t rest = todo;
+            for (int i = 0; i < at; ++i) rest &= rest - 1;
+            from = __ffs(rest) - 1;
+            d = unit(from);
+            sum(acc, w0 + from, d.w, wid % per, per);
+        }
+        if (per > 1) {                                          // once: every warp has one unit or none
+            s_o[wid][lane] = acc.o;
+            s_ml[wid][lane] = acc.ml;
+            __syncthreads();
+            if (at >= units || wid % per != 0) return;
+            for (int i = 1; i < per; ++i) acc.add(s_o[wid + i][lane], s_ml[wid + i][lane]);
+        }
+        write(acc, d);
     }
 }
 
@@ -632,7 +646,7 @@ template <typename T, int D, int NT, bool SEL> cudaError_t launch(Attn8& p, cuda
     cudaError_t e = xsv_launch_dep(kernel, dim3(grid), dim3(THREADS), smem, st, p);
     if (e != cudaSuccess) return e;
     xsv_count_launch(1);
-    e = xsv_launch_dep(page8_attn_merge_kernel<T, D, NT, SEL>, dim3((workers + 7) / 8, NT * (D / 16)), dim3(MERGE_WARPS * 32), 0, st, p, workers);
+    e = xsv_launch_dep(page8_attn_merge_kernel<T, D, NT, SEL>, dim3((workers + MERGE_UNITS - 1) / MERGE_UNITS, NT * (D / 16)), dim3(MERGE_WARPS * 32), 0, st, p, workers);
     if (e == cudaSuccess) xsv_count_launch(1);
     return e;
 }

@@ -8,11 +8,16 @@
 // in steps of 2^-9: 24 bits, so that no order of summation matters), for the mean key that a selection scores.
 // Bound by HBM: 2 bytes read and 1 written per element.
 //
-// xsv_page8_read: a thread decodes 16 channels of one token.
+// xsv_page8_read: a thread looks one token up and decodes 8 channels of it, of up to 4 heads.
+#include <type_traits>
+
 #include "../../include/xsv.h"
 #include "page8_layout.cuh"
 #include "xsv_kernels.h"
 
+#ifndef AP_FEW
+#define AP_FEW 4LL
+#endif
 namespace {
 
 struct Append8 {
@@ -24,39 +29,62 @@ struct Append8 {
     const int* seq;
     const int* cu;
     const int* total;
-    int n_tokens, n_seqs;
+    int n_tokens, n_seqs, across;      // across: heads of a block
 };
 __device__ __forceinline__ bool place_of(const Append8& p, int t, PagePlace& q) {
     return page_place(p.slot, p.seq, p.cu, p.total, p.n_tokens, p.n_seqs, p.pool.n_pages, t, q);
 }
 
-// Pairs of inputs brought to +-65504 (bf16: +-65536, whose code is the same); a NaN becomes the bound.
-template <typename T> __device__ __forceinline__ uint32_t bounded2(uint32_t w);
-template <> __device__ __forceinline__ uint32_t bounded2<__half>(uint32_t w) { return max2<__half>(min2<__half>(w, 0x7BFF7BFFu), 0xFBFFFBFFu); }
-template <> __device__ __forceinline__ uint32_t bounded2<__nv_bfloat16>(uint32_t w) { return max2<__nv_bfloat16>(min2<__nv_bfloat16>(w, 0x47804780u), 0xC780C780u); }
-
-// 16 channels of a row, and the larger of the magnitudes so far (as bit patterns, two a word: positive 16-bit floats compare
+// Inputs count as at most 65504 in magnitude (bf16: 65536, whose code is the same).  Where a magnitude, as bits, is beyond BOUND,
+// infinities and NaN among them, pairs are brought to it; a NaN becomes the bound.
+template <typename T> constexpr uint32_t BOUND = 0x7BFFu;
+template <> constexpr uint32_t BOUND<__nv_bfloat16> = 0x4780u;
+template <typename T> __device__ __forceinline__ uint32_t bounded2(uint32_t w) {
+    constexpr uint32_t HI = BOUND<T> * 0x10001u, LO = HI | 0x80008000u;
+    return max2<T>(min2<T>(w, HI), LO);
+}
+template <typename T> __device__ __forceinline__ uint4 bounded8(const uint4& r) { return make_uint4(bounded2<T>(r.x), bounded2<T>(r.y), bounded2<T>(r.z), bounded2<T>(r.w)); }
+// 8 channels of a row, and the larger of the magnitudes so far (as bit patterns, two a word: positive 16-bit floats compare
 // like whole numbers).
-struct Row16 { uint4 a, b; };
-template <typename T> __device__ __forceinline__ Row16 load16(const void* x) {
-    const uint4* p = reinterpret_cast<const uint4*>(x);
-    Row16 r{p[0], p[1]};
-    r.a = make_uint4(bounded2<T>(r.a.x), bounded2<T>(r.a.y), bounded2<T>(r.a.z), bounded2<T>(r.a.w));
-    r.b = make_uint4(bounded2<T>(r.b.x), bounded2<T>(r.b.y), bounded2<T>(r.b.z), bounded2<T>(r.b.w));
-    return r;
-}
-__device__ __forceinline__ uint32_t mag16(const Row16& r, uint32_t m) {
+__device__ __forceinline__ uint4 load8(const void* x) { return *reinterpret_cast<const uint4*>(x); }
+__device__ __forceinline__ uint32_t mag8(const uint4& r, uint32_t m) {
     constexpr uint32_t ABS = 0x7FFF7FFFu;
-    m = __vmaxu2(m, __vmaxu2(__vmaxu2(r.a.x & ABS, r.a.y & ABS), __vmaxu2(r.a.z & ABS, r.a.w & ABS)));
-    return __vmaxu2(m, __vmaxu2(__vmaxu2(r.b.x & ABS, r.b.y & ABS), __vmaxu2(r.b.z & ABS, r.b.w & ABS)));
+    return __vmaxu2(m, __vmaxu2(__vmaxu2(r.x & ABS, r.y & ABS), __vmaxu2(r.z & ABS, r.w & ABS)));
 }
-template <typename T> __device__ __forceinline__ float mag_value(uint32_t m) { return xsv_unpack2<T>(max(m & 0xFFFFu, m >> 16)).x; }
-template <typename T> __device__ __forceinline__ uint32_t codes4(uint32_t w0, uint32_t w1, float inv) {
-    const float2 a = xsv_unpack2<T>(w0), b = xsv_unpack2<T>(w1);
-    return p8_codes2(a.x * inv, a.y * inv) | p8_codes2(b.x * inv, b.y * inv) << 16;
-}
-template <typename T> __device__ __forceinline__ uint4 codes16(const Row16& r, float inv) {
-    return make_uint4(codes4<T>(r.a.x, r.a.y, inv), codes4<T>(r.a.z, r.a.w, inv), codes4<T>(r.b.x, r.b.y, inv), codes4<T>(r.b.z, r.b.w, inv));
+__device__ __forceinline__ uint32_t warp_mag(uint32_t m) { return __reduce_max_sync(0xFFFFFFFFu, max(m & 0xFFFFu, m >> 16)); }
+template <typename T> __device__ __forceinline__ int exponent_of_mag(uint32_t m) { return p8_exponent(xsv_unpack2<T>(min(m, BOUND<T>)).x); }
+
+// Codes of 8 channels for the scale 2^e.  x / 2^e is taken in the inputs' own type: exact, or so small that its code is 0.  fp16
+// does not hold 2^-e for e below -14: by way of float32 then.
+template <typename T> struct Quant;
+template <> struct Quant<__nv_bfloat16> {
+    uint32_t inv;
+    __device__ __forceinline__ explicit Quant(int e) : inv((uint32_t)(127 - e) << 7) { inv |= inv << 16; }
+    __device__ __forceinline__ uint32_t two(uint32_t w) const {
+        uint32_t y;
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(w), "r"(inv));
+        const float2 f = xsv_unpack2<__nv_bfloat16>(y);
+        return p8_codes2(f.x, f.y);
+    }
+};
+template <> struct Quant<__half> {
+    uint32_t inv;
+    float wide;                                                // 0: inv holds it
+    __device__ __forceinline__ explicit Quant(int e) : inv((uint32_t)(15 - max(e, -14)) << 10), wide(e < -14 ? p8_pow2(-e) : 0.f) { inv |= inv << 16; }
+    __device__ __forceinline__ uint32_t two(uint32_t w) const {
+        if (wide != 0.f) {                                     // the same for the whole warp
+            const float2 f = xsv_unpack2<__half>(w);
+            return p8_codes2(f.x * wide, f.y * wide);
+        }
+        uint32_t y;
+        unsigned short r;
+        asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(y) : "r"(w), "r"(inv));
+        asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(y));
+        return r;
+    }
+};
+template <typename T> __device__ __forceinline__ uint2 codes8(const uint4& r, const Quant<T>& q) {
+    return make_uint2(__byte_perm(q.two(r.x), q.two(r.y), 0x5410), __byte_perm(q.two(r.z), q.two(r.w), 0x5410));
 }
 // four codes at another scale
 __device__ __forceinline__ uint32_t rescale4(uint32_t w, float f) {
@@ -65,7 +93,7 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t w, float f) {
     const float2 a = xsv_unpack2<__half>(lo), b = xsv_unpack2<__half>(hi);
     return p8_codes2(a.x * f, a.y * f) | p8_codes2(b.x * f, b.y * f) << 16;
 }
-__device__ __forceinline__ uint4 rescale16(const uint4& w, float f) { return make_uint4(rescale4(w.x, f), rescale4(w.y, f), rescale4(w.z, f), rescale4(w.w, f)); }
+__device__ __forceinline__ uint2 rescale8(const uint2& w, float f) { return make_uint2(rescale4(w.x, f), rescale4(w.y, f)); }
 __device__ __forceinline__ void add4(uint32_t w, float* s) {
     uint32_t lo, hi;
     p8_halves(w, lo, hi);
@@ -73,22 +101,13 @@ __device__ __forceinline__ void add4(uint32_t w, float* s) {
     s[0] += a.x; s[1] += a.y; s[2] += b.x; s[3] += b.y;
 }
 
-// Where 16 channels (from 16 piece on) of a token stand.
-template <int D> __device__ __forceinline__ int k_at(int tok, int piece) { return (((tok >> 3) * (D / 64) + (piece >> 2)) * 32 + (tok & 7) * 4 + (piece & 3)) * 16; }
-template <int D> __device__ __forceinline__ int v_index(int tok) { return ((tok >> 4) * 4 + (tok >> 3 & 1) * 2 + (tok & 1)) * 32 + (tok >> 1 & 3); }
-template <int D> __device__ __forceinline__ uint4 v_load(const uint8_t* rec, int tok, int piece) {
-    if (D == 128) return *reinterpret_cast<const uint4*>(rec + Page8Rec<D>::V_CODES + (v_index<D>(tok) + 4 * piece) * 16);
-    const uint2 x = *reinterpret_cast<const uint2*>(rec + Page8Rec<D>::V_CODES + (v_index<D>(tok) + 8 * piece) * 8);
-    const uint2 y = *reinterpret_cast<const uint2*>(rec + Page8Rec<D>::V_CODES + (v_index<D>(tok) + 8 * piece + 4) * 8);
-    return make_uint4(x.x, x.y, y.x, y.y);
+// Where 8 channels (from 8 piece on) of a token stand.
+template <int D> __device__ __forceinline__ uint2* k_at(uint8_t* rec, int tok, int piece) {
+    return reinterpret_cast<uint2*>(rec + Page8Rec<D>::K_CODES + (((tok >> 3) * (D / 64) + (piece >> 3)) * 32 + (tok & 7) * 4 + (piece >> 1 & 3)) * 16) + (piece & 1);
 }
-template <int D> __device__ __forceinline__ void v_store(uint8_t* rec, int tok, int piece, const uint4& c) {
-    if (D == 128) {
-        *reinterpret_cast<uint4*>(rec + Page8Rec<D>::V_CODES + (v_index<D>(tok) + 4 * piece) * 16) = c;
-    } else {
-        *reinterpret_cast<uint2*>(rec + Page8Rec<D>::V_CODES + (v_index<D>(tok) + 8 * piece) * 8) = make_uint2(c.x, c.y);
-        *reinterpret_cast<uint2*>(rec + Page8Rec<D>::V_CODES + (v_index<D>(tok) + 8 * piece + 4) * 8) = make_uint2(c.z, c.w);
-    }
+template <int D> __device__ __forceinline__ uint2* v_at(uint8_t* rec, int tok, int piece) {
+    const int i = ((tok >> 4) * 4 + (tok >> 3 & 1) * 2 + (tok & 1)) * 32 + (tok >> 1 & 3);
+    return reinterpret_cast<uint2*>(rec + Page8Rec<D>::V_CODES) + (D == 128 ? 2 * (i + 4 * (piece >> 1)) + (piece & 1) : i + 4 * piece);
 }
 
 // The mean key from a warp's sums of the page's key codes, channels (D / 32) lane on.
@@ -112,7 +131,7 @@ constexpr int WARPS = 4, THREADS = WARPS * 32;
 template <typename T, int D>
 __global__ void __launch_bounds__(THREADS) page8_append_few_kernel(const __grid_constant__ Append8 p) {
     using R = Page8Rec<D>;
-    constexpr int PIECES = D / 16, ROWS = 32 / PIECES;        // rows of a turn
+    constexpr int PIECES = D / 8, ROWS = 32 / PIECES;         // rows of a turn
     xsv_dep_release();
     xsv_dep_sync();
     const int lane = threadIdx.x & 31, across = (p.pool.heads + WARPS - 1) / WARPS;
@@ -121,50 +140,54 @@ __global__ void __launch_bounds__(THREADS) page8_append_few_kernel(const __grid_
     if (head >= p.pool.heads || !place_of(p, t, q) || !(t == q.begin || q.off == 0)) return;
     const int run = min(XSV_PAGE - q.off, q.end - t), r_lane = lane / PIECES, piece = lane % PIECES;
     uint8_t* rec = page8_rec<D>(p.pool, q.page, head);
-    const T* K = (const T*)p.K + (size_t)t * p.k_stride + (size_t)head * D + 16 * piece;
-    const T* V = (const T*)p.V + (size_t)t * p.v_stride + (size_t)head * D + 16 * piece;
+    const T* K = (const T*)p.K + (size_t)t * p.k_stride + (size_t)head * D + 8 * piece;
+    const T* V = (const T*)p.V + (size_t)t * p.v_stride + (size_t)head * D + 8 * piece;
     float2* const params = reinterpret_cast<float2*>(rec + R::PARAMS);
     const float2 was = q.off > 0 ? *params : make_float2(0.f, 0.f);
     // the first turn's rows stay, further ones are read again
-    Row16 k{}, v{};
+    uint4 k = make_uint4(0u, 0u, 0u, 0u), v = k;
     if (r_lane < run) {
-        k = load16<T>(K + (size_t)r_lane * p.k_stride);
-        v = load16<T>(V + (size_t)r_lane * p.v_stride);
+        k = load8(K + (size_t)r_lane * p.k_stride);
+        v = load8(V + (size_t)r_lane * p.v_stride);
     }
-    uint32_t mk = mag16(k, 0u), mv = mag16(v, 0u);
+    uint32_t mk = mag8(k, 0u), mv = mag8(v, 0u);
     for (int r = ROWS + r_lane; r < run; r += ROWS) {
-        mk = mag16(load16<T>(K + (size_t)r * p.k_stride), mk);
-        mv = mag16(load16<T>(V + (size_t)r * p.v_stride), mv);
+        mk = mag8(load8(K + (size_t)r * p.k_stride), mk);
+        mv = mag8(load8(V + (size_t)r * p.v_stride), mv);
     }
-    mk = __reduce_max_sync(0xFFFFFFFFu, max(mk & 0xFFFFu, mk >> 16));
-    mv = __reduce_max_sync(0xFFFFFFFFu, max(mv & 0xFFFFu, mv >> 16));
-    int ek = p8_exponent(mag_value<T>(mk)), ev = p8_exponent(mag_value<T>(mv));
+    mk = warp_mag(mk);
+    mv = warp_mag(mv);
+    int ek = exponent_of_mag<T>(mk), ev = exponent_of_mag<T>(mv);
     if (q.off > 0) {
         const int ok = p8_exponent_of(was.x), ov = p8_exponent_of(was.y);
         if (ek > ok) {                                         // a larger scale: what stands there moves to it
-            for (int i = lane; i < (q.off + 7) / 8 * (D / 64) * 32; i += 32) {
-                uint4* c = reinterpret_cast<uint4*>(rec + R::K_CODES) + i;
-                *c = rescale16(*c, p8_pow2(max(ok - ek, -126)));
+            for (int i = lane; i < (q.off + 7) / 8 * D; i += 32) {
+                uint2* c = reinterpret_cast<uint2*>(rec + R::K_CODES) + i;
+                *c = rescale8(*c, p8_pow2(max(ok - ek, -126)));
             }
         }
         if (ev > ov) {
-            for (int i = lane; i < (q.off + 15) / 16 * D; i += 32) {
-                uint4* c = reinterpret_cast<uint4*>(rec + R::V_CODES) + i;
-                *c = rescale16(*c, p8_pow2(max(ov - ev, -126)));
+            for (int i = lane; i < (q.off + 15) / 16 * 2 * D; i += 32) {
+                uint2* c = reinterpret_cast<uint2*>(rec + R::V_CODES) + i;
+                *c = rescale8(*c, p8_pow2(max(ov - ev, -126)));
             }
         }
         ek = max(ek, ok);
         ev = max(ev, ov);
         __syncwarp();                                          // (they touch places that new rows go to)
     }
-    const float ik = p8_pow2(-ek), iv = p8_pow2(-ev);
+    const Quant<T> qk(ek), qv(ev);
     for (int r = r_lane; r < run; r += ROWS) {
         if (r >= ROWS) {
-            k = load16<T>(K + (size_t)r * p.k_stride);
-            v = load16<T>(V + (size_t)r * p.v_stride);
+            k = load8(K + (size_t)r * p.k_stride);
+            v = load8(V + (size_t)r * p.v_stride);
         }
-        *reinterpret_cast<uint4*>(rec + R::K_CODES + k_at<D>(q.off + r, piece)) = codes16<T>(k, ik);
-        v_store<D>(rec, q.off + r, piece, codes16<T>(v, iv));
+        if (max(mk, mv) > BOUND<T>) {
+            k = bounded8<T>(k);
+            v = bounded8<T>(v);
+        }
+        *k_at<D>(rec, q.off + r, piece) = codes8(k, qk);
+        *v_at<D>(rec, q.off + r, piece) = codes8(v, qv);
     }
     if (lane == 0) *params = make_float2(p8_pow2(ek), p8_pow2(ev));
     if (q.off + run < XSV_PAGE) return;
@@ -173,10 +196,10 @@ __global__ void __launch_bounds__(THREADS) page8_append_few_kernel(const __grid_
 #pragma unroll 16
     for (int tok = 0; tok < XSV_PAGE; ++tok) {
         if (D == 128) {
-            add4(*reinterpret_cast<const uint32_t*>(rec + k_at<D>(tok, lane >> 2) + 4 * (lane & 3)), s);
+            add4(*(reinterpret_cast<const uint32_t*>(k_at<D>(rec, tok, lane >> 1)) + (lane & 1)), s);
         } else {
             uint32_t lo, hi;
-            p8_halves(*reinterpret_cast<const unsigned short*>(rec + k_at<D>(tok, lane >> 3) + 2 * (lane & 7)), lo, hi);
+            p8_halves(*(reinterpret_cast<const unsigned short*>(k_at<D>(rec, tok, lane >> 2)) + (lane & 3)), lo, hi);
             const float2 a = xsv_unpack2<__half>(lo);
             s[0] += a.x; s[1] += a.y;
         }
@@ -184,103 +207,119 @@ __global__ void __launch_bounds__(THREADS) page8_append_few_kernel(const __grid_
     store_mean<D>(rec, s, p8_pow2(ek), lane);
 }
 
-// ---- prompts: a block per (page, head), pages found among 32 new tokens
+// ---- prompts: a block looks for the first new tokens of pages among CHUNK ones and stores the keys, or the values, of p.across heads of
+// each page, one after the other
 constexpr int CHUNK = 32;
 
-template <typename T, int D>
-__global__ void __launch_bounds__(THREADS, 4) page8_append_kernel(const __grid_constant__ Append8 p) {
+template <typename T, int D, bool KEYS>
+__device__ __forceinline__ void append_pages(const Append8& p, int t_block, int head0, uint32_t (*s_mag)[WARPS], float (*s_sum)[D]) {
     using R = Page8Rec<D>;
-    constexpr int PIECES = D / 16, ROWS = THREADS / PIECES, TURNS = XSV_PAGE / ROWS;
-    __shared__ uint32_t s_mag[2][2][WARPS];
-    __shared__ __align__(16) float s_sum[WARPS][D];
-    xsv_dep_release();
-    xsv_dep_sync();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, piece = tid % PIECES, r0 = tid / PIECES;
-    const int head = blockIdx.x % p.pool.heads, t_block = blockIdx.x / p.pool.heads * CHUNK;
+    constexpr int PIECES = D / 8, ROWS = THREADS / PIECES, TURNS = XSV_PAGE / ROWS;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, piece = tid % PIECES;
+    // Row of a turn: a warp's rows are every other token, those that share sectors of the value codes.
+    const int r0 = D == 128 ? 4 * (warp >> 1) + (warp & 1) + 2 * (lane >> 4) : 8 * (warp >> 1) + (warp & 1) + 2 * (lane >> 3);
+    const int heads = min(p.across, p.pool.heads - head0);
     PagePlace mine{};
     const bool first = t_block + lane < p.n_tokens && place_of(p, t_block + lane, mine) && (t_block + lane == mine.begin || mine.off == 0);
     int buf = 0;
-    for (uint32_t todo = __ballot_sync(0xFFFFFFFFu, first); todo; todo &= todo - 1, buf ^= 1) {      // the same for every warp
+    for (uint32_t todo = __ballot_sync(0xFFFFFFFFu, first); todo; todo &= todo - 1) {      // the same for every warp
         const int from = __ffs(todo) - 1, t = t_block + from;
         const int off = __shfl_sync(0xFFFFFFFFu, mine.off, from), page = __shfl_sync(0xFFFFFFFFu, mine.page, from);
         const int run = min(XSV_PAGE - off, __shfl_sync(0xFFFFFFFFu, mine.end, from) - t);
-        uint8_t* rec = page8_rec<D>(p.pool, page, head);
-        const T* K = (const T*)p.K + (long long)(t - off) * p.k_stride + (size_t)head * D + 16 * piece;
-        const T* V = (const T*)p.V + (long long)(t - off) * p.v_stride + (size_t)head * D + 16 * piece;
-        float2* const params = reinterpret_cast<float2*>(rec + R::PARAMS);
-        const float2 was = off > 0 ? *params : make_float2(0.f, 0.f);
-        Row16 k[TURNS] = {}, v[TURNS] = {};
-#pragma unroll
-        for (int i = 0; i < TURNS; ++i) {
-            const int r = i * ROWS + r0;
-            if (r >= off && r < off + run) {
-                k[i] = load16<T>(K + (long long)r * p.k_stride);
-                v[i] = load16<T>(V + (long long)r * p.v_stride);
-            }
-        }
-        uint32_t mk = 0u, mv = 0u;
-#pragma unroll
-        for (int i = 0; i < TURNS; ++i) { mk = mag16(k[i], mk); mv = mag16(v[i], mv); }
-        mk = __reduce_max_sync(0xFFFFFFFFu, max(mk & 0xFFFFu, mk >> 16));
-        mv = __reduce_max_sync(0xFFFFFFFFu, max(mv & 0xFFFFu, mv >> 16));
-        if (lane == 0) { s_mag[buf][0][warp] = mk; s_mag[buf][1][warp] = mv; }
-        __syncthreads();
-        mk = max(max(s_mag[buf][0][0], s_mag[buf][0][1]), max(s_mag[buf][0][2], s_mag[buf][0][3]));
-        mv = max(max(s_mag[buf][1][0], s_mag[buf][1][1]), max(s_mag[buf][1][2], s_mag[buf][1][3]));
-        int ek = p8_exponent(mag_value<T>(mk)), ev = p8_exponent(mag_value<T>(mv));
-        float fk = 1.f, fv = 1.f;                              // from the old scale to the new one
-        if (off > 0) {
-            const int ok = p8_exponent_of(was.x), ov = p8_exponent_of(was.y);
-            fk = p8_pow2(max(min(ok - ek, 0), -126));
-            fv = p8_pow2(max(min(ov - ev, 0), -126));
-            ek = max(ek, ok);
-            ev = max(ev, ov);
-        }
-        const float ik = p8_pow2(-ek), iv = p8_pow2(-ev);
         const bool full = off + run == XSV_PAGE;
-        float s[16] = {};
+        const long long stride = KEYS ? p.k_stride : p.v_stride;
+        const T* x = (const T*)(KEYS ? p.K : p.V) + (long long)(t - off) * stride + (size_t)head0 * D + 8 * piece;
+        uint8_t* rec = page8_rec<D>(p.pool, page, head0);
+        // the heads, for a page that the call fills from its first row to its last (nothing else to ask about) and for others
+        auto store = [&](auto whole_c) {
+            constexpr bool WHOLE = decltype(whole_c)::value;
+#pragma unroll 1
+            for (int h = 0; h < heads; ++h, buf ^= 1, x += D, rec += R::BYTES) {
+                float* const scale = reinterpret_cast<float*>(rec + R::PARAMS) + (KEYS ? 0 : 1);
+                float was = 0.f;                               // of the tokens that stand in the page
+                if (!WHOLE && off > 0) was = *scale;
+                uint4 row[TURNS];
+                uint32_t mag = 0u;
 #pragma unroll
-        for (int i = 0; i < TURNS; ++i) {
-            const int r = i * ROWS + r0;
-            if (r >= off + run) continue;
-            uint8_t* const k_to = rec + R::K_CODES + k_at<D>(r, piece);
-            uint4 c;
-            if (r >= off) {
-                c = codes16<T>(k[i], ik);
-                *reinterpret_cast<uint4*>(k_to) = c;
-                v_store<D>(rec, r, piece, codes16<T>(v[i], iv));
-            } else {
-                c = make_uint4(0u, 0u, 0u, 0u);
-                if (full || fk != 1.f) c = *reinterpret_cast<const uint4*>(k_to);
-                if (fk != 1.f) {
-                    c = rescale16(c, fk);
-                    *reinterpret_cast<uint4*>(k_to) = c;
+                for (int i = 0; i < TURNS; ++i) {
+                    const int r = i * ROWS + r0;
+                    if (!WHOLE) row[i] = make_uint4(0u, 0u, 0u, 0u);
+                    if (WHOLE || (r >= off && r < off + run)) row[i] = load8(x + (long long)r * stride);
                 }
-                if (fv != 1.f) v_store<D>(rec, r, piece, rescale16(v_load<D>(rec, r, piece), fv));
-            }
-            if (full) { add4(c.x, s); add4(c.y, s + 4); add4(c.z, s + 8); add4(c.w, s + 12); }
-        }
-        if (tid == 0) *params = make_float2(p8_pow2(ek), p8_pow2(ev));
-        if (full) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
+                for (int i = 0; i < TURNS; ++i) mag = mag8(row[i], mag);
+                mag = warp_mag(mag);
+                if (lane == 0) s_mag[buf][warp] = mag;
+                __syncthreads();
+                mag = max(max(s_mag[buf][0], s_mag[buf][1]), max(s_mag[buf][2], s_mag[buf][3]));
+                if (mag > BOUND<T>)
 #pragma unroll
-                for (int o = PIECES; o < 32; o <<= 1) s[i] += __shfl_xor_sync(0xFFFFFFFFu, s[i], o);
-            if (lane < PIECES)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(&s_sum[warp][16 * piece + 4 * i]) = make_float4(s[4 * i], s[4 * i + 1], s[4 * i + 2], s[4 * i + 3]);
-            __syncthreads();
-            if (warp == 0) {                                   // (done before this warp passes the next page's barrier)
-                float m[D / 32];
-#pragma unroll
-                for (int i = 0; i < D / 32; ++i) {
-                    const int c = lane * (D / 32) + i;
-                    m[i] = (s_sum[0][c] + s_sum[1][c]) + (s_sum[2][c] + s_sum[3][c]);
+                    for (int i = 0; i < TURNS; ++i) row[i] = bounded8<T>(row[i]);
+                int e = exponent_of_mag<T>(mag);
+                float f = 1.f;                                 // from the old scale to the new one
+                if (!WHOLE && off > 0) {
+                    const int o = p8_exponent_of(was);
+                    f = p8_pow2(max(min(o - e, 0), -126));
+                    e = max(e, o);
                 }
-                store_mean<D>(rec, m, p8_pow2(ek), lane);
+                const Quant<T> q(e);
+                float s[8] = {};
+#pragma unroll
+                for (int i = 0; i < TURNS; ++i) {
+                    const int r = i * ROWS + r0;
+                    if (!WHOLE && r >= off + run) continue;
+                    uint2* const to = KEYS ? k_at<D>(rec, r, piece) : v_at<D>(rec, r, piece);
+                    uint2 c;
+                    if (WHOLE || r >= off) {
+                        c = codes8(row[i], q);
+                        *to = c;
+                    } else {
+                        c = make_uint2(0u, 0u);
+                        if ((KEYS && full) || f != 1.f) c = *to;
+                        if (f != 1.f) {
+                            c = rescale8(c, f);
+                            *to = c;
+                        }
+                    }
+                    if (KEYS && (WHOLE || full)) { add4(c.x, s); add4(c.y, s + 4); }
+                }
+                if (tid == 0) *scale = p8_pow2(e);
+                if (KEYS && (WHOLE || full)) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+#pragma unroll
+                        for (int o = 16; o >= PIECES; o >>= 1) s[i] += __shfl_xor_sync(0xFFFFFFFFu, s[i], o);
+                    if (lane < PIECES) {
+                        *reinterpret_cast<float4*>(&s_sum[warp][8 * piece]) = make_float4(s[0], s[1], s[2], s[3]);
+                        *reinterpret_cast<float4*>(&s_sum[warp][8 * piece + 4]) = make_float4(s[4], s[5], s[6], s[7]);
+                    }
+                    __syncthreads();
+                    if (warp == 0) {                           // (done before this warp passes the next barrier)
+                        float m[D / 32];
+#pragma unroll
+                        for (int i = 0; i < D / 32; ++i) {
+                            const int c = lane * (D / 32) + i;
+                            m[i] = (s_sum[0][c] + s_sum[1][c]) + (s_sum[2][c] + s_sum[3][c]);
+                        }
+                        store_mean<D>(rec, m, p8_pow2(e), lane);
+                    }
+                }
             }
-        }
+        };
+        if (off == 0 && run == XSV_PAGE) store(std::true_type{});
+        else store(std::false_type{});
     }
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(THREADS, D == 64 ? 9 : 7) page8_append_kernel(const __grid_constant__ Append8 p) {
+    __shared__ uint32_t s_mag[2][WARPS];
+    __shared__ __align__(16) float s_sum[WARPS][D];
+    xsv_dep_release();
+    xsv_dep_sync();
+    const int parts = (p.pool.heads + p.across - 1) / p.across, t_block = blockIdx.x / parts * CHUNK, head0 = (blockIdx.x % parts) * p.across;
+    if (blockIdx.y == 0) append_pages<T, D, true>(p, t_block, head0, s_mag, s_sum);
+    else append_pages<T, D, false>(p, t_block, head0, s_mag, s_sum);
 }
 
 // ------------------------------------------------------------------ reading back
@@ -314,33 +353,43 @@ template <typename T> __device__ __forceinline__ uint4 values8(uint32_t c0, uint
     return make_uint4(value2<T>(a, s), value2<T>(b, s), value2<T>(c, s), value2<T>(d, s));
 }
 
+constexpr int READ_HEADS = 4;                 // heads of a token that a thread has on their way together
+
 template <typename T, int D>
 __global__ void __launch_bounds__(256) page8_read_kernel(const __grid_constant__ Read8 p) {
     using R = Page8Rec<D>;
-    constexpr int PIECES = D / 16;
+    constexpr int PIECES = D / 8;
     xsv_dep_release();
     xsv_dep_sync();
-    const int head = blockIdx.y, piece = threadIdx.x % PIECES;
+    const int head0 = blockIdx.y * READ_HEADS, piece = threadIdx.x % PIECES;
     const long long r = (long long)blockIdx.x * (256 / PIECES) + threadIdx.x / PIECES;
     if (r >= p.n_rows) return;
     const int seq = p.seq[r], pos = p.pos[r];
     int page = -1;
     const int len = seq >= 0 && seq < p.n_seqs ? p.total[seq] : 0;
     if (pos >= 0 && pos < len && pos / XSV_PAGE < p.width) page = p.table[(size_t)seq * p.width + pos / XSV_PAGE];
-    uint4 out[4] = {};
-    if (page >= 0 && page < p.pool.n_pages) {
-        const uint8_t* rec = page8_rec<D>(p.pool, page, head);
-        const int tok = pos % XSV_PAGE;
-        const float2 s = *reinterpret_cast<const float2*>(rec + R::PARAMS);
-        const uint4 k = *reinterpret_cast<const uint4*>(rec + R::K_CODES + k_at<D>(tok, piece)), v = v_load<D>(rec, tok, piece);
-        out[0] = values8<T>(k.x, k.y, s.x); out[1] = values8<T>(k.z, k.w, s.x);
-        out[2] = values8<T>(v.x, v.y, s.y); out[3] = values8<T>(v.z, v.w, s.y);
+    const bool is = page >= 0 && page < p.pool.n_pages;
+    const int tok = pos & (XSV_PAGE - 1), heads = min(READ_HEADS, p.pool.heads - head0);
+    float2 s[READ_HEADS];
+    uint2 k[READ_HEADS], v[READ_HEADS];
+#pragma unroll
+    for (int h = 0; h < READ_HEADS; ++h) {
+        s[h] = make_float2(0.f, 0.f);
+        k[h] = v[h] = make_uint2(0u, 0u);
+        if (is && h < heads) {
+            uint8_t* rec = page8_rec<D>(p.pool, page, head0 + h);
+            s[h] = *reinterpret_cast<const float2*>(rec + R::PARAMS);
+            k[h] = *k_at<D>(rec, tok, piece);
+            v[h] = *v_at<D>(rec, tok, piece);
+        }
     }
-    const size_t to = ((size_t)r * p.pool.heads + head) * D + 16 * piece;
-    uint4* const k_to = reinterpret_cast<uint4*>((T*)p.K + to);
-    uint4* const v_to = reinterpret_cast<uint4*>((T*)p.V + to);
-    k_to[0] = out[0]; k_to[1] = out[1];
-    v_to[0] = out[2]; v_to[1] = out[3];
+#pragma unroll
+    for (int h = 0; h < READ_HEADS; ++h) {
+        if (h >= heads) break;
+        const size_t to = ((size_t)r * p.pool.heads + head0 + h) * D + 8 * piece;
+        *reinterpret_cast<uint4*>((T*)p.K + to) = values8<T>(k[h].x, k[h].y, s[h].x);
+        *reinterpret_cast<uint4*>((T*)p.V + to) = values8<T>(v[h].x, v[h].y, s[h].y);
+    }
 }
 
 }  // namespace
@@ -370,10 +419,13 @@ extern "C" xsv_status xsv_page8_append(const xsv_page8_pool* pool, const void* K
     p.K = K; p.V = V; p.k_stride = k_stride; p.v_stride = v_stride;
     p.slot = slot_map; p.seq = token_seq; p.cu = cu_new; p.total = total_len;
     p.n_tokens = n_tokens; p.n_seqs = n_seqs;
-    const bool few = (long long)n_tokens <= 4LL * n_seqs;
-    const long long blocks = few ? (long long)n_tokens * ((pool->kv_heads + WARPS - 1) / WARPS) : ((long long)n_tokens + CHUNK - 1) / CHUNK * pool->kv_heads;
+    const bool few = (long long)n_tokens <= AP_FEW * n_seqs;
+    const long long chunks = ((long long)n_tokens + CHUNK - 1) / CHUNK;
+    p.across = few ? WARPS : 4;
+    while (!few && p.across > 1 && chunks * 2 * ((pool->kv_heads + p.across - 1) / p.across) < 8LL * xsv_sm_count()) p.across /= 2;
+    const long long blocks = (few ? n_tokens : chunks) * ((pool->kv_heads + p.across - 1) / p.across);
     if (blocks > 0x7FFFFFFFLL) return XSV_ERR_LIMIT;
-    auto go = [&](auto kernel) { return xsv_launch_dep(kernel, dim3((unsigned)blocks), dim3(THREADS), 0, (cudaStream_t)stream, p); };
+    auto go = [&](auto kernel) { return xsv_launch_dep(kernel, dim3((unsigned)blocks, few ? 1 : 2), dim3(THREADS), 0, (cudaStream_t)stream, p); };
     cudaError_t e;
     if (pool->dtype == XSV_F16) {
         if (few) e = pool->head_dim == 64 ? go(page8_append_few_kernel<__half, 64>) : go(page8_append_few_kernel<__half, 128>);
@@ -398,8 +450,8 @@ extern "C" xsv_status xsv_page8_read(const xsv_page8_pool* pool, const int* bloc
     if (((uintptr_t)K_out | (uintptr_t)V_out) & 15) return XSV_ERR_SHAPE;
     p.table = block_table; p.total = total_len; p.seq = token_seq; p.pos = positions; p.K = K_out; p.V = V_out;
     p.width = table_width; p.n_seqs = n_seqs; p.n_rows = n_rows;
-    const int rows = 256 / (pool->head_dim / 16);
-    const dim3 grid((unsigned)(((long long)n_rows + rows - 1) / rows), pool->kv_heads);
+    const int rows = 256 / (pool->head_dim / 8);
+    const dim3 grid((unsigned)(((long long)n_rows + rows - 1) / rows), (pool->kv_heads + READ_HEADS - 1) / READ_HEADS);
     auto go = [&](auto kernel) { return xsv_launch_dep(kernel, grid, dim3(256), 0, (cudaStream_t)stream, p); };
     cudaError_t e;
     if (pool->dtype == XSV_F16) e = pool->head_dim == 64 ? go(page8_read_kernel<__half, 64>) : go(page8_read_kernel<__half, 128>);

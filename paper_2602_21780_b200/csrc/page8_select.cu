@@ -225,9 +225,13 @@ template <int W> __device__ __forceinline__ void list_of(const Select& p, const 
 // of a token, so that the first step of the maximum over its heads needs no exchange.
 template <int ROWS> __device__ __forceinline__ void row_place(int rr, int& token, int& head) {
     const int g = rr & 7, high = rr >> 3;
-    if (ROWS == 1) { token = rr; head = 0; return; }
-    token = g / (ROWS / 2);
-    head = g % (ROWS / 2) * 2 + high;
+    if constexpr (ROWS == 1) {
+        token = rr;
+        head = 0;
+    } else {
+        token = g / (ROWS / 2);
+        head = g % (ROWS / 2) * 2 + high;
+    }
 }
 
 // Many tokens: 16 pages a warp and turn instead of 32, so that registers for 32 warps a multiprocessor remain.
@@ -398,44 +402,39 @@ __global__ void __launch_bounds__(THREADS, MODE == MANY ? 4 : 2) page8_select_ke
             // The rest of the maximum over a token's rows: of the values i < N that two lanes have, the lane whose bit is clear keeps the
             // first half, the other one the second, as long as there are several; then the keys.
             auto put = [&](int i, bool live, const float (&x)[NU][2]) {
-                constexpr int N0 = 2 * NU, N1 = N0 / 2, N2 = N1 / 2, N3 = N2 > 1 ? N2 / 2 : 1;
+                constexpr int N0 = 2 * NU, N1 = N0 / 2, N2 = N1 / 2;      // N2: 2 or 1
                 auto store_one = [&](float v, int at) {        // value `at` of the turn's: page 8 (at / 2) + 2 j + at % 2
                     store(live, i, base + 8 * (at >> 1) + 2 * j + (at & 1), ((at & 1) ? is[1] : is[0]) >> (at >> 1) & 1u ? order_of(v) : 0u);
                 };
                 float v[N0];
 #pragma unroll
                 for (int u = 0; u < NU; ++u) { v[2 * u] = x[u][0]; v[2 * u + 1] = x[u][1]; }
-                if (ROWS <= 2) {
+                const int b0 = g & 1, b1 = g >> 1 & 1, b2 = g >> 2;
+                if constexpr (ROWS <= 2) {
 #pragma unroll
                     for (int e = 0; e < N0; ++e) store_one(v[e], e);
-                    return;
-                }
-                const int b0 = g & 1, b1 = g >> 1 & 1, b2 = g >> 2;
-                float v1[N1];
+                } else {
+                    float v1[N1];
 #pragma unroll
-                for (int e = 0; e < N1; ++e) v1[e] = fmaxf(b0 ? v[N1 + e] : v[e], __shfl_xor_sync(0xFFFFFFFFu, b0 ? v[e] : v[N1 + e], 4));
-                if (ROWS == 4) {
+                    for (int e = 0; e < N1; ++e) v1[e] = fmaxf(b0 ? v[N1 + e] : v[e], __shfl_xor_sync(0xFFFFFFFFu, b0 ? v[e] : v[N1 + e], 4));
+                    if constexpr (ROWS == 4) {
 #pragma unroll
-                    for (int e = 0; e < N1; ++e) store_one(v1[e], N1 * b0 + e);
-                    return;
-                }
-                float v2[N2];
+                        for (int e = 0; e < N1; ++e) store_one(v1[e], N1 * b0 + e);
+                    } else {
+                        float v2[N2];
 #pragma unroll
-                for (int e = 0; e < N2; ++e) v2[e] = fmaxf(b1 ? v1[N2 + e] : v1[e], __shfl_xor_sync(0xFFFFFFFFu, b1 ? v1[e] : v1[N2 + e], 8));
-                if (ROWS == 8) {
+                        for (int e = 0; e < N2; ++e) v2[e] = fmaxf(b1 ? v1[N2 + e] : v1[e], __shfl_xor_sync(0xFFFFFFFFu, b1 ? v1[e] : v1[N2 + e], 8));
+                        if constexpr (ROWS == 8) {
 #pragma unroll
-                    for (int e = 0; e < N2; ++e) store_one(v2[e], N1 * b0 + N2 * b1 + e);
-                    return;
-                }
-                if (N2 > 1) {
-                    float v3[N3];
-#pragma unroll
-                    for (int e = 0; e < N3; ++e) v3[e] = fmaxf(b2 ? v2[N3 + e] : v2[e], __shfl_xor_sync(0xFFFFFFFFu, b2 ? v2[e] : v2[N3 + e], 16));
-#pragma unroll
-                    for (int e = 0; e < N3; ++e) store_one(v3[e], N1 * b0 + N2 * b1 + N3 * b2 + e);
-                } else {                                       // one left: both lanes have it
-                    const float one = fmaxf(v2[0], __shfl_xor_sync(0xFFFFFFFFu, v2[0], 16));
-                    if (b2 == 0) store_one(one, N1 * b0 + N2 * b1);
+                            for (int e = 0; e < N2; ++e) store_one(v2[e], N1 * b0 + N2 * b1 + e);
+                        } else if constexpr (N2 > 1) {
+                            const float one = fmaxf(b2 ? v2[1] : v2[0], __shfl_xor_sync(0xFFFFFFFFu, b2 ? v2[0] : v2[1], 16));
+                            store_one(one, N1 * b0 + N2 * b1 + b2);
+                        } else {                               // one left: both lanes have it
+                            const float one = fmaxf(v2[0], __shfl_xor_sync(0xFFFFFFFFu, v2[0], 16));
+                            if (b2 == 0) store_one(one, N1 * b0 + N2 * b1);
+                        }
+                    }
                 }
             };
             if (ROWS < 16) {
