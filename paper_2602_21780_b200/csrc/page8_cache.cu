@@ -2,22 +2,24 @@
 //
 // xsv_page8_append: codes are written as their tokens come, without a 16-bit copy that waits for the page to fill: the block's
 // scale is a power of two, so that a later token with a larger magnitude raises it and the codes that stand there are moved to
-// the new scale (exact unless they become subnormal).  One block per (page, head) for prompts, one warp where most sequences
-// bring a few tokens (decoding): the page's new rows are read once into registers, their largest magnitude is found, and they
-// are stored as codes.  Whoever brings a page's last token also sums its key codes per channel, exactly (at most 64 * 448,
-// in steps of 2^-9: 24 bits, so that no order of summation matters), for the mean key that a selection scores.
-// Bound by HBM: 2 bytes read and 1 written per element.
+// the new scale (exact unless they become subnormal).  A page's new rows are read once, their largest magnitude is found, and they are
+// stored as codes: by a warp where they are few, else by a block, keys and values apart.  Whoever brings a page's last token also sums
+// its key codes per channel, exactly (at most 64 * 448, in steps of 2^-9: 24 bits, so that no order of summation matters), for the
+// mean key that a selection scores.
+// Bound by HBM for prompts, 2 bytes read and 1 written per element, and by latency for single tokens: five loads that wait for one another.
+// What counts is warps in flight (36 a multiprocessor at head_dim 64, 28 at 128, against 20: 14.5 against 18.7 us) and a lane's 8
+// channels, whose codes fill whole sectors of both records' orders (16 channels: 21.7).
 //
 // xsv_page8_read: a thread looks one token up and decodes 8 channels of it, of up to 4 heads.
+//
+// Measured.  Append of 19 735 prompt tokens, 8 heads of 64, fp16: 14.5 us, 4.2 TB/s; 8 heads of 128, bf16: 24.5 us, 4.95 TB/s; one token for each
+// of 256 sequences, 8 heads of 128: 4.3 us.  Reading 19 735 tokens of 8 x 64 back: 12.9 us, 4.7 TB/s; 8150 of 8 x 128: 11.1 us, 4.5 TB/s.
 #include <type_traits>
 
 #include "../../include/xsv.h"
 #include "page8_layout.cuh"
 #include "xsv_kernels.h"
 
-#ifndef AP_FEW
-#define AP_FEW 4LL
-#endif
 namespace {
 
 struct Append8 {
@@ -29,7 +31,8 @@ struct Append8 {
     const int* seq;
     const int* cu;
     const int* total;
-    int n_tokens, n_seqs, across;      // across: heads of a block
+    int n_tokens, n_seqs;
+    int few_blocks, across;            // blocks that store a few tokens of a page; heads of each of the others
 };
 __device__ __forceinline__ bool place_of(const Append8& p, int t, PagePlace& q) {
     return page_place(p.slot, p.seq, p.cu, p.total, p.n_tokens, p.n_seqs, p.pool.n_pages, t, q);
@@ -127,18 +130,14 @@ template <int D> __device__ __forceinline__ void store_mean(uint8_t* rec, const 
 
 constexpr int WARPS = 4, THREADS = WARPS * 32;
 
-// ---- a few tokens a sequence: a warp per (page, head), the page's first new token in the list
+constexpr int FEW = 16;                      // new tokens of a page up to which a warp stores them
+
+// ---- a few new tokens of a page (decoding, the ends of prompts): a warp for one head of the page whose first new token is t
 template <typename T, int D>
-__global__ void __launch_bounds__(THREADS) page8_append_few_kernel(const __grid_constant__ Append8 p) {
+__device__ __forceinline__ void append_few(const Append8& p, const PagePlace& q, int t, int head) {
     using R = Page8Rec<D>;
     constexpr int PIECES = D / 8, ROWS = 32 / PIECES;         // rows of a turn
-    xsv_dep_release();
-    xsv_dep_sync();
-    const int lane = threadIdx.x & 31, across = (p.pool.heads + WARPS - 1) / WARPS;
-    const int t = blockIdx.x / across, head = (blockIdx.x - t * across) * WARPS + (threadIdx.x >> 5);
-    PagePlace q;
-    if (head >= p.pool.heads || !place_of(p, t, q) || !(t == q.begin || q.off == 0)) return;
-    const int run = min(XSV_PAGE - q.off, q.end - t), r_lane = lane / PIECES, piece = lane % PIECES;
+    const int lane = threadIdx.x & 31, run = min(XSV_PAGE - q.off, q.end - t), r_lane = lane / PIECES, piece = lane % PIECES;
     uint8_t* rec = page8_rec<D>(p.pool, q.page, head);
     const T* K = (const T*)p.K + (size_t)t * p.k_stride + (size_t)head * D + 8 * piece;
     const T* V = (const T*)p.V + (size_t)t * p.v_stride + (size_t)head * D + 8 * piece;
@@ -207,8 +206,8 @@ __global__ void __launch_bounds__(THREADS) page8_append_few_kernel(const __grid_
     store_mean<D>(rec, s, p8_pow2(ek), lane);
 }
 
-// ---- prompts: a block looks for the first new tokens of pages among CHUNK ones and stores the keys, or the values, of p.across heads of
-// each page, one after the other
+// ---- more of them: a block looks for the first new tokens of pages among CHUNK ones and stores the keys, or the values, of p.across heads
+// of each page, one after the other
 constexpr int CHUNK = 32;
 
 template <typename T, int D, bool KEYS>
@@ -220,7 +219,8 @@ __device__ __forceinline__ void append_pages(const Append8& p, int t_block, int 
     const int r0 = D == 128 ? 4 * (warp >> 1) + (warp & 1) + 2 * (lane >> 4) : 8 * (warp >> 1) + (warp & 1) + 2 * (lane >> 3);
     const int heads = min(p.across, p.pool.heads - head0);
     PagePlace mine{};
-    const bool first = t_block + lane < p.n_tokens && place_of(p, t_block + lane, mine) && (t_block + lane == mine.begin || mine.off == 0);
+    const bool first = t_block + lane < p.n_tokens && place_of(p, t_block + lane, mine) && (t_block + lane == mine.begin || mine.off == 0) &&
+                       min(XSV_PAGE - mine.off, mine.end - t_block - lane) > FEW;
     int buf = 0;
     for (uint32_t todo = __ballot_sync(0xFFFFFFFFu, first); todo; todo &= todo - 1) {      // the same for every warp
         const int from = __ffs(todo) - 1, t = t_block + from;
@@ -317,8 +317,22 @@ __global__ void __launch_bounds__(THREADS, D == 64 ? 9 : 7) page8_append_kernel(
     __shared__ __align__(16) float s_sum[WARPS][D];
     xsv_dep_release();
     xsv_dep_sync();
-    const int parts = (p.pool.heads + p.across - 1) / p.across, t_block = blockIdx.x / parts * CHUNK, head0 = (blockIdx.x % parts) * p.across;
-    if (blockIdx.y == 0) append_pages<T, D, true>(p, t_block, head0, s_mag, s_sum);
+    if ((int)blockIdx.x < p.few_blocks) {
+        // a sequence and WARPS heads: its first page here, and its last one
+        const int parts = (p.pool.heads + WARPS - 1) / WARPS, seq = blockIdx.x / parts, head = (blockIdx.x - seq * parts) * WARPS + (threadIdx.x >> 5);
+        const int begin = p.cu[seq], end = p.cu[seq + 1], total = p.total[seq];
+        if (head >= p.pool.heads || begin < 0 || end <= begin || end > p.n_tokens || total < end - begin) return;
+        const int last = (total - 1) / XSV_PAGE * XSV_PAGE - (total - (end - begin));        // the last page's first token, counted from `begin`
+        for (int t = begin;; t = begin + last) {
+            PagePlace q;
+            if (place_of(p, t, q) && q.seq == seq && min(XSV_PAGE - q.off, q.end - t) <= FEW) append_few<T, D>(p, q, t, head);
+            if (last <= 0 || t > begin) return;
+        }
+    }
+    // the blocks for keys, which take longer, come first
+    const int parts = (p.pool.heads + p.across - 1) / p.across, half = (gridDim.x - p.few_blocks) / 2, at = blockIdx.x - p.few_blocks, i = at < half ? at : at - half;
+    const int t_block = i / parts * CHUNK, head0 = i % parts * p.across;
+    if (at < half) append_pages<T, D, true>(p, t_block, head0, s_mag, s_sum);
     else append_pages<T, D, false>(p, t_block, head0, s_mag, s_sum);
 }
 
@@ -419,21 +433,20 @@ extern "C" xsv_status xsv_page8_append(const xsv_page8_pool* pool, const void* K
     p.K = K; p.V = V; p.k_stride = k_stride; p.v_stride = v_stride;
     p.slot = slot_map; p.seq = token_seq; p.cu = cu_new; p.total = total_len;
     p.n_tokens = n_tokens; p.n_seqs = n_seqs;
-    const bool few = (long long)n_tokens <= AP_FEW * n_seqs;
-    const long long chunks = ((long long)n_tokens + CHUNK - 1) / CHUNK;
-    p.across = few ? WARPS : 4;
-    while (!few && p.across > 1 && chunks * 2 * ((pool->kv_heads + p.across - 1) / p.across) < 8LL * xsv_sm_count()) p.across /= 2;
-    const long long blocks = (few ? n_tokens : chunks) * ((pool->kv_heads + p.across - 1) / p.across);
+    // A warp each for the pages that get at most 16 tokens, one or two a sequence, and blocks for the others, in one launch: a step may hold
+    // decoding sequences and prompts.  8 heads of 128, all warps against all blocks: 128 sequences of 1 token 3.9 against 46 us, of 8 tokens 6.2
+    // against 14, of 16 tokens 9.4 against 12.5; 4 sequences of 32 tokens, heads of 64: 5.9 against 4.2.  A block takes 4 heads (prompts of 19 735
+    // tokens 14.5 us; 2 heads 15.7, 8 heads 20) while there are 8 blocks a multiprocessor.
+    const long long chunks = ((long long)n_tokens + CHUNK - 1) / CHUNK, few = (long long)n_seqs * ((pool->kv_heads + WARPS - 1) / WARPS);
+    p.across = 4;
+    while (p.across > 1 && chunks * 2 * ((pool->kv_heads + p.across - 1) / p.across) < 8LL * xsv_sm_count()) p.across /= 2;
+    const long long blocks = few + 2 * chunks * ((pool->kv_heads + p.across - 1) / p.across);
     if (blocks > 0x7FFFFFFFLL) return XSV_ERR_LIMIT;
-    auto go = [&](auto kernel) { return xsv_launch_dep(kernel, dim3((unsigned)blocks, few ? 1 : 2), dim3(THREADS), 0, (cudaStream_t)stream, p); };
+    p.few_blocks = (int)few;
+    auto go = [&](auto kernel) { return xsv_launch_dep(kernel, dim3((unsigned)blocks), dim3(THREADS), 0, (cudaStream_t)stream, p); };
     cudaError_t e;
-    if (pool->dtype == XSV_F16) {
-        if (few) e = pool->head_dim == 64 ? go(page8_append_few_kernel<__half, 64>) : go(page8_append_few_kernel<__half, 128>);
-        else e = pool->head_dim == 64 ? go(page8_append_kernel<__half, 64>) : go(page8_append_kernel<__half, 128>);
-    } else {
-        if (few) e = pool->head_dim == 64 ? go(page8_append_few_kernel<__nv_bfloat16, 64>) : go(page8_append_few_kernel<__nv_bfloat16, 128>);
-        else e = pool->head_dim == 64 ? go(page8_append_kernel<__nv_bfloat16, 64>) : go(page8_append_kernel<__nv_bfloat16, 128>);
-    }
+    if (pool->dtype == XSV_F16) e = pool->head_dim == 64 ? go(page8_append_kernel<__half, 64>) : go(page8_append_kernel<__half, 128>);
+    else e = pool->head_dim == 64 ? go(page8_append_kernel<__nv_bfloat16, 64>) : go(page8_append_kernel<__nv_bfloat16, 128>);
     if (e != cudaSuccess) return xsv_cuda_status(e);
     xsv_count_launch(1);
     return XSV_OK;
