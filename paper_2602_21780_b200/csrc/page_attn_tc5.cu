@@ -1,4 +1,4 @@
-// Attention of many query rows a head over the 4-bit pages, on the 5th-generation tensor cores (tcgen05.mma,
+// Attention of many query rows a head over the 4-bit or 8-bit pages, on the 5th-generation tensor cores (tcgen05.mma,
 // accumulators in tensor memory): out = softmax(scale q K^T, causal, window) V.
 //
 // A unit is (sequence, pair of 128-row query tiles, key/value head), a row being (new token, query head of the
@@ -20,12 +20,14 @@
 // that bf16 of any size fits; P is fp16, sums and accumulators are float32.  Every wait is bounded; when one runs out the
 // kernel runs to its end and the rows it touched become NaN.
 //
-// Measured.  1374 tokens on 21 984, 16 heads of 64: 215 to 228 us, 560 to 590 TFLOP/s (0.40 to 0.42 of the sustained bf16
-// peak; the kernel for few rows took 788); 6 chunks of 300 to 2047 tokens on up to 9000, 32 / 8 heads of 128: 418 us,
-// 830 TFLOP/s (0.59; 2545).  At head_dim 64 the exponentials alone, 16 a clock and multiprocessor, take about 115 us of the former.
+// Measured.  1374 tokens on 21 984, 16 heads of 64, 4 bit: 217 us, 590 TFLOP/s (0.42 of the sustained bf16 peak; the kernel for few
+// rows took 788); 6 chunks of 300 to 2047 tokens on up to 9000, 32 / 8 heads of 128: 4 bit 398 us, 876 TFLOP/s (0.62), 8 bit 369 us, 945
+// TFLOP/s (0.67; first version 403).  At head_dim 64 the exponentials alone, 16 a clock and multiprocessor, take about 115 us of the frame.
 // The softmax warps are busy 90 % of the time, the producers wait 55 % of it for free stages.  Storing the tiles
 // through generic addresses cost 20 %; the second half of the logits arriving under the first half's exponentials and the
-// range of unmasked pages known per unit gave 5 %; a share of 1/8 of the exponentials as polynomials cost 10 %.
+// range of unmasked pages known per unit gave 5 %; a share of 1/8 of the exponentials as polynomials cost 10 %; quarters of the logits with
+// the next step's first one ahead cost 4 to 7 % (more waits, more registers).  A unit's begin and end took 17 % of the chunks: queries by
+// asynchronous copies under the results' way out, parts in an order that a warp writes whole, 32-bit divisions: 5 to 8 %.
 #include <algorithm>
 
 #include "page8_layout.cuh"
@@ -36,9 +38,10 @@
 namespace {
 
 constexpr int BM = 128, NPROD = 6, NTHREADS = (8 + NPROD + 2) * 32;
-// Cost of a step with two query tiles, with one, and of entering a unit, in ticks: the ratios of the attention over
-// the contiguous cache, whose steps are two pages, taken over as they are and not fitted to this kernel.
-constexpr int COST_PAIR = 16, COST_SINGLE = 13, COST_UNIT = 144, MIN_SPAN = 320;
+// Cost of a step with two query tiles, with one, and of entering a unit, in ticks: the steps' are the ratios of the attention over the
+// contiguous cache; a unit's is fitted (6 chunks, 8-bit pages: 72 430 us, 100 405, 144 377, 160 369, 200 373; 4-bit 448, 425, 398, 398, 401; a
+// frame on 21 984 does not tell them apart).
+constexpr int COST_PAIR = 16, COST_SINGLE = 13, COST_UNIT = 160, MIN_SPAN = 320;
 constexpr float SUM_LIMIT = 256.f;             // a row sum that reaches 2^8: look for the maximum again
 constexpr float NO_MAX = -1e30f;
 
@@ -57,7 +60,7 @@ template <int D> struct Cfg {
     static_assert(2 * NBUF * 64 + 2 * D <= 512, "tensor memory");
     static constexpr uint32_t IDESC_QK = (1u << 4) | (64u >> 3 << 17) | ((uint32_t)(BM >> 4) << 24);
     static constexpr uint32_t IDESC_PV = (1u << 4) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
-    static constexpr int PART = 256 * (D + 2);                       // floats of a part: rows, then (maximum, sum)
+    static constexpr int PART = 256 * (D + 2);                       // floats of a part: [D / 4][256 rows] of 4 channels, then (maximum, sum) of the rows
 };
 
 // One pair of query tiles of one sequence, for every head alike.
@@ -167,9 +170,13 @@ __device__ __forceinline__ void settle(const Work& w, Units& u) {          // fr
     for (;;) {
         if (u.e >= u.entries || u.base >= u.t1) { u.valid = false; return; }
         const int cost = step_cost(u.en);
-        const long long a = u.t0 - u.base - COST_UNIT, b = u.t1 - u.base - COST_UNIT;
-        u.kv0 = (int)min(max(a <= 0 ? 0LL : (a + cost - 1) / cost, 0LL), (long long)u.en.pages);
-        u.kv1 = (int)min(max(b <= 0 ? 0LL : (b + cost - 1) / cost, 0LL), (long long)u.en.pages);
+        // steps that begin before a tick of the unit (a unit's ticks are a 32-bit number; so are its divisions)
+        auto steps = [&](long long tick) {
+            const long long x = tick - u.base - COST_UNIT;
+            return x <= 0 ? 0 : x >= (long long)u.en.pages * cost ? u.en.pages : (int)(((uint32_t)x + cost - 1) / (uint32_t)cost);
+        };
+        u.kv0 = steps(u.t0);
+        u.kv1 = steps(u.t1);
         if (u.kv0 < u.kv1) { u.valid = true; return; }
         u.base += u.en.ticks;
         if (++u.h == u.heads) {
@@ -513,6 +520,66 @@ __device__ __forceinline__ void softmax32(const uint32_t (&v)[32], unsigned long
     }
 }
 
+// A warp's 32 rows of a query tile, of queries and of results, in turns of ROWS rows with 16 bytes a lane, so that global memory
+// sees whole rows.  Functions of their own, with their loops rolled: the registers and the instruction cache are the softmax's.
+template <int D> struct RowTurns {
+    static constexpr int PER_ROW = D / 8, ROWS = 32 / PER_ROW, TURNS = 32 / ROWS;
+};
+// The rows of a unit on their way into the tile, as they are.  Called when the tile's products with the rows before are done: the
+// results' way out hides the latency.
+template <typename T, int D>
+__device__ __noinline__ void fetch_queries(const PageAttn& p, int t0, int row0, int n_rows, int h, int X, uint32_t tile) {
+    constexpr int PER_ROW = RowTurns<D>::PER_ROW, ROWS = RowTurns<D>::ROWS, TURNS = RowTurns<D>::TURNS;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, chunk = lane % PER_ROW, first = (warp & 3) * 32 + lane / PER_ROW;
+    const T* base = (const T*)p.Q + (size_t)h * p.group * D + 8 * chunk;
+    const int q0 = row0 + X * BM;
+#pragma unroll 4
+    for (int y = 0; y < TURNS; ++y) {
+        const int row = first + y * ROWS, q = min(q0 + row, n_rows - 1);
+        int qi, qh;
+        page_row(p, q, qi, qh);
+        cp_async16(tile + (chunk >> 3) * 16384 + swz(row, chunk & 7), base + (size_t)(t0 + qi) * p.q_stride + (size_t)qh * D, q0 + row < n_rows ? 16u : 0u);
+    }
+    cp_async_commit();
+}
+// In place: the thread's row -> fp16, its largest element in [1, 2); returns its logit factor.
+template <typename T, int D>
+__device__ __noinline__ float scale_query(float scale, uint8_t* tile) {
+    const int row = threadIdx.x & 127;
+    auto at = [&](int k) { return reinterpret_cast<uint4*>(tile + (k >> 3) * 16384 + swz(row, k & 7)); };
+    cp_async_wait_all();
+    __syncwarp();                                          // the row is other lanes' copies
+    float mx = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < D / 8; ++k) {
+        const uint4 x = *at(k);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float2 f = xsv_unpack2<T>(word(x, q));
+            mx = fmax3(mx, fabsf(f.x), fabsf(f.y));
+        }
+    }
+    const int e = mx > 0.f ? max((__float_as_int(mx) >> 23) - 127, -126) : 0;
+    const float s1 = __int_as_float((127 - e / 2) << 23), s2 = __int_as_float((127 - (e - e / 2)) << 23);
+#pragma unroll 1
+    for (int k0 = 0; k0 < D / 8; k0 += 4) {
+        uint4 x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = *at(k0 + k);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            uint32_t z[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float2 f = xsv_unpack2<T>(word(x[k], q));
+                z[q] = pack_h2(f.x * s1 * s2, f.y * s1 * s2);
+            }
+            *at(k0 + k) = make_uint4(z[0], z[1], z[2], z[3]);
+        }
+    }
+    return fmaxf(scale * __int_as_float((127 + min(e, 127)) << 23), MIN_FACTOR);
+}
+
 // BITS 8: a page's keys have a scale, which goes into the factor of its logits, and its values one, 2^ev, by which the weights are
 // multiplied; so the logits are moved by ev, the maximum is that of the moved ones, and the sum takes ev back.
 template <typename T, int D, int BITS>
@@ -523,48 +590,24 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tS = c.tmem + lane_base + C::tm_s(X, 0), tO = c.tmem + lane_base + C::tm_o(X);
     uint8_t* sQ = c.smem + X * C::Q_TILE;
+    auto row_token = [&](int q) { int i, h; page_row(p, q, i, h); return i; };
     uint32_t it = 0, cX = 0;                       // steps of the CTA; steps of this query tile
+    bool fetched = false;
     // Completion of the P V of step j (see the attention over the contiguous cache: one barrier per S buffer, never more
     // than one phase ahead of the waits on it)
     auto wait_pv = [&](uint32_t j) { mbar_wait(BAR(C::PVDONE + X * C::NBUF + (int)(j % C::NBUF)), (j / C::NBUF) & 1u, c.abort_flag, c.status, XSV_DEV_SITE_PV); };
-    for (; u.valid; next_unit(w, u)) {
+    while (u.valid) {
         const int n = u.kv1 - u.kv0, r = u.en.row0 + X * BM + row;
-        if (u.en.row0 + X * BM >= u.en.n_rows) { it += (uint32_t)n; continue; }     // no second tile
-        int i, h;
-        page_row(p, min(r, u.en.n_rows - 1), i, h);
-        const int qpos = u.en.first + i, total = min(u.en.first + u.en.n_rows / p.group, p.width * XSV_PAGE);
-        // ---- the query row -> fp16, its largest element in [1, 2)
-        float sc;
-        {
-            const T* src = (const T*)p.Q + (size_t)(u.en.t0 + i) * p.q_stride + (size_t)(u.h * p.group + h) * D;
-            const bool there = r < u.en.n_rows;
-            float mx = 0.f;
-#pragma unroll
-            for (int k = 0; k < D / 8; ++k) {
-                uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                if (there) x = reinterpret_cast<const uint4*>(src)[k];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float2 f = xsv_unpack2<T>(word(x, q));
-                    mx = fmaxf(mx, fmaxf(fabsf(f.x), fabsf(f.y)));
-                }
-            }
-            const int e = mx > 0.f ? max((__float_as_int(mx) >> 23) - 127, -126) : 0;
-            const float s1 = __int_as_float((127 - e / 2) << 23), s2 = __int_as_float((127 - (e - e / 2)) << 23);
-            sc = fmaxf(p.scale * __int_as_float((127 + min(e, 127)) << 23), MIN_FACTOR);
-#pragma unroll
-            for (int k = 0; k < D / 8; ++k) {
-                uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                if (there) x = reinterpret_cast<const uint4*>(src)[k];
-                uint32_t y[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float2 f = xsv_unpack2<T>(word(x, q));
-                    y[q] = pack_h2(f.x * s1 * s2, f.y * s1 * s2);
-                }
-                *reinterpret_cast<uint4*>(sQ + (k >> 3) * 16384 + swz(row, k & 7)) = make_uint4(y[0], y[1], y[2], y[3]);
-            }
+        if (u.en.row0 + X * BM >= u.en.n_rows) {           // no second tile
+            it += (uint32_t)n;
+            next_unit(w, u);
+            continue;
         }
+        const int qpos = u.en.first + row_token(min(r, u.en.n_rows - 1)), total = min(u.en.first + u.en.n_rows / p.group, p.width * XSV_PAGE);
+        // ---- the query rows (the first unit's are fetched here, the others' ahead)
+        if (!fetched) fetch_queries<T, D>(p, u.en.t0, u.en.row0, u.en.n_rows, u.h, X, smem_u32(sQ));
+        fetched = false;
+        const float sc = scale_query<T, D>(p.scale, sQ);
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(BAR(C::QFULL + X));
@@ -662,22 +705,29 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
             first = false;
         }
         it += (uint32_t)n;
-        // ---- epilogue
-        wait_pv(cX - 1u);
-        tc_fence_after();
-        const bool full = u.kv0 == 0 && u.kv1 == u.en.pages;
-        if (*c.abort_flag) l = __int_as_float(0x7FC00000);
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+        // ---- epilogue, the next unit's queries on their way meanwhile
+        const bool full = u.kv0 == 0 && u.kv1 == u.en.pages, there = u.en.row0 + X * BM + row < u.en.n_rows;
+        int i, h;
+        page_row(p, min(u.en.row0 + X * BM + row, u.en.n_rows - 1), i, h);
         T* dst = (T*)p.out + ((size_t)(u.en.t0 + i) * p.q_heads + u.h * p.group + h) * D;
         float* part = w.part + ((size_t)blockIdx.x * 2 + (u.kv0 > 0 ? 0 : 1)) * C::PART;
-        float4* pr = reinterpret_cast<float4*>(part + (size_t)(X * BM + row) * D);
-#pragma unroll
+        float4* pr = reinterpret_cast<float4*>(part) + X * BM + row;        // [D / 4 channels][256 rows]
+        next_unit(w, u);
+        if (u.valid && u.en.row0 + X * BM < u.en.n_rows) {
+            fetch_queries<T, D>(p, u.en.t0, u.en.row0, u.en.n_rows, u.h, X, smem_u32(sQ));
+            fetched = true;
+        }
+        wait_pv(cX - 1u);
+        tc_fence_after();
+        if (*c.abort_flag) l = __int_as_float(0x7FC00000);
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll 2
         for (int q = 0; q < D / 16; ++q) {
             uint32_t o[16];
             tmem_ld16(tO + 16u * q, o);
             tc_wait_ld();
             if (full) {
-                if (r < u.en.n_rows) {
+                if (there) {
                     uint32_t y[8];
 #pragma unroll
                     for (int k = 0; k < 8; ++k) y[k] = page_result2<T>(__uint_as_float(o[2 * k]) * inv, __uint_as_float(o[2 * k + 1]) * inv);
@@ -687,7 +737,7 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
             } else {
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    pr[4 * q + k] = make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]), __uint_as_float(o[4 * k + 2]), __uint_as_float(o[4 * k + 3]));
+                    pr[(4 * q + k) * 256] = make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]), __uint_as_float(o[4 * k + 2]), __uint_as_float(o[4 * k + 3]));
             }
         }
         if (!full) reinterpret_cast<float2*>(part + 256 * D)[X * BM + row] = make_float2(m_used, l);
@@ -878,7 +928,7 @@ __global__ void __launch_bounds__(256) page_attn_tc5_merge_kernel(const __grid_c
     const int4 d = w.desc[b];
     if (d.z == 0) return;
     const Entry en = load_entry(w, d.x);
-    const int row = blockIdx.y * 16 + (threadIdx.x >> 4), c = threadIdx.x & 15, r = en.row0 + row;
+    const int row = blockIdx.y * 16 + (threadIdx.x & 15), c = threadIdx.x >> 4, r = en.row0 + row;
     if (r >= en.n_rows) return;
     auto part = [&](int i) { return w.part + ((size_t)(b - 1 + i) * 2 + (i == 0 ? 1 : 0)) * C::PART; };
     float m = NO_MAX, l = 0.f;
@@ -894,7 +944,7 @@ __global__ void __launch_bounds__(256) page_attn_tc5_merge_kernel(const __grid_c
         l = l * a + ml.y * e;
 #pragma unroll
         for (int k = 0; k < D / 64; ++k) {
-            const float4 x = reinterpret_cast<const float4*>(src + (size_t)row * D)[16 * k + c];
+            const float4 x = reinterpret_cast<const float4*>(src)[(16 * k + c) * 256 + row];
             o[k] = make_float4(o[k].x * a + x.x * e, o[k].y * a + x.y * e, o[k].z * a + x.z * e, o[k].w * a + x.w * e);
         }
     }
