@@ -17,6 +17,11 @@
 // steps as the list has places.  A warp works alone (own page buffer in shared memory, filled by bulk copies, own softmax state): while
 // it takes the products with a page's keys the values arrive, and the other way round.  A unit shared by several warps is
 // merged by a second kernel in the order of the warps, so results do not depend on timing.
+//
+// Measured.  64 sequences of 900 to 16 000 tokens, one new token each, 32 query and 8 key/value heads of 128, bf16: 184 us, 6.0 TB/s (0.93 of the
+// copy rate); 4 tokens over 200 001: 78 us, 5.2 TB/s; one sequence of 261, 16 heads of 64: 8.1 us with the merge, launch and latency.  Selected:
+// 32 sequences, 32 pages a head: 34.7 us, 3.9 TB/s (4.6 pages a warp behind four loads that wait for one another); 509 tokens of
+// one sequence, 24 pages each: 152 us, 10.5 TB/s out of L2: 760 instructions a page, of which 265 convert, at 11 warps a multiprocessor.
 #include <algorithm>
 #include <cmath>
 
@@ -620,7 +625,9 @@ int workers_of(int head_dim, int nt) {
 // 8 query rows a tile where a head has no more, else 16
 int tiles_of(long long rows) { return rows <= 8 ? 1 : 2; }
 
-// Sequences with more query rows a head go to the tensor-memory kernel.
+// Sequences with more query rows a head go to the tensor-memory kernel, whose time does not depend on them up to 128.
+// 8 sequences of 8000 tokens, this kernel against that one: 16 heads of 64, 64 rows 92 against 98 us, 80 rows 112 against 99; 8
+// key/value heads of 128, 32 rows 60 against 74, 48 rows 70 against 75, 64 rows 87 against 75.
 int few_rows(int head_dim) { return head_dim == 64 ? 64 : 48; }
 bool many_rows(int max_new, int group, int head_dim) { return (long long)max_new * group > few_rows(head_dim); }
 

@@ -7,9 +7,10 @@
 // roundings that the formula has, whatever order the sums are taken in: a selection can be repeated bit for bit.
 //
 // Reads d + 4 bytes a page and head where the attention reads 128 d, so what bounds it is latency for single tokens, and
-// instructions for many.  A block takes a few tokens of one head: mma.m16n8k32 over 16 pages x 8 query rows, keys of the scores
-// (unsigned, in their order) into shared memory, then the k-th largest by bisection and a pass that writes page numbers in order.  A cluster of up to 8 blocks shares the pages of one token where few tokens have long sequences: each
-// stores its scores into the first block's shared memory, which selects.
+// instructions for many.  A block takes a token, or a few, of one head: mma.m16n8k32 over 16 query rows x 8 pages, the scores as unsigned
+// numbers in their order ("keys") into shared memory, then the k-th largest by bracketing and a pass that writes page numbers in order.
+// A cluster of up to 8 blocks shares the pages of one token where few tokens have long sequences: each stores its keys into the first block's
+// shared memory, which selects.
 //
 // Measured.  32 query and 8 key/value heads of 128, 32 pages each: 16 tokens over 2000 to 60 000: 11.4 us, of which the launch and
 // four loads that wait for one another (token, table, mean key; query) are about 6, the selection 3; 1021 tokens over 40 000: 41 us, half of it
@@ -550,12 +551,15 @@ extern "C" xsv_status xsv_page8_select(const xsv_page8_pool* pool, const void* Q
     p.Q = Q; p.q_stride = q_stride; p.table = block_table; p.seq = token_seq; p.pos = positions; p.slot = slot_map; p.out = selected;
     p.width = table_width; p.n_seqs = n_seqs; p.n_tokens = n_tokens; p.top = top; p.first = first; p.recent = recent;
     p.rows = p.group > 8 ? (p.group + 15) / 16 * 16 : p.group > 4 ? 8 : p.group > 2 ? 4 : p.group;
-    // Many tokens: 8 a block, a warp selects for each; few: one, and up to 8 blocks a token while there are idle
-    // multiprocessors and each block has 128 pages at least.
+    // Many tokens: 8 a block, a warp selects for each.  8 heads of 128 over 40 000 tokens, 8 tokens a block against one: 24 tokens of a sequence
+    // 12.6 against 11.4 us, 40 tokens 13.2 against 16.8, 296 tokens 16.6 against 72.  Where they belong to as many sequences a block scores for
+    // one after the other: 64 sequences 41 against 22, 128 sequences 44 against 38, 512 sequences 26 against 82.
+    // Few: one a block, and 2 to 8 blocks a token while that leaves them two multiprocessors each and each has 128 pages at least (one sequence of
+    // 200 000 tokens: 1 block 23.2 us, 8 blocks 13.3; 20 000: 1 block 7.1, 2 blocks 6.9; 16 sequences of 60 000: 2 blocks 13.3, 4 blocks 16.5).
     const long long units = (long long)n_tokens * pool->kv_heads;
     p.tokens = 1;
     p.cluster = 1;
-    if (units >= 8LL * 2 * xsv_sm_count()) {
+    if (units >= (n_tokens >= 8LL * n_seqs ? 2LL : 8LL) * xsv_sm_count()) {
         p.tokens = 8;
         while (p.tokens > 1 && (smem_of(p.tokens, p.rows, pool->head_dim, table_width) > SMEM_MAX || p.tokens * p.rows > XSV_PAGE8_MAX_GROUP)) p.tokens /= 2;
     } else {
