@@ -630,6 +630,12 @@ int tiles_of(long long rows) { return rows <= 8 ? 1 : 2; }
 // key/value heads of 128, 32 rows 60 against 74, 48 rows 70 against 75, 64 rows 87 against 75.
 int few_rows(int head_dim) { return head_dim == 64 ? 64 : 48; }
 bool many_rows(int max_new, int group, int head_dim) { return (long long)max_new * group > few_rows(head_dim); }
+// ... unless there is so little to do that its launches and its units' begins and ends, 28 to 40 us, are most of it.  What bounds the work is
+// known on the host: pages that the table has room for, times tiles of 16 rows.  This kernel against that one: heads of 128, a bound of 1584 19 us
+// against 38, 8448 34 against 39, 9696 37 against 39, 16 448 54 against 40; heads of 64, 4608 20 against 33, 14 784 35 against 36, 20 736 40 against 36.
+bool little_work(int n_tokens, int n_seqs, int group, int heads, int width, int head_dim) {
+    return ((long long)n_tokens * group / 16 + n_seqs) * heads * width <= (head_dim == 64 ? 14336 : 8960);
+}
 
 size_t few_space(int nt, int head_dim) {
     const size_t workers = (size_t)workers_of(head_dim, nt), pf = (size_t)nt * (head_dim / 16) * 128 + nt * 16;
@@ -710,7 +716,7 @@ extern "C" xsv_status xsv_page8_attention(const xsv_page8_pool* pool, const void
     cudaStream_t st = (cudaStream_t)stream;
     cudaError_t e = cudaSuccess;
     p.row_limit = 1 << 30;
-    if (many_rows(max_new, p.group, pool->head_dim)) {
+    if (many_rows(max_new, p.group, pool->head_dim) && !little_work(n_tokens, n_seqs, p.group, pool->kv_heads, table_width, pool->head_dim)) {
         p.row_limit = n_seqs == 1 ? 0 : few_rows(pool->head_dim);
         e = xsv_launch_page8_tc5(p, pool->dtype, pool->head_dim, (char*)workspace + few_space(nt, pool->head_dim), st);
     }
