@@ -257,8 +257,8 @@ def test_append_at_the_ends_of_the_range(dtype):
 
 
 @pytest.mark.parametrize("d", [64, 128])
-def test_both_append_kernels_store_the_same(d):
-    # the same tokens beside many idle sequences go to the kernel for a few tokens a sequence
+def test_append_beside_idle_sequences(d):
+    # sequences that bring nothing change nothing, wherever they stand
     n, hkv = 397, 3
     g = torch.Generator(device="cuda").manual_seed(3)
     k, v = (torch.randn(n, hkv, d, device="cuda", generator=g).to(torch.bfloat16) for _ in range(2))
@@ -299,7 +299,7 @@ def test_append_skips_tokens_without_a_place():
     sv = Server(2, 2, 64, "fp16", pages=8, width=4)
     sv.step([10, 70])
     before = sv.pages.clone()
-    for idle in (0, 8):                                     # both kernels
+    for idle in (0, 8):
         k = torch.ones(8, 2, 64, device="cuda", dtype=sv.dt)
         for slot, seq, cu, total in (([-1] * 8, [0] * 8, [0, 8, 8], [18, 70]),             # refused
                                      ([5] * 8, [99] * 8, [0, 8, 8], [18, 70]),             # no such sequence
