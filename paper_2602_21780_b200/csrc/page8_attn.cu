@@ -21,7 +21,7 @@
 // Measured.  64 sequences of 900 to 16 000 tokens, one new token each, 32 query and 8 key/value heads of 128, bf16: 184 us, 6.0 TB/s (0.93 of the
 // copy rate); 4 tokens over 200 001: 78 us, 5.2 TB/s; one sequence of 261, 16 heads of 64: 8.1 us with the merge, launch and latency.  Selected:
 // 32 sequences, 32 pages a head: 34.7 us, 3.9 TB/s (4.6 pages a warp behind four loads that wait for one another); 509 tokens of
-// one sequence, 24 pages each: 152 us, 10.5 TB/s out of L2: 760 instructions a page, of which 265 convert, at 11 warps a multiprocessor.
+// one sequence, 24 pages each: 152 us, 10.5 TB/s out of L2, which bounds it (142 without the conversions, a third of 760 instructions a page).
 #include <algorithm>
 #include <cmath>
 

@@ -14,9 +14,9 @@
 // near 10^6 would be off by 0.03 rad.  With several positions a token (time, height, width) the thread that serves a frequency
 // looks up once which of them it turns by.  Norms are float32, the layer norm's variance from differences to the mean (two
 // passes over registers); results are rounded once, to the output type.
-// Measured: 8191 tokens, 32 + 8 + 8 heads of 128, fp16: 43.6 us, 4.6 TB/s; 1374 tokens, 3 x 16 heads of 64: 6.2 us; one token: 2.5 us.
-// What is left to the copy rate is loads in flight: 8 blocks of 4 warps with one or two rows each; four rows a lane group or fewer
-// blocks were slower (48-52 us), and packed float32 arithmetic changed nothing.
+// Measured: 8191 tokens, 32 + 8 + 8 heads of 128, fp16: 41.8 us, 4.8 TB/s (one token a turn: 44.5); 1374 tokens, 3 x 16 heads of 64: 7.5 us with two
+// positions; one token: 2.6 us.  What is left to the copy rate is loads in flight: 7 or 8 blocks of 4 warps with two rows each; three to
+// six rows a lane group or fewer blocks were slower (48-54 us), and packed float32 arithmetic changed nothing.
 #include <algorithm>
 #include <type_traits>
 
@@ -49,10 +49,12 @@ template <typename T> __device__ __forceinline__ void unpack4(const uint2& w, fl
 
 constexpr int THREADS = 128, FLIGHT = 2;      // FLIGHT: rows of a lane group in flight
 
-template <typename T, int D, int ROPE, int NORM, bool BIAS>
-__global__ void __launch_bounds__(THREADS, 8) qk_norm_rope_kernel(const __grid_constant__ NormRope p) {
+// TOK: tokens of a turn.  2 (many tokens): the two rows in flight are the same head of two tokens, all threads compute sines, and
+// a barrier serves both tokens.
+template <typename T, int D, int ROPE, int NORM, bool BIAS, int TOK>
+__global__ void __launch_bounds__(THREADS, TOK == 2 ? 7 : 8) qk_norm_rope_kernel(const __grid_constant__ NormRope p) {
     constexpr int L = D / 8, GROUPS = THREADS / L;
-    __shared__ float2 cs[2][D / 2];
+    __shared__ float2 cs[2][TOK][D / 2];
     xsv_dep_release();
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
     // the lane's two pieces of four channels, and the index of the first frequency of each pair it rotates
@@ -86,23 +88,26 @@ __global__ void __launch_bounds__(THREADS, 8) qk_norm_rope_kernel(const __grid_c
             }
         }
     }
-    const int n_freq = p.n_rot / 2, h0 = blockIdx.y * GROUPS, step = gridDim.y * GROUPS;
-    // the frequency this thread serves; its position is fetched a token ahead
-    const bool serves = ROPE != XSV_ROPE_NONE && (int)threadIdx.x < n_freq;
+    const int n_freq = p.n_rot / 2, h0 = TOK == 2 ? 0 : blockIdx.y * GROUPS, step = TOK == 2 ? GROUPS : gridDim.y * GROUPS;
+    // the frequency this thread serves, of which of the turn's tokens; its position is fetched a turn ahead
+    const int mine = TOK == 2 ? (int)threadIdx.x / (D / 2) : 0, fi = (int)threadIdx.x - mine * (D / 2);
+    const bool serves = ROPE != XSV_ROPE_NONE && mine < TOK && fi < n_freq;
     int coord = 0, at = 0;
     double freq = 0.0;
     if (serves) {
         const int per = ROPE == XSV_ROPE_2D ? n_freq / 2 : n_freq;
-        coord = threadIdx.x / per;
-        freq = (double)p.inv_freq[threadIdx.x - coord * per];
+        coord = fi / per;
+        freq = (double)p.inv_freq[fi - coord * per];
         if (ROPE != XSV_ROPE_2D && p.axes) {
-            coord = p.axes[threadIdx.x];
+            coord = p.axes[fi];
             if (coord < 0 || coord >= p.n_pos) { coord = 0; freq = 0.0; }       // no such position: not rotated
         }
-        at = p.pos[(size_t)blockIdx.x * p.n_pos + coord];
+        const int t = blockIdx.x + mine * gridDim.x;
+        if (t < p.n_tokens) at = p.pos[(size_t)t * p.n_pos + coord];
     }
     int buf = 0;
-    for (int t = blockIdx.x; t < p.n_tokens; t += gridDim.x, buf ^= 1) {
+    for (int t = blockIdx.x; t < p.n_tokens; t += TOK * gridDim.x, buf ^= 1) {
+        const bool second = TOK == 2 && t + (int)gridDim.x < p.n_tokens;
         float2 r[4];
         if (ROPE != XSV_ROPE_NONE) {
             if (serves) {
@@ -110,13 +115,14 @@ __global__ void __launch_bounds__(THREADS, 8) qk_norm_rope_kernel(const __grid_c
                 turns -= rint(turns);
                 float s, c;
                 sincospif(2.f * (float)turns, &s, &c);
-                cs[buf][threadIdx.x] = make_float2(c, s);
-                const int next = t + gridDim.x;
+                cs[buf][mine][fi] = make_float2(c, s);
+                const int next = t + (mine + TOK) * (int)gridDim.x;
                 if (next < p.n_tokens) at = p.pos[(size_t)next * p.n_pos + coord];
             }
-            __syncthreads();                                // two buffers: the last token's are read before this one
+            __syncthreads();                                // two buffers: the last turn's are read before this one
+            if (TOK == 1)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) r[i] = rot ? cs[buf][f + i] : make_float2(1.f, 0.f);
+                for (int i = 0; i < 4; ++i) r[i] = rot ? cs[buf][0][f + i] : make_float2(1.f, 0.f);
         }
 #pragma unroll
         for (int part = 0; part < 3; ++part) {
@@ -124,27 +130,28 @@ __global__ void __launch_bounds__(THREADS, 8) qk_norm_rope_kernel(const __grid_c
             if (h0 >= heads) continue;
             const T* src = (const T*)p.x[part] + (size_t)t * p.stride[part];
             T* dst = (T*)p.y[part] + (size_t)t * p.y_tok[part];
+            const size_t src_on = TOK == 2 ? (size_t)gridDim.x * p.stride[part] : 0, dst_on = TOK == 2 ? (size_t)gridDim.x * p.y_tok[part] : 0;      // to the second token
             float w[8], b[8];
             if (NORM != XSV_NORM_NONE && part < 2) {
                 unpack4<T>(wgt[part][0], w); unpack4<T>(wgt[part][1], w + 4);
                 if (BIAS) { unpack4<T>(bias[part][0], b); unpack4<T>(bias[part][1], b + 4); }
             }
             // two rows of the group at a time; every lane of the warp takes part in the shuffles, whatever its row
-            for (int base = h0; base < heads; base += FLIGHT * step) {
+            for (int base = h0; base < heads; base += TOK == 2 ? step : FLIGHT * step) {
                 uint2 in[FLIGHT][2];
 #pragma unroll
                 for (int u = 0; u < FLIGHT; ++u) {
-                    const int h = base + u * step + group;
+                    const int h = base + (TOK == 2 ? 0 : u * step) + group;
                     in[u][0] = in[u][1] = make_uint2(0u, 0u);
-                    if (h < heads) {
-                        in[u][0] = *reinterpret_cast<const uint2*>(src + (size_t)h * D + ca);
-                        in[u][1] = *reinterpret_cast<const uint2*>(src + (size_t)h * D + cb);
+                    if (h < heads && (TOK == 1 || u == 0 || second)) {
+                        in[u][0] = *reinterpret_cast<const uint2*>(src + u * src_on + (size_t)h * D + ca);
+                        in[u][1] = *reinterpret_cast<const uint2*>(src + u * src_on + (size_t)h * D + cb);
                     }
                 }
 #pragma unroll
                 for (int u = 0; u < FLIGHT; ++u) {
-                    const int h = base + u * step + group;
-                    if (base + u * step >= heads) break;    // the same for the whole block
+                    const int h = base + (TOK == 2 ? 0 : u * step) + group;
+                    if (TOK == 1 && base + u * step >= heads) break;    // the same for the whole block
                     if (part < 2 && (NORM != XSV_NORM_NONE || ROPE != XSV_ROPE_NONE)) {
                         float v[8];
                         unpack4<T>(in[u][0], v);
@@ -170,18 +177,19 @@ __global__ void __launch_bounds__(THREADS, 8) qk_norm_rope_kernel(const __grid_c
                         if (ROPE != XSV_ROPE_NONE) {
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
+                                const float2 turn = TOK == 1 ? r[i] : rot ? cs[buf][u % TOK][f + i] : make_float2(1.f, 0.f);
                                 float& lo = ROPE == XSV_ROPE_PAIRS ? v[2 * i] : v[i];
                                 float& hi = ROPE == XSV_ROPE_PAIRS ? v[2 * i + 1] : v[4 + i];
                                 const float x0 = lo, x1 = hi;
-                                lo = x0 * r[i].x - x1 * r[i].y;
-                                hi = x1 * r[i].x + x0 * r[i].y;
+                                lo = x0 * turn.x - x1 * turn.y;
+                                hi = x1 * turn.x + x0 * turn.y;
                             }
                         }
                         in[u][0] = make_uint2(xsv_pack2<T>(v[0], v[1]), xsv_pack2<T>(v[2], v[3]));
                         in[u][1] = make_uint2(xsv_pack2<T>(v[4], v[5]), xsv_pack2<T>(v[6], v[7]));
                     }
-                    if (h < heads) {
-                        T* to = dst + (size_t)h * p.y_head[part];
+                    if (h < heads && (TOK == 1 || u == 0 || second)) {
+                        T* to = dst + u * dst_on + (size_t)h * p.y_head[part];
                         *reinterpret_cast<uint2*>(to + ca) = in[u][0];
                         *reinterpret_cast<uint2*>(to + cb) = in[u][1];
                     }
@@ -198,14 +206,26 @@ cudaError_t launch(const NormRope& p, int norm, int rope, cudaStream_t st) {
     // through its share of them (32 + 8 + 8 heads of 128: 148 tokens 3.1 against 3.6 us, 296 tokens 3.9 either way, 592
     // tokens 5.8 against 4.4).
     const dim3 grid(std::min(p.n_tokens, full), p.n_tokens >= 2 * xsv_sm_count() ? 1 : (most + groups - 1) / groups);
-    auto go = [&](auto kernel) { return xsv_launch_dep(kernel, grid, dim3(THREADS), 0, st, p); };
+    // Two tokens a turn where each block gets more than one turn of them, in as many blocks as make the turns come out even (8219 tokens, heads of 128
+    // 44.8 -> 42.0 us; 8000 tokens, heads of 64, layer norm 30.8 -> 24.3).
+    const int pairs = (p.n_tokens + 1) / 2, most2 = 7 * xsv_sm_count(), turns = (pairs + most2 - 1) / most2;
+    const bool two = turns > 1;
+    const dim3 grid2((pairs + turns - 1) / turns);
     const bool bias = p.b[0] || p.b[1];
     auto with = [&](auto rope_c) {
         constexpr int ROPE = decltype(rope_c)::value;
+        auto go = [&](auto norm_c, auto bias_c) {
+            constexpr int NORM = decltype(norm_c)::value;
+            constexpr bool BIAS = decltype(bias_c)::value;
+            return two ? xsv_launch_dep(qk_norm_rope_kernel<T, D, ROPE, NORM, BIAS, 2>, grid2, dim3(THREADS), 0, st, p)
+                       : xsv_launch_dep(qk_norm_rope_kernel<T, D, ROPE, NORM, BIAS, 1>, grid, dim3(THREADS), 0, st, p);
+        };
+        using Rms = std::integral_constant<int, XSV_NORM_RMS>;
+        using Layer = std::integral_constant<int, XSV_NORM_LAYER>;
         switch (norm) {
-            case XSV_NORM_RMS: return bias ? go(qk_norm_rope_kernel<T, D, ROPE, XSV_NORM_RMS, true>) : go(qk_norm_rope_kernel<T, D, ROPE, XSV_NORM_RMS, false>);
-            case XSV_NORM_LAYER: return bias ? go(qk_norm_rope_kernel<T, D, ROPE, XSV_NORM_LAYER, true>) : go(qk_norm_rope_kernel<T, D, ROPE, XSV_NORM_LAYER, false>);
-            default: return go(qk_norm_rope_kernel<T, D, ROPE, XSV_NORM_NONE, false>);
+            case XSV_NORM_RMS: return bias ? go(Rms{}, std::true_type{}) : go(Rms{}, std::false_type{});
+            case XSV_NORM_LAYER: return bias ? go(Layer{}, std::true_type{}) : go(Layer{}, std::false_type{});
+            default: return go(std::integral_constant<int, XSV_NORM_NONE>{}, std::false_type{});
         }
     };
     switch (rope) {
