@@ -114,12 +114,13 @@ def mean_key(codes, e):
 def scores(q, means):
     """float32 scores of pages with (codes, factor) for the query rows q [group, d] of one token."""
     best = np.full(len(means), -np.inf, np.float32)
+    if not means:
+        return best
+    codes, factor = np.stack([m[0] for m in means]).astype(np.int64), np.array([m[1] for m in means], np.float32)
     for row in np.asarray(q, np.float32):
         a = np.maximum(np.abs(row).max(), np.float32(2.0 ** -60)).astype(np.float32)
         q8 = np.rint(row * (np.float32(127) / a)).astype(np.int64)
-        for i, (codes, factor) in enumerate(means):
-            s = np.float32(int(q8 @ codes)) * np.float32(factor) * a
-            best[i] = max(best[i], s)
+        best = np.maximum(best, (codes @ q8).astype(np.float32) * factor * a)
     return best
 
 

@@ -326,10 +326,14 @@ def test_attention_single_tokens(dtype, d, hq, hkv):
         sv.check_attention(plan, new, hq, window=130, scale=0.3)
 
 
+WIDE = 1500           # table rows with room for so much that the kernel for many rows takes what it can
+
+
+@pytest.mark.parametrize("width", [16, WIDE])
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
 @pytest.mark.parametrize("d,hq,hkv", SHAPES)
-def test_attention_many_tokens(dtype, d, hq, hkv):
-    sv = Server(5, hkv, d, dtype, pages=60, width=16, seed=hq + 1)
+def test_attention_many_tokens(dtype, d, hq, hkv, width):
+    sv = Server(5, hkv, d, dtype, pages=60, width=width, seed=hq + 1)
     for new in ([3, 130, 64, 1, 0], [7, 2, 5, 3, 1], [65, 33, 129, 64, 300]):
         plan = sv.step(new)
         sv.check_attention(plan, new, hq)
@@ -337,11 +341,11 @@ def test_attention_many_tokens(dtype, d, hq, hkv):
         sv.check_attention(plan, new, hq, window=77)
 
 
-@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("new,width", [(1, 8), (40, 8), (40, WIDE)])
 @pytest.mark.parametrize("dtype,spread", [("bf16", 1e-12), ("bf16", 1e-3), ("fp16", 1e-3), ("bf16", 300.0), ("fp16", 300.0), ("fp16", 6000.0)])
-def test_attention_over_values_of_any_size(new, dtype, spread):
+def test_attention_over_values_of_any_size(new, width, dtype, spread):
     # queries shrink as keys grow, so that the logits stay; the output grows with the values
-    sv = Server(2, 2, 64, dtype, pages=20, width=8, seed=3, spread=spread)
+    sv = Server(2, 2, 64, dtype, pages=20, width=width, seed=3, spread=spread)
     sv.step([300, 70])
     plan = sv.step([new, new])
     scale = None if spread > 1e-6 else 1e12
@@ -349,19 +353,38 @@ def test_attention_over_values_of_any_size(new, dtype, spread):
     sv.check_attention(plan, [new, new], 4, q=q.to(sv.dt), scale=scale)
 
 
-@pytest.mark.parametrize("new", [1, 40])
-def test_pages_of_very_different_scales(new):
+@pytest.mark.parametrize("new,width", [(1, 12), (40, 12), (40, WIDE)])
+def test_pages_of_very_different_scales(new, width):
     # pages 2^10 apart in both directions: neither the logits' factor nor the values' may come from a neighbour
-    sv = Server(1, 2, 128, "bf16", pages=20, width=12, seed=8)
+    sv = Server(1, 2, 128, "bf16", pages=20, width=width, seed=8)
     sizes = np.repeat(2.0 ** np.array([0, -10, 3, -5, 0, -8, 1]), PAGE)
     sv.step([7 * PAGE], sizes=sizes.tolist())
     plan = sv.step([new], sizes=[1.0] * new)
     sv.check_attention(plan, [new], 4, q=(sv.rnd(new, 4, 128) * 0.05).to(sv.dt))
 
 
-@pytest.mark.parametrize("new", [1, 3, 60])
-def test_attention_past_missing_pages_and_short_rows(new):
-    sv = Server(2, 2, 64, "bf16", pages=20, width=8, seed=6)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("hq,new", [(12, 4), (12, 10)])     # 48 and 120 query rows a head: both kernels
+def test_a_long_sequence_of_values_with_a_mean(d, dtype, hq, new):
+    # The weights' roundings, independent over 20 480 tokens, average out against a mean of 3: 2^-11 / sqrt(3 * 20480) of it. What stays is
+    # the result's, at most half a step and evenly spread, HALF / sqrt(3) rms; a tenth is left for sums in float32 (320 pages).
+    sv = Server(1, 1, d, dtype, pages=330, width=WIDE, seed=d + new)
+    for n in (20480, new):
+        plan = binding.page_plan(sv.len, ints([n]), sv.table, sv.ring, sv.state, n)
+        sv.len, sv.state = plan.total_len, plan.ring_state
+        k, v = ((sv.rnd(n, 1, d) + sv.mu) * sv.w).to(sv.dt), (sv.rnd(n, 1, d) + 3).to(sv.dt)
+        binding.page8_append(sv.pages, k, v, plan.slot_map, plan.token_seq, plan.cu_new, plan.total_len)
+        sv.note([n], plan, k, v)
+    q = sv.rnd(new, hq, d).to(sv.dt)
+    out, r = host(binding.page8_attention(q, sv.pages, sv.table, plan.cu_new, plan.total_len, new)), sv.ref[0][0]
+    ref = np.stack([orc4.attention(host(q[:, h]), r.k, r.v, d ** -0.5) for h in range(hq)], 1)
+    assert np.linalg.norm(out - ref) <= 1.1 * HALF[sv.dt] / np.sqrt(3) * np.linalg.norm(ref)
+
+
+@pytest.mark.parametrize("new,width", [(1, 8), (3, 8), (60, 8), (60, WIDE)])
+def test_attention_past_missing_pages_and_short_rows(new, width):
+    sv = Server(2, 2, 64, "bf16", pages=20, width=width, seed=6)
     sv.step([330, 100])
     plan = sv.step([new, new])
     q = sv.rnd(2 * new, 4, 64).to(sv.dt)
@@ -385,28 +408,28 @@ def test_attention_past_missing_pages_and_short_rows(new):
         assert np.linalg.norm(out[0, h] - ref) <= 3 * ATTN[sv.dt] * np.linalg.norm(ref)
 
 
-@pytest.mark.parametrize("new", [2, 50])
-def test_refused_sequences_and_rows_behind_the_last(new):
-    sv = Server(3, 2, 64, "fp16", pages=12, width=6, seed=2)
-    sv.step([100, 70, 64])
-    plan = binding.page_plan(sv.len, ints([new, 400, new]), sv.table, sv.ring, sv.state, 2 * new + 400 + 5)
+@pytest.mark.parametrize("new,width", [(2, 6), (50, 6), (50, WIDE)])
+def test_refused_sequences_and_rows_behind_the_last(new, width):
+    sv = Server(3, 2, 64, "fp16", pages=9, width=width, seed=2)
+    sv.step([100, 64, 70])
+    plan = binding.page_plan(sv.len, ints([new, new, 400]), sv.table, sv.ring, sv.state, 2 * new + 400 + 5)
     assert int(plan.ring_state[2]) == 1
     q = sv.rnd(2 * new + 405, 4, 64).to(sv.dt)
     k = sv.rnd(2 * new + 405, 2, 64).to(sv.dt)
     binding.page8_append(sv.pages, k, k, plan.slot_map, plan.token_seq, plan.cu_new, plan.total_len)
     out = torch.full_like(q, 7.0)
     binding.page8_attention(q, sv.pages, sv.table, plan.cu_new, plan.total_len, 400, out=out, slot_map=plan.slot_map)
-    assert not out[new:new + 400].any() and (out[2 * new + 400:] == 7).all() and out[:new].abs().sum() > 0
+    assert not out[2 * new:2 * new + 400].any() and (out[2 * new + 400:] == 7).all() and out[:2 * new].abs().sum() > 0
     sel = binding.page8_select(q, sv.pages, sv.table, plan.token_seq, plan.positions, 3, slot_map=plan.slot_map)
-    assert (sel[new:new + 400] == -1).all() and (sel[2 * new + 400:] == -1).all() and (sel[:new, :, 0] == 0).all()
+    assert (sel[2 * new:2 * new + 400] == -1).all() and (sel[2 * new + 400:] == -1).all() and (sel[:2 * new, :, 0] == 0).all()
     out.fill_(7.0)
     binding.page8_attention_selected(q, sv.pages, sv.table, plan.token_seq, plan.positions, sel, out=out)
-    assert not out[new:new + 400].any() and (out[2 * new + 400:] == 7).all() and out[:new].abs().sum() > 0
+    assert not out[2 * new:2 * new + 400].any() and (out[2 * new + 400:] == 7).all() and out[:2 * new].abs().sum() > 0
 
 
 def test_attention_in_the_place_of_the_queries_and_at_a_stride():
-    sv = Server(3, 2, 128, "bf16", pages=20, width=8, seed=7)
-    for new in ([100, 3, 1], [1, 1, 1]):
+    sv = Server(3, 2, 128, "bf16", pages=20, width=WIDE, seed=7)
+    for new in ([100, 3, 1], [1, 1, 1], [70, 1, 60]):
         plan = sv.step(new)
         n = sum(new)
         wide = sv.rnd(n, 7, 128).to(sv.dt)
@@ -442,6 +465,52 @@ def test_select_for_many_tokens(d, hq, hkv, n):
     new = [n // 2 + 1, 3, 0, n - n // 2 - 4]
     plan = sv.step(new, pad=9)
     sv.check_selection(plan, hq, 6, 1, 2)
+
+
+@pytest.mark.parametrize("d,hq,hkv", [(64, 40, 2), (128, 34, 1), (64, 128, 1), (128, 17, 1)])
+def test_large_groups(d, hq, hkv):
+    # more query heads to a key/value head than a tile has rows: several tiles of scores and of attention
+    sv = Server(3, hkv, d, "bf16", pages=60, width=20, seed=hq)
+    sv.step([0, 300, 900])
+    for new in ([1, 1, 1], [70, 3, 200]):                   # (one token a block, several)
+        plan = sv.step(new, pad=1)
+        sv.check_selection(plan, hq, 5, 1, 1)
+        sv.check_attention(plan, new, hq)
+
+
+def test_select_for_many_sequences():
+    # a block takes several tokens of as many sequences
+    n, hkv, d = 400, 4, 64
+    sv = Server(n, hkv, d, "fp16", pages=3 * n, width=4, seed=4)
+    sv.step([(37 * i) % 250 for i in range(n)])
+    plan = sv.step([1 if i % 7 else 0 for i in range(n)])
+    sv.check_selection(plan, 8, 2, 0, 1)
+
+
+def made_up_pool(pages, hkv, d, g):
+    pool = torch.zeros(pages, hkv, 130 * d, dtype=torch.uint8, device="cuda")
+    mean = torch.randint(-127, 128, (pages, hkv, d), device="cuda", generator=g, dtype=torch.int8)
+    factor = torch.rand(pages, hkv, device="cuda", generator=g)
+    pool[..., 128 * d + 32:129 * d + 32] = mean.view(torch.uint8)
+    pool[..., 64 * d + 8:64 * d + 12] = factor[..., None].contiguous().view(torch.uint8)
+    return pool, mean.cpu().numpy().astype(np.int64), factor.cpu().numpy()
+
+
+@pytest.mark.parametrize("tokens,width,top", [(1, 32768, 1024), (1, 9000, 3), (160, 1300, 40), (150, 4000, 200)])
+def test_select_over_wide_tables(tokens, width, top):
+    # more pages than a lane holds scores of, for one token and for several a block; up to the widest table and the longest list
+    d, pages, hkv = 64, 3000, 2 if tokens > 1 else 1
+    g = torch.Generator(device="cuda").manual_seed(width)
+    pool, mean, factor = made_up_pool(pages, hkv, d, g)
+    table = torch.randint(0, pages, (1, width), device="cuda", generator=g).to(torch.int32)      # pages appear twice: equal scores
+    q = torch.randn(tokens, 2 * hkv, d, device="cuda", generator=g).to(torch.bfloat16)
+    positions = [64 * width - 1 - 64 * 7 * i for i in range(tokens)]
+    sel = binding.page8_select(q, pool, table, ints([0] * tokens), ints(positions), top, first=1, recent=2).cpu().numpy()
+    row, qh = table[0].cpu().numpy(), host(q)
+    for t in range(0, tokens, 9):
+        for h in range(hkv):
+            means = [(mean[p, h], factor[p, h]) for p in row]
+            assert sel[t, h].tolist() == orc.select(qh[t, 2 * h:2 * h + 2], means, positions[t] // 64, top, 1, 2)
 
 
 @pytest.mark.parametrize("hkv,top", [(1, 40), (2, 7), (8, 300)])
@@ -562,7 +631,7 @@ def test_steps_in_captured_graphs(dtype, d):
 
 
 def test_calls_repeat_bit_for_bit_and_on_several_streams():
-    sv = Server(4, 2, 128, "bf16", pages=60, width=20, seed=12)
+    sv = Server(4, 2, 128, "bf16", pages=60, width=WIDE, seed=12)
     sv.step([900, 300, 64, 0])
     new = [1, 30, 1, 70]
     plan = sv.step(new)
