@@ -19,9 +19,9 @@
 // merged by a second kernel in the order of the warps, so results do not depend on timing.
 //
 // Measured.  64 sequences of 900 to 16 000 tokens, one new token each, 32 query and 8 key/value heads of 128, bf16: 184 us, 6.0 TB/s (0.93 of the
-// copy rate); 4 tokens over 200 001: 78 us, 5.2 TB/s; one sequence of 261, 16 heads of 64: 8.1 us with the merge, launch and latency.  Selected:
-// 32 sequences, 32 pages a head: 34.7 us, 3.9 TB/s (4.6 pages a warp behind four loads that wait for one another); 509 tokens of
-// one sequence, 24 pages each: 152 us, 10.5 TB/s out of L2, which bounds it (142 without the conversions, a third of 760 instructions a page).
+// copy rate); 4 tokens over 200 001: 78 us, 5.2 TB/s; one sequence of 261, 16 heads of 64: 7.8 us with the merge, launch and latency.  Selected:
+// 32 sequences, 32 pages a head: 33.9 us, 4.0 TB/s (4.6 pages a warp behind four loads that wait for one another); 509 tokens of
+// one sequence, 24 pages each: 151 us, 10.6 TB/s out of L2, which bounds it (142 without the conversions, a third of 760 instructions a page).
 #include <algorithm>
 #include <cmath>
 
@@ -37,7 +37,7 @@ namespace {
 constexpr float P_BIAS = 6.f, P_SLACK = 4.f, NO_MAX = -1e30f;
 
 struct Attn8 : PageAttn {
-    int4* desc;          // [workers] units that begin to be shared: {sequence or token, head, tile, parts}; parts 0: none
+    int4* desc;          // [workers] units that begin to be shared: {first token, head, tile, parts << 8 | rows to write}; 0 parts: none
     float* part;         // [2 workers][slot] unnormalised rows
     // selected only
     const int* selected; // [n_tokens][heads][top]
@@ -181,7 +181,9 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page8_attn_kern
                 if (k > last) last = (int)k;
                 while (last + 1 < workers && steps * (last + 1) / workers < unit1) ++last;
                 while (last > worker && steps * last / workers >= unit1) --last;
-                if (lane == 0) p.desc[worker] = make_int4(cur.s, cur.head, cur.tile, last - worker + 2);
+                const bool write = !SEL || cur.q.total > 0 || (p.seq[cur.s] >= 0 && p.seq[cur.s] < p.n_seqs);
+                const int rows = write ? min(ROWS, cur.q.new_ * p.group - cur.tile * ROWS) : 0;
+                if (lane == 0) p.desc[worker] = make_int4(first_token<SEL>(p, cur.s), cur.head, cur.tile, (last - worker + 2) << 8 | rows);
             }
         }
     }
@@ -548,8 +550,10 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page8_attn_kern
 // Units that several warps share.  A block of 8 warps looks at the descriptions of 16 workers and merges 16 channels of the units that
 // begin to be shared there: as many warps a unit as there are for it, which take its parts in turn and are merged in their order; a lane has
 // 4 values (2 rows x 2 channels).  (The whole block for one unit after the other: 15 us instead of 5 where most units have two parts.)
+// (One warp for all channels of a unit: 147 instead of 151 us where a unit has at most two parts, 211 instead of 184 and 45 instead of 34 where
+// there are more.)  It costs the calls that share units 6 to 9 us: its launch, its descriptions' and then its parts' latency.
 constexpr int MERGE_UNITS = 16, MERGE_WARPS = 8;
-template <typename T, int D, int NT, bool SEL>
+template <typename T, int D, int NT>
 __global__ void __launch_bounds__(MERGE_WARPS * 32) page8_attn_merge_kernel(const __grid_constant__ Attn8 p, int workers) {
     constexpr int ROWS = 8 * NT, CT = D / 16, PF = Part<D, NT>::FLOATS;
     __shared__ float4 s_o[MERGE_WARPS][32], s_ml[MERGE_WARPS][32];
@@ -572,24 +576,34 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) page8_attn_merge_kernel(cons
     if (lane < MERGE_UNITS && w0 + lane < workers) mine = p.desc[w0 + lane];
     auto unit = [&](int from) { return make_int4(__shfl_sync(0xFFFFFFFFu, mine.x, from), __shfl_sync(0xFFFFFFFFu, mine.y, from), __shfl_sync(0xFFFFFFFFu, mine.z, from), __shfl_sync(0xFFFFFFFFu, mine.w, from)); };
     auto sum = [&](Acc& acc, int w, int parts, int i0, int step) {
-#pragma unroll 4
-        for (int i = i0; i < parts; i += step) {
-            const float* part = p.part + (size_t)(i == 0 ? 2 * (w - 1) + 1 : 2 * (w + i - 1)) * PF;
-            acc.add(reinterpret_cast<const float4*>(part)[(n * CT + ct) * 32 + lane], *reinterpret_cast<const float4*>(part + NT * CT * 128 + 2 * r0));
+        constexpr int AHEAD = 4;                                // parts on their way together (8: 3 % slower where units have few)
+        for (int i = i0; i < parts; i += AHEAD * step) {
+            float4 x[AHEAD], y[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int at = i + k * step;
+                x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                y[k] = make_float4(NO_MAX, 0.f, NO_MAX, 0.f);
+                if (at < parts) {
+                    const float* part = p.part + (size_t)(at == 0 ? 2 * (w - 1) + 1 : 2 * (w + at - 1)) * PF;
+                    x[k] = reinterpret_cast<const float4*>(part)[(n * CT + ct) * 32 + lane];
+                    y[k] = *reinterpret_cast<const float4*>(part + NT * CT * 128 + 2 * r0);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+                if (i + k * step < parts) acc.add(x[k], y[k]);
         }
     };
     auto write = [&](const Acc& acc, const int4& d) {
-        const Unit8 q = unit_of<SEL>(p, d.x, ROWS);
-        const int n_rows = q.new_ * p.group, t0 = first_token<SEL>(p, d.x);
-        if (SEL && q.total == 0 && !(p.seq[d.x] >= 0 && p.seq[d.x] < p.n_seqs)) return;
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
+            if (r0 + c >= (d.w & 255)) continue;
             const int r = d.z * ROWS + r0 + c;
-            if (r >= n_rows) continue;
             int i, h;
             page_row(p, r, i, h);
             const float l = c ? acc.ml.w : acc.ml.y, inv = l == 0.f ? 0.f : 1.f / l;
-            T* dst = (T*)p.out + ((size_t)(t0 + i) * p.q_heads + d.y * p.group + h) * D + (D / 8) * g + 2 * ct;
+            T* dst = (T*)p.out + ((size_t)(d.x + i) * p.q_heads + d.y * p.group + h) * D + (D / 8) * g + 2 * ct;
             *reinterpret_cast<uint32_t*>(dst) = page_result2<T>((c ? acc.o.y : acc.o.x) * inv, (c ? acc.o.w : acc.o.z) * inv);
         }
     };
@@ -604,7 +618,7 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) page8_attn_merge_kernel(cons
             for (int i = 0; i < at; ++i) rest &= rest - 1;
             from = __ffs(rest) - 1;
             d = unit(from);
-            sum(acc, w0 + from, d.w, wid % per, per);
+            sum(acc, w0 + from, d.w >> 8, wid % per, per);
         }
         if (per > 1) {                                          // once: every warp has one unit or none
             s_o[wid][lane] = acc.o;
@@ -659,7 +673,7 @@ template <typename T, int D, int NT, bool SEL> cudaError_t launch(Attn8& p, cuda
     cudaError_t e = xsv_launch_dep(kernel, dim3(grid), dim3(THREADS), smem, st, p);
     if (e != cudaSuccess) return e;
     xsv_count_launch(1);
-    e = xsv_launch_dep(page8_attn_merge_kernel<T, D, NT, SEL>, dim3((workers + MERGE_UNITS - 1) / MERGE_UNITS, NT * (D / 16)), dim3(MERGE_WARPS * 32), 0, st, p, workers);
+    e = xsv_launch_dep(page8_attn_merge_kernel<T, D, NT>, dim3((workers + MERGE_UNITS - 1) / MERGE_UNITS, NT * (D / 16)), dim3(MERGE_WARPS * 32), 0, st, p, workers);
     if (e == cudaSuccess) xsv_count_launch(1);
     return e;
 }
