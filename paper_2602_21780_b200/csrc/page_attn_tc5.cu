@@ -21,8 +21,9 @@
 // kernel runs to its end and the rows it touched become NaN.
 //
 // Measured.  1374 tokens on 21 984, 16 heads of 64, 4 bit: 217 us, 590 TFLOP/s (0.42 of the sustained bf16 peak; the kernel for few
-// rows took 788); 6 chunks of 300 to 2047 tokens on up to 9000, 32 / 8 heads of 128: 4 bit 398 us, 876 TFLOP/s (0.62), 8 bit 369 us, 945
-// TFLOP/s (0.67; first version 403).  At head_dim 64 the exponentials alone, 16 a clock and multiprocessor, take about 115 us of the frame.
+// rows took 788); 6 chunks of 300 to 2047 tokens on up to 9000, 32 / 8 heads of 128, in bursts: 4 bit 400 us, 872 TFLOP/s (0.61), 8 bit 380 us,
+// 917 TFLOP/s (0.65; 373 without the products that bring the values to their unit); call after call, under the power cap, 8 bit takes 395 to
+// 405 us (0.61 to 0.62).  At head_dim 64 the exponentials alone, 16 a clock and multiprocessor, take about 115 us of the frame.
 // The softmax warps are busy 90 % of the time, the producers wait 55 % of it for free stages.  Storing the tiles
 // through generic addresses cost 20 %; the second half of the logits arriving under the first half's exponentials and the
 // range of unmasked pages known per unit gave 5 %; a share of 1/8 of the exponentials as polynomials cost 10 %; quarters of the logits with
@@ -42,7 +43,10 @@ constexpr int BM = 128, NPROD = 6, NTHREADS = (8 + NPROD + 2) * 32;
 // contiguous cache; a unit's is fitted (6 chunks, 8-bit pages: 72 430 us, 100 405, 144 377, 160 369, 200 373; 4-bit 448, 425, 398, 398, 401; a
 // frame on 21 984 does not tell them apart).
 constexpr int COST_PAIR = 16, COST_SINGLE = 13, COST_UNIT = 160, MIN_SPAN = 320;
-constexpr float SUM_LIMIT = 256.f;             // a row sum that reaches 2^8: look for the maximum again
+// A row sum that reaches 2^8: look for the maximum again.  Over 8-bit pages weights and sums are 2^P_BIAS larger, still below fp16's largest
+// value, so that a weight keeps fp16's full significand down to 2^-21 of the maximum.
+constexpr float P_BIAS = 7.f;
+template <int BITS> constexpr float SUM_LIMIT = BITS == 8 ? 32768.f : 256.f;
 constexpr float NO_MAX = -1e30f;
 
 template <int D> struct Cfg {
@@ -362,7 +366,12 @@ __device__ __noinline__ void producer_loop(const PageAttn& p, const Work& w, con
     }
 }
 
-// 8-bit pages: the codes as fp16, without their scale, which the softmax warps take in; a stage's scales beside its page.
+// 8-bit pages: the codes as fp16.  The softmax warps take in the keys' scale, which stands beside a stage's page.  The values' scale 2^ev goes
+// into the operand: a unit's output is summed in units of 2^ref, and codes, whole numbers of 2^-9 up to 448, times 2^(ev - ref) are exact in
+// fp16 from 2^-15 to 2^7.  So pages whose scales are up to 2^22 apart share a ref, and the weights have nothing to do with scales.  ref is
+// settled for 32 steps at a time and changes as little as it can; where the scales of 32 pages are further apart each page is its own ref, and the
+// softmax warps move the output when ref changes.  (The exponent in the logits instead, as it once was, cost the weights beside a page with a
+// single large value their bits, or all of themselves.)
 // A slab is 64 tokens x 64 channels of keys, or half the values: at head_dim 128 all channels of 32 tokens (a lane's 8 tokens are
 // 8 consecutive columns of the tile), at 64 all 64 tokens.
 template <typename T, int D>
@@ -372,21 +381,36 @@ __device__ __noinline__ void producer8_loop(const PageAttn& p, const Work& w, co
     constexpr int SLABS = 2 * C::BLK;
     const int lane = threadIdx.x & 31, pw = (threadIdx.x >> 5) - 8, g = lane >> 2, j = lane & 3, odd = g & 1;
     auto BAR = [&](int i) { return c.bars + 8u * (uint32_t)i; };
-    struct Regs { uint4 code[8]; float2 scale; };
+    constexpr int MOVE_MIN = -15, MOVE_MAX = 7, REF_MIN = P8_EXP_MIN - MOVE_MIN, NO_REF = -1000;
+    struct Regs { uint4 code[8]; float scale; };
+    struct Step { int page, ref, move; };                      // its page (-1: none), what its output is counted in, and the values' way there
     uint32_t it = 0;                                           // steps of the CTA before the unit
     int slab = pw;                                             // this warp's next slab, counted from the unit's first
     for (; u.valid; next_unit(w, u)) {
         const int n = u.kv1 - u.kv0, total = min(u.en.first + u.en.n_rows / p.group, p.width * XSV_PAGE);
         const int* row = p.table + (size_t)u.en.seq * p.width + u.en.p0 + u.kv0;
-        int ids = -1, ids_from = -32;                          // page indices of 32 steps, one a lane
-        auto page_of = [&](int k) {
+        // pages, refs and ev - ref of 32 steps, one a lane; the last ref (a warp looks at every 32 steps that a unit has, in order)
+        int ids = -1, refs = 0, moves = 0, ids_from = -32, ref = NO_REF;
+        auto step_of = [&](int k) {
             if (k - ids_from >= 32) {
                 ids_from = k & ~31;
                 const int pg = u.en.p0 + u.kv0 + ids_from + lane;
                 ids = ids_from + lane < n && pg < p.width && pg * XSV_PAGE < total ? row[ids_from + lane] : -1;
                 if ((unsigned long long)(long long)ids >= (unsigned long long)p.pool.n_pages) ids = -1;
+                const bool is = ids >= 0;
+                int ev = 0;
+                if (is) ev = p8_exponent_of(reinterpret_cast<const float*>(page8_rec<D>(p.pool, ids, u.h) + R::PARAMS)[1]);
+                const int hi = __reduce_max_sync(0xFFFFFFFFu, is ? ev : NO_REF), lo = __reduce_min_sync(0xFFFFFFFFu, is ? ev : -NO_REF);
+                if (hi - lo <= MOVE_MAX - MOVE_MIN) {          // (no page at all: as before)
+                    if (hi >= lo) ref = max(min(max(ref == NO_REF ? (hi + lo) / 2 + 4 : ref, hi - MOVE_MAX), lo - MOVE_MIN), REF_MIN);
+                    refs = ref == NO_REF ? 0 : ref;
+                } else {
+                    refs = max(is ? ev : hi, REF_MIN);
+                    ref = __shfl_sync(0xFFFFFFFFu, refs, 31);
+                }
+                moves = is ? ev - refs : 0;
             }
-            return __shfl_sync(0xFFFFFFFFu, ids, k & 31);
+            return Step{__shfl_sync(0xFFFFFFFFu, ids, k & 31), __shfl_sync(0xFFFFFFFFu, refs, k & 31), __shfl_sync(0xFFFFFFFFu, moves, k & 31)};
         };
         auto fetch = [&](int sl, int page, Regs& r) {
             if (page < 0) return;
@@ -395,7 +419,7 @@ __device__ __noinline__ void producer8_loop(const PageAttn& p, const Work& w, co
             if (part < C::BLK) {
 #pragma unroll
                 for (int a = 0; a < 8; ++a) r.code[a] = ld16(rec + R::K_CODES + ((a * C::BLK + part) * 32 + lane) * 16);
-                if (part == 0) r.scale = *reinterpret_cast<const float2*>(rec + R::PARAMS);
+                if (part == 0) r.scale = *reinterpret_cast<const float*>(rec + R::PARAMS);
             } else if (D == 128) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) r.code[i] = ld16(rec + R::V_CODES + ((8 * (part - C::BLK) + i) * 32 + lane) * 16);
@@ -409,28 +433,28 @@ __device__ __noinline__ void producer8_loop(const PageAttn& p, const Work& w, co
             }
         };
         Regs cur{}, nxt{};
-        int page = -1, page_n = -1;
+        Step here{-1, 0, 0}, ahead{-1, 0, 0};
         if (slab < n * SLABS) {
-            page = page_of(slab / SLABS);
-            fetch(slab, page, cur);
+            here = step_of(slab / SLABS);
+            fetch(slab, here.page, cur);
         }
         while (slab < n * SLABS) {
             const int k = slab / SLABS, part = slab % SLABS, next = slab + NPROD;
             if (next < n * SLABS) {
-                page_n = page_of(next / SLABS);
-                fetch(next, page_n, nxt);
+                ahead = step_of(next / SLABS);
+                fetch(next, ahead.page, nxt);
             }
             const uint32_t step = it + (uint32_t)k, st = step % C::NSTAGE;
             if (step >= (uint32_t)C::NSTAGE) mbar_wait(BAR(C::EMPTY + (int)st), (step / C::NSTAGE - 1u) & 1u, c.abort_flag, c.status, XSV_DEV_SITE_STAGE);
-            const int held = page < 0 ? 0 : total - (u.en.p0 + u.kv0 + k) * XSV_PAGE;      // tokens of the page
+            const int held = here.page < 0 ? 0 : total - (u.en.p0 + u.kv0 + k) * XSV_PAGE;      // tokens of the page
             const uint32_t stage = c.base + C::OFF_KV + st * C::STAGE;
             if (part < C::BLK) {
                 const uint32_t tile = stage + part * 8192;
                 if (part == 0 && lane == 0) {
-                    asm volatile("st.shared.b32 [%0], %1;" ::"r"(c.page_ok + 4u * st), "r"(page >= 0 ? 1 : 0) : "memory");
-                    // keys' scale, and the values' as the exponent that the logits are moved by
-                    asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(c.page_ok + 4u * C::NSTAGE + 8u * st), "f"(page >= 0 ? cur.scale.x : 1.f),
-                                 "f"(page >= 0 ? (float)p8_exponent_of(cur.scale.y) : 0.f) : "memory");
+                    asm volatile("st.shared.b32 [%0], %1;" ::"r"(c.page_ok + 4u * st), "r"(here.page >= 0 ? 1 : 0) : "memory");
+                    // keys' scale, ref
+                    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(c.page_ok + 4u * C::NSTAGE + 8u * st),
+                                 "r"(__float_as_int(here.page >= 0 ? cur.scale : 1.f)), "r"(here.ref) : "memory");
                 }
                 // 16 channels of a token: two chunks of its row (keys of places without a token are masked, whatever they are)
 #pragma unroll
@@ -445,6 +469,13 @@ __device__ __noinline__ void producer8_loop(const PageAttn& p, const Work& w, co
             } else {
                 const int v = part - C::BLK;
                 const uint32_t tile = stage + C::K_TILE;
+                // 2^move, a pair of fp16 (2^-15 is a subnormal one)
+                const uint32_t by = (here.move == MOVE_MIN ? 0x0200u : (uint32_t)(here.move + 15) << 10) * 0x10001u;
+                auto values = [&](uint32_t codes, uint32_t& lo, uint32_t& hi) {
+                    p8_halves(codes, lo, hi);
+                    lo = hmul2_u(lo, by);
+                    hi = hmul2_u(hi, by);
+                };
                 if (held < XSV_PAGE) {                         // places without a token: zeros, whatever the record holds there
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
@@ -464,8 +495,8 @@ __device__ __noinline__ void producer8_loop(const PageAttn& p, const Work& w, co
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
                             const uint32_t x = word(cur.code[2 * q], i), y = word(cur.code[2 * q + 1], i);
-                            p8_halves(__byte_perm(x, y, 0x5140), e[0][q], e[1][q]);
-                            p8_halves(__byte_perm(x, y, 0x7362), e[2][q], e[3][q]);
+                            values(__byte_perm(x, y, 0x5140), e[0][q], e[1][q]);
+                            values(__byte_perm(x, y, 0x7362), e[2][q], e[3][q]);
                         }
 #pragma unroll
                         for (int q = 0; q < 4; q += 2) {       // lanes of odd g in another order, so that a store's lanes touch different banks
@@ -482,8 +513,8 @@ __device__ __noinline__ void producer8_loop(const PageAttn& p, const Work& w, co
 #pragma unroll
                         for (int q = 0; q < 8; ++q) {
                             const uint32_t x = word(cur.code[q], i), y = word(cur.code[q], i + 2);
-                            p8_halves(__byte_perm(x, y, 0x5140), e[0][q], e[1][q]);
-                            p8_halves(__byte_perm(x, y, 0x7362), e[2][q], e[3][q]);
+                            values(__byte_perm(x, y, 0x5140), e[0][q], e[1][q]);
+                            values(__byte_perm(x, y, 0x7362), e[2][q], e[3][q]);
                         }
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
@@ -499,7 +530,7 @@ __device__ __noinline__ void producer8_loop(const PageAttn& p, const Work& w, co
             __syncwarp();
             if (lane == 0) mbar_arrive(BAR((part < C::BLK ? C::KFULL : C::VFULL) + (int)st));
             cur = nxt;
-            page = page_n;
+            here = ahead;
             slab = next;
         }
         it += (uint32_t)n;
@@ -580,8 +611,9 @@ __device__ __noinline__ float scale_query(float scale, uint8_t* tile) {
     return fmaxf(scale * __int_as_float((127 + min(e, 127)) << 23), MIN_FACTOR);
 }
 
-// BITS 8: a page's keys have a scale, which goes into the factor of its logits, and its values one, 2^ev, by which the weights are
-// multiplied; so the logits are moved by ev, the maximum is that of the moved ones, and the sum takes ev back.
+// BITS 8: a page's keys have a scale, which goes into the factor of its logits; its values are counted in 2^ref (see the producers), and so
+// is the output, which is brought there when ref changes: exactly, since float32 holds sums of values up to 2^16 in units of the smallest ref,
+// 2^-65, and of the smallest values in units of the largest.
 template <typename T, int D, int BITS>
 __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, const Cta c, Units u) {
     using C = Cfg<D>;
@@ -616,6 +648,7 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
         const int q_min = min(__reduce_min_sync(0xFFFFFFFFu, qpos), total - 1), q_max = __reduce_max_sync(0xFFFFFFFFu, qpos);
         const int tok_lo = p.window > 0 ? q_max - p.window + 1 : 0, tok_hi = q_min - (XSV_PAGE - 1);
         float m_used = NO_MAX, l = 0.f;
+        int ref_used = 0;
         bool first = true;
         for (int k = 0; k < n; ++k) {
             const int tok0 = (u.en.p0 + u.kv0 + k) * XSV_PAGE;
@@ -626,19 +659,22 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
             tmem_ld32(tSb, va);
             int ok;
             asm volatile("ld.shared.b32 %0, [%1];" : "=r"(ok) : "r"(c.page_ok + 4u * ((it + (uint32_t)k) % C::NSTAGE)) : "memory");
-            float sp = sc, ev = 0.f;
+            float sp = sc;
+            int ref = 0;
             if (BITS == 8) {
-                float ks;
-                asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(ks), "=f"(ev) : "r"(c.page_ok + 4u * C::NSTAGE + 8u * ((it + (uint32_t)k) % C::NSTAGE)) : "memory");
-                sp = fmaxf(sc * ks, MIN_FACTOR);
+                int ks;
+                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(ks), "=r"(ref) : "r"(c.page_ok + 4u * C::NSTAGE + 8u * ((it + (uint32_t)k) % C::NSTAGE)) : "memory");
+                sp = fmaxf(sc * __int_as_float(ks), MIN_FACTOR);
+                if (first) ref_used = ref;
             }
+            const bool moved = BITS == 8 && ref != ref_used;           // uniform
             tc_wait_ld();
             tmem_ld32(tSb + 32u, vb);              // arrives under the first half's exponentials
             const bool mask = !(tok0 >= tok_lo && tok0 <= tok_hi && ok);     // uniform
             float ls = 0.f;
-            bool careful = first || mask;
+            bool careful = first || mask || moved;
             if (!careful) {
-                const unsigned long long sc2 = f2_pack(sp, sp), nm2 = f2_pack(BITS == 8 ? ev - m_used : -m_used, BITS == 8 ? ev - m_used : -m_used);
+                const unsigned long long sc2 = f2_pack(sp, sp), nm2 = f2_pack(BITS == 8 ? P_BIAS - m_used : -m_used, BITS == 8 ? P_BIAS - m_used : -m_used);
                 unsigned long long ls2 = f2_pack(0.f, 0.f);
                 softmax32(va, sc2, nm2, ls2, pk);
                 tmem_st16(tSb, pk);
@@ -648,7 +684,7 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
                 float l0, l1;
                 f2_unpack(ls2, l0, l1);
                 ls = l0 + l1;
-                careful = __any_sync(0xFFFFFFFFu, !(ls < SUM_LIMIT));
+                careful = __any_sync(0xFFFFFFFFu, !(ls < SUM_LIMIT<BITS>));
             } else {
                 tc_wait_ld();
             }
@@ -664,9 +700,9 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
                 float mx = -INFINITY;
 #pragma unroll
                 for (int q = 0; q < 32; ++q) mx = fmax3(mx, __uint_as_float(va[q]), __uint_as_float(vb[q]));
-                const float m_new = BITS == 8 ? fmaf(mx, sp, ev) : mx * sc;
+                const float m_new = mx * sp;
                 const bool need = m_new > m_used;
-                if (__any_sync(0xFFFFFFFFu, need)) {
+                if (moved || __any_sync(0xFFFFFFFFu, need)) {
                     if (!first) {
                         wait_pv(cX - 1u);
                         tc_fence_after();
@@ -674,6 +710,8 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
                     const float alpha = need ? ex2(m_used - m_new) : 1.f;
                     if (need) m_used = m_new;
                     l *= alpha;
+                    const float beta = BITS == 8 ? alpha * p8_pow2(ref_used - ref) : alpha;
+                    ref_used = ref;
                     if (!first) {
 #pragma unroll 1
                         for (int q = 0; q < D / 16; ++q) {
@@ -681,12 +719,12 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
                             tmem_ld16(tO + 16u * q, o);
                             tc_wait_ld();
 #pragma unroll
-                            for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * alpha);
+                            for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * beta);
                             tmem_st16(tO + 16u * q, o);
                         }
                     }
                 }
-                const unsigned long long sc2 = f2_pack(sp, sp), nm2 = f2_pack(BITS == 8 ? ev - m_used : -m_used, BITS == 8 ? ev - m_used : -m_used);
+                const unsigned long long sc2 = f2_pack(sp, sp), nm2 = f2_pack(BITS == 8 ? P_BIAS - m_used : -m_used, BITS == 8 ? P_BIAS - m_used : -m_used);
                 unsigned long long ls2 = f2_pack(0.f, 0.f);
                 softmax32(va, sc2, nm2, ls2, pk);
                 tmem_st16(tSb, pk);
@@ -696,7 +734,7 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
                 f2_unpack(ls2, l0, l1);
                 ls = l0 + l1;
             }
-            l = BITS == 8 ? fmaf(ls, p8_pow2(-(int)ev), l) : l + ls;
+            l += ls;
             tc_wait_st();
             tc_fence_before();
             __syncwarp();
@@ -720,7 +758,7 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
         wait_pv(cX - 1u);
         tc_fence_after();
         if (*c.abort_flag) l = __int_as_float(0x7FC00000);
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float unit = BITS == 8 ? p8_pow2(ref_used) : 1.f, inv = l == 0.f ? 0.f : unit / l;
 #pragma unroll 2
         for (int q = 0; q < D / 16; ++q) {
             uint32_t o[16];
@@ -737,7 +775,8 @@ __device__ __noinline__ void softmax_loop(const PageAttn& p, const Work& w, cons
             } else {
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    pr[(4 * q + k) * 256] = make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]), __uint_as_float(o[4 * k + 2]), __uint_as_float(o[4 * k + 3]));
+                    pr[(4 * q + k) * 256] = make_float4(__uint_as_float(o[4 * k]) * unit, __uint_as_float(o[4 * k + 1]) * unit, __uint_as_float(o[4 * k + 2]) * unit,
+                                                        __uint_as_float(o[4 * k + 3]) * unit);
             }
         }
         if (!full) reinterpret_cast<float2*>(part + 256 * D)[X * BM + row] = make_float2(m_used, l);
