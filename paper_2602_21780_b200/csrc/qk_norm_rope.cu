@@ -12,11 +12,12 @@
 //
 // Angles: position * inv_freq in turns as a float64 product, its fraction in float32: a float32 angle of a position
 // near 10^6 would be off by 0.03 rad.  With several positions a token (time, height, width) the thread that serves a frequency
-// looks up once which of them it turns by.  Norms are float32, the layer norm's variance from differences to the mean (two
-// passes over registers); results are rounded once, to the output type.
-// Measured: 8191 tokens, 32 + 8 + 8 heads of 128, fp16: 41.8 us, 4.8 TB/s (one token a turn: 44.5); 1374 tokens, 3 x 16 heads of 64: 7.5 us with two
-// positions; one token: 2.6 us.  What is left to the copy rate is loads in flight: 7 or 8 blocks of 4 warps with two rows each; three to
-// six rows a lane group or fewer blocks were slower (48-54 us), and packed float32 arithmetic changed nothing.
+// looks up once which of them it turns by, in kernels of their own: the calls with one position lose 1 to 4 % to the lookup
+// otherwise.  Norms are float32, the layer norm's variance from differences to the mean (two passes over registers); results
+// are rounded once, to the output type.
+// Measured: 8191 tokens, 32 + 8 + 8 heads of 128, fp16: 41.8 us, 4.8 TB/s (one token a turn: 43.7); 1374 tokens, 3 x 16 heads of 64, rotated by
+// row and column: 7.4 us; one token: 2.5 us.  What is left to the copy rate is loads in flight: 7 or 8 blocks of 4 warps with two rows each;
+// three to six rows a lane group or fewer blocks were slower (48-54 us), and packed float32 arithmetic changed nothing.
 #include <algorithm>
 #include <type_traits>
 
@@ -51,7 +52,7 @@ constexpr int THREADS = 128, FLIGHT = 2;      // FLIGHT: rows of a lane group in
 
 // TOK: tokens of a turn.  2 (many tokens): the two rows in flight are the same head of two tokens, all threads compute sines, and
 // a barrier serves both tokens.
-template <typename T, int D, int ROPE, int NORM, bool BIAS, int TOK>
+template <typename T, int D, int ROPE, bool AXES, int NORM, bool BIAS, int TOK>
 __global__ void __launch_bounds__(THREADS, TOK == 2 ? 7 : 8) qk_norm_rope_kernel(const __grid_constant__ NormRope p) {
     constexpr int L = D / 8, GROUPS = THREADS / L;
     __shared__ float2 cs[2][TOK][D / 2];
@@ -92,18 +93,19 @@ __global__ void __launch_bounds__(THREADS, TOK == 2 ? 7 : 8) qk_norm_rope_kernel
     // the frequency this thread serves, of which of the turn's tokens; its position is fetched a turn ahead
     const int mine = TOK == 2 ? (int)threadIdx.x / (D / 2) : 0, fi = (int)threadIdx.x - mine * (D / 2);
     const bool serves = ROPE != XSV_ROPE_NONE && mine < TOK && fi < n_freq;
+    auto place = [&](int t, int c) { return AXES ? (size_t)t * p.n_pos + c : ROPE == XSV_ROPE_2D ? 2 * (size_t)t + c : (size_t)t; };
     int coord = 0, at = 0;
     double freq = 0.0;
     if (serves) {
-        const int per = ROPE == XSV_ROPE_2D ? n_freq / 2 : n_freq;
-        coord = fi / per;
-        freq = (double)p.inv_freq[fi - coord * per];
-        if (ROPE != XSV_ROPE_2D && p.axes) {
+        coord = ROPE == XSV_ROPE_2D && fi >= n_freq / 2 ? 1 : 0;
+        float f0 = p.inv_freq[fi - coord * (n_freq / 2)];      // on its way together with the position
+        if (AXES) {
             coord = p.axes[fi];
-            if (coord < 0 || coord >= p.n_pos) { coord = 0; freq = 0.0; }       // no such position: not rotated
+            if (coord < 0 || coord >= p.n_pos) { coord = 0; f0 = 0.f; }         // no such position: not rotated
         }
         const int t = blockIdx.x + mine * gridDim.x;
-        if (t < p.n_tokens) at = p.pos[(size_t)t * p.n_pos + coord];
+        if (TOK == 1 || t < p.n_tokens) at = p.pos[place(t, coord)];
+        freq = (double)f0;
     }
     int buf = 0;
     for (int t = blockIdx.x; t < p.n_tokens; t += TOK * gridDim.x, buf ^= 1) {
@@ -117,7 +119,7 @@ __global__ void __launch_bounds__(THREADS, TOK == 2 ? 7 : 8) qk_norm_rope_kernel
                 sincospif(2.f * (float)turns, &s, &c);
                 cs[buf][mine][fi] = make_float2(c, s);
                 const int next = t + (mine + TOK) * (int)gridDim.x;
-                if (next < p.n_tokens) at = p.pos[(size_t)next * p.n_pos + coord];
+                if (next < p.n_tokens) at = p.pos[place(next, coord)];
             }
             __syncthreads();                                // two buffers: the last turn's are read before this one
             if (TOK == 1)
@@ -206,19 +208,31 @@ cudaError_t launch(const NormRope& p, int norm, int rope, cudaStream_t st) {
     // through its share of them (32 + 8 + 8 heads of 128: 148 tokens 3.1 against 3.6 us, 296 tokens 3.9 either way, 592
     // tokens 5.8 against 4.4).
     const dim3 grid(std::min(p.n_tokens, full), p.n_tokens >= 2 * xsv_sm_count() ? 1 : (most + groups - 1) / groups);
-    // Two tokens a turn where each block gets more than one turn of them, in as many blocks as make the turns come out even (8219 tokens, heads of 128
-    // 44.8 -> 42.0 us; 8000 tokens, heads of 64, layer norm 30.8 -> 24.3).
-    const int pairs = (p.n_tokens + 1) / 2, most2 = 7 * xsv_sm_count(), turns = (pairs + most2 - 1) / most2;
-    const bool two = turns > 1;
-    const dim3 grid2((pairs + turns - 1) / turns);
+    // Two tokens a turn, in 7 blocks a multiprocessor.  What it saves is rounds of a lane group's two rows (of a part's heads, or of one head of two
+    // tokens); what it costs is the last turn, which is up to twice as long.  Half or two thirds of the rounds (head counts up to THREADS / 8 lanes
+    // of 64, / 16 of 128 have one row to a round otherwise): from 6/5 of a turn on (16 + 16 + 16 heads of 64: 2300 tokens 10.0 either
+    // way, 2500 10.9 against 12.7 us, 4145 14.6 against 17.7, 8191 24.8 against 31.2; 32 + 8 + 8: 2300 10.9 against 9.6, 2500 11.6
+    // either way, 4600 18.3 against 17.8, 8191 26.0 against 29.3).  Three quarters: where the last turn is nearly full (32 + 8 + 8 heads of 128: 2300
+    // tokens 18.0 against 14.6, 3700 21.7 against 23.2, 4600 29.0 against 26.4, 8191 42.1 against 44.0, 9000 49.4 against 48.6).  More: never (16 + 16 +
+    // 16 heads of 128: 4144 tokens 22.3 against 22.2, 8191 40.9 against 39.4).
+    int rounds1 = 0, rounds2 = 0;
+    for (int part = 0; part < 3; ++part) {
+        rounds1 += 2 * ((p.heads[part] + FLIGHT * groups - 1) / (FLIGHT * groups));
+        rounds2 += (p.heads[part] + groups - 1) / groups;
+    }
+    const int pairs = (p.n_tokens + 1) / 2, most2 = 7 * xsv_sm_count();
+    const long long turns = (pairs + most2 - 1) / most2;
+    const bool two = 3 * rounds2 <= 2 * rounds1 ? 5LL * pairs >= 6LL * most2 : 4 * rounds2 <= 3 * rounds1 && turns > 1 && 9LL * pairs >= 8 * turns * most2;
+    const dim3 grid2(std::min(pairs, most2));
     const bool bias = p.b[0] || p.b[1];
-    auto with = [&](auto rope_c) {
+    auto with = [&](auto rope_c, auto axes_c) {
         constexpr int ROPE = decltype(rope_c)::value;
+        constexpr bool AXES = decltype(axes_c)::value;
         auto go = [&](auto norm_c, auto bias_c) {
             constexpr int NORM = decltype(norm_c)::value;
             constexpr bool BIAS = decltype(bias_c)::value;
-            return two ? xsv_launch_dep(qk_norm_rope_kernel<T, D, ROPE, NORM, BIAS, 2>, grid2, dim3(THREADS), 0, st, p)
-                       : xsv_launch_dep(qk_norm_rope_kernel<T, D, ROPE, NORM, BIAS, 1>, grid, dim3(THREADS), 0, st, p);
+            return two ? xsv_launch_dep(qk_norm_rope_kernel<T, D, ROPE, AXES, NORM, BIAS, 2>, grid2, dim3(THREADS), 0, st, p)
+                       : xsv_launch_dep(qk_norm_rope_kernel<T, D, ROPE, AXES, NORM, BIAS, 1>, grid, dim3(THREADS), 0, st, p);
         };
         using Rms = std::integral_constant<int, XSV_NORM_RMS>;
         using Layer = std::integral_constant<int, XSV_NORM_LAYER>;
@@ -228,11 +242,15 @@ cudaError_t launch(const NormRope& p, int norm, int rope, cudaStream_t st) {
             default: return go(std::integral_constant<int, XSV_NORM_NONE>{}, std::false_type{});
         }
     };
+    using No = std::false_type;
+    using Yes = std::true_type;
+    using Half = std::integral_constant<int, XSV_ROPE_HALF>;
+    using Pairs = std::integral_constant<int, XSV_ROPE_PAIRS>;
     switch (rope) {
-        case XSV_ROPE_HALF: return with(std::integral_constant<int, XSV_ROPE_HALF>{});
-        case XSV_ROPE_PAIRS: return with(std::integral_constant<int, XSV_ROPE_PAIRS>{});
-        case XSV_ROPE_2D: return with(std::integral_constant<int, XSV_ROPE_2D>{});
-        default: return with(std::integral_constant<int, XSV_ROPE_NONE>{});
+        case XSV_ROPE_HALF: return p.axes ? with(Half{}, Yes{}) : with(Half{}, No{});
+        case XSV_ROPE_PAIRS: return p.axes ? with(Pairs{}, Yes{}) : with(Pairs{}, No{});
+        case XSV_ROPE_2D: return with(std::integral_constant<int, XSV_ROPE_2D>{}, No{});
+        default: return with(std::integral_constant<int, XSV_ROPE_NONE>{}, No{});
     }
 }
 
