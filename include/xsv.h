@@ -644,7 +644,8 @@ size_t xsv_page8_attention_workspace(int n_tokens, int n_seqs, int max_new, int 
  *                  whole number sum of q8 * mean, a = max(max |q|, 2^-60) and q8 = nearest-even of q * (127 / a), and
  *                  mean = nearest-even of S * (127 / A), factor = A * s / 64 with S the sum of a channel's 64 key codes and A the
  *                  largest |S| (0 where that is 0): a logit against the page's mean key, but for a constant.  Equal scores:
- *                  the lower page first.  A page that the table does not have is not taken.
+ *                  the lower page first.  A page that the table does not have is not taken, be it a first, recent or other one;
+ *                  its place is the next best one's.
  *   Q            : device, n_tokens rows of [q_heads][head_dim] at q_stride elements (a multiple of 8).
  *   token_seq, positions : the plan's, [n_tokens]; a token of sequence -1 selects nothing.  All pages before the token's own
  *                  must have been filled by appends.

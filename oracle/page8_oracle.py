@@ -124,10 +124,12 @@ def scores(q, means):
     return best
 
 
-def select(q, means, mine, top, first, recent):
-    """Pages that a token whose own page is `mine` selects; means[p] is None for a page that is not there."""
-    keep = [p for p in range(mine + 1) if p < first or p > mine - recent]
-    middle = [p for p in range(mine + 1) if p not in keep and means[p] is not None]
+def select(q, means, mine, top, first, recent, there=None):
+    """Pages that a token whose own page is `mine` selects; means[p] is None for a page that is not there, or not full (as the last
+    may be); there[p]: whether it is there (None: all of the first and the most recent are)."""
+    fixed = [p for p in range(mine + 1) if p < first or p > mine - recent]
+    middle = [p for p in range(mine + 1) if p not in fixed and means[p] is not None]
+    keep = [p for p in fixed if there is None or there[p]]
     s = scores(q, [means[p] for p in middle])
     order = sorted(range(len(middle)), key=lambda i: (-float(s[i]), middle[i]))
     out = sorted(keep + [middle[i] for i in order[:top - len(keep)]])

@@ -12,6 +12,9 @@
 // A cluster of up to 8 blocks shares the pages of one token where few tokens have long sequences: each stores its keys into the first block's
 // shared memory, which selects.
 //
+// The first and the recent pages are looked up in the table at the start, beside the scores' loads, since one that is not there is not
+// listed and leaves its place to another.
+//
 // Measured.  32 query and 8 key/value heads of 128, 32 pages each: 16 tokens over 2000 to 60 000: 11.4 us, of which the launch and
 // four loads that wait for one another (token, table, mean key; query) are about 6, the selection 3; 1021 tokens over 40 000: 41 us, half of it
 // the scores' and half of it the selections' instructions, at 32 warps a multiprocessor (at 16: 50).
@@ -206,16 +209,42 @@ template <int W> __device__ __forceinline__ int take_any(const uint32_t* keys, i
     return take<W, 0>(keys, n, k, from, to, note, wid);
 }
 
-// One token's list: the first pages, the best of those between, the most recent ones, -1.
-template <int W> __device__ __forceinline__ void list_of(const Select& p, const uint32_t* keys, int mine, int* out, int* note, int wid) {
+// The pages that a token whose own page is `mine` takes unscored if the table has them: the first nf, and those from r0 on.
+struct Fixed {
+    int nf, r0, n;
+    __device__ __forceinline__ Fixed(const Select& p, int mine) : nf(min(p.first, mine + 1)), r0(max(nf, mine - p.recent + 1)), n(nf + mine + 1 - r0) {}
+    __device__ __forceinline__ int page(int x) const { return x < nf ? x : r0 + x - nf; }
+};
+// The place of the x-th of them, -1 beyond the last.
+__device__ __forceinline__ int fixed_place(const Select& p, const Fixed& f, int seq, int x) { return x < f.n ? p.table[(size_t)seq * p.width + f.page(x)] : -1; }
+
+// One token's list: the first pages, the best of those between, the most recent ones, -1.  ahead: fixed_place of this lane, looked up before.
+template <int W> __device__ __forceinline__ void list_of(const Select& p, const uint32_t* keys, int seq, int mine, int ahead, int* out, int* note, int wid) {
     const int lane = threadIdx.x & 31, tid = wid * 32 + lane;
     int n = 0;
     if (mine >= 0) {
-        const int nf = min(p.first, mine + 1), r0 = max(nf, mine - p.recent + 1), nr = mine + 1 - r0;      // recent: [r0, mine]
-        for (int i = tid; i < nf; i += 32 * W) out[i] = i;
-        const int mid = take_any<W>(keys + nf, r0 - nf, p.top - nf - nr, nf, out + nf, note, wid);
-        for (int i = tid; i < nr; i += 32 * W) out[nf + mid + i] = r0 + i;
-        n = nf + mid + nr;
+        const Fixed f(p, mine);
+        auto there = [&](int x0) {                             // of the 32 from x0 on
+            const int page = x0 == 0 ? ahead : fixed_place(p, f, seq, x0 + lane);
+            return __ballot_sync(0xFFFFFFFFu, (unsigned long long)(long long)page < (unsigned long long)p.pool.n_pages);
+        };
+        int has = 0, has_first = 0;
+        for (int x0 = 0; x0 < f.n; x0 += 32) {
+            const uint32_t in = there(x0);
+            has += __popc(in);
+            if (x0 < f.nf) has_first += __popc(f.nf - x0 < 32 ? in & ((1u << (f.nf - x0)) - 1u) : in);
+        }
+        const int mid = take_any<W>(keys + f.nf, f.r0 - f.nf, p.top - has, f.nf, out + has_first, note, wid);
+        n = has + mid;
+        if (wid == 0) {
+            int at = 0;
+            for (int x0 = 0; x0 < f.n; x0 += 32) {
+                const uint32_t in = there(x0);
+                const int x = x0 + lane;
+                if (in >> lane & 1u) out[at + __popc(in & ((1u << lane) - 1u)) + (x < f.nf ? 0 : mid)] = f.page(x);
+                at += __popc(in);
+            }
+        }
     }
     for (int i = n + tid; i < p.top; i += 32 * W) out[i] = -1;
 }
@@ -297,6 +326,10 @@ __global__ void __launch_bounds__(THREADS, MODE == MANY ? 4 : 2) page8_select_ke
             }
         }
     };
+    // (a warp's token is its number where a block has several, 8 at most)
+    const int listed = MODE == MANY ? wid : 0;
+    int ahead = -1;
+    if (listed < here && s_mine[listed] >= 0) ahead = fixed_place(p, Fixed(p, s_mine[listed]), s_seq[listed], lane);
     const int base0 = p.first + (rank * WARPS + wid) * TURN, step = (CLUSTER ? p.cluster : 1) * WARPS * TURN;
     begin_run(0);
     if (base0 < end) fetch(look_up(0, base0));                 // on their way while the queries are read
@@ -470,12 +503,10 @@ __global__ void __launch_bounds__(THREADS, MODE == MANY ? 4 : 2) page8_select_ke
     }
     __syncthreads();
     // ---- the lists
-    if (MODE == MANY) {
-        for (int i = wid; i < here; i += WARPS)
-            list_of<1>(p, keys + i * across, s_mine[i], p.out + ((size_t)(t0 + i) * p.pool.heads + head) * p.top, s_note, 0);
-    } else {
-        list_of<WARPS>(p, keys, s_mine[0], p.out + ((size_t)t0 * p.pool.heads + head) * p.top, s_note, wid);
-    }
+    static_assert(WARPS >= 8, "a warp for each of a block's tokens");
+    if (listed < here)
+        list_of<MODE == MANY ? 1 : WARPS>(p, keys + listed * across, s_seq[listed], s_mine[listed], ahead, p.out + ((size_t)(t0 + listed) * p.pool.heads + head) * p.top,
+                                          s_note, MODE == MANY ? 0 : wid);
 }
 
 size_t smem_of(int tokens, int rows, int head_dim, int width) {

@@ -157,3 +157,13 @@ def test_binding_refuses_tensors_it_cannot_take():
                   lambda: binding.page8_attention_selected(x, pages, i[None], i, i, i.view(1, 1, 3))):
         with pytest.raises(ValueError, match="CUDA"):
             call_()
+
+
+def test_select_without_pages_that_are_not_there():
+    means = [(np.array([p, 0]), 1.0) for p in range(12)]                     # the later, the better
+    q, lost = np.array([[127.0, 0.0]]), [p not in (0, 8, 11) for p in range(12)]
+    gone = [m if there else None for m, there in zip(means, lost)]
+    assert orc.select(q, means, 11, 6, 2, 3) == [0, 1, 8, 9, 10, 11]
+    assert orc.select(q, gone, 11, 6, 2, 3, lost) == [1, 5, 6, 7, 9, 10]
+    assert orc.select(q, [None] * 12, 11, 3, 1, 2, [False] * 12) == [-1] * 3
+    assert orc.select(q, gone, 1, 6, 2, 3, lost) == [1] + [-1] * 5
