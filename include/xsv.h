@@ -593,7 +593,8 @@ size_t xsv_page_attention_workspace(int n_tokens, int n_seqs, int max_new, int q
  * below 2^-6 s.  Codes are written as their tokens come (there is no 16-bit tail); when a later token of an unfilled page
  * needs a larger scale, the codes that stand there are brought to it, which rounds only those that become smaller than
  * 2^-6 s.  Inputs are finite; magnitudes beyond 65504 count as 65504, whose code stands for 65536 (read back as 65504 in
- * fp16).  A full page also has its mean key, in whole numbers of 8 bits with a factor, for xsv_page8_select.
+ * fp16), and so would infinities and NaN, which the pages cannot tell any more.  A full page also has its mean key, in
+ * whole numbers of 8 bits with a factor, for xsv_page8_select.
  *
  * Block tables, lengths and slots are those of xsv_page_plan.  A step of a model: xsv_page_plan once, then per layer
  * xsv_qk_norm_rope, xsv_page8_append, and xsv_page8_attention, or xsv_page8_select and xsv_page8_attention_selected.

@@ -551,7 +551,9 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) page8_attn_kern
 // begin to be shared there: as many warps a unit as there are for it, which take its parts in turn and are merged in their order; a lane has
 // 4 values (2 rows x 2 channels).  (The whole block for one unit after the other: 15 us instead of 5 where most units have two parts.)
 // (One warp for all channels of a unit: 147 instead of 151 us where a unit has at most two parts, 211 instead of 184 and 45 instead of 34 where
-// there are more.)  It costs the calls that share units 6 to 9 us: its launch, its descriptions' and then its parts' latency.
+// there are more.)  Measured with and without the second launch, it costs one
+// sequence of 261 2.3 us, 64 sequences and 4 tokens over 200 001 7.5, 32 selecting sequences 5.4, 509 selecting tokens 8.7: its launch, its
+// descriptions' and then its parts' latency.
 constexpr int MERGE_UNITS = 16, MERGE_WARPS = 8;
 template <typename T, int D, int NT>
 __global__ void __launch_bounds__(MERGE_WARPS * 32) page8_attn_merge_kernel(const __grid_constant__ Attn8 p, int workers) {

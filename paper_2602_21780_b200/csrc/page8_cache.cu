@@ -13,7 +13,9 @@
 // xsv_page8_read: a thread looks one token up and decodes 8 channels of it, of up to 4 heads.
 //
 // Measured.  Append of 19 735 prompt tokens, 8 heads of 64, fp16: 14.5 us, 4.2 TB/s; 8 heads of 128, bf16: 24.5 us, 4.95 TB/s; one token for each
-// of 256 sequences, 8 heads of 128: 4.3 us.  Reading 19 735 tokens of 8 x 64 back: 12.9 us, 4.7 TB/s; 8150 of 8 x 128: 11.1 us, 4.5 TB/s.
+// of 256 sequences, 8 heads of 128: 4.3 us.  Reading 19 735 tokens of 8 x 64 back: 12.8 us, 4.7 TB/s; 8150 of 8 x 128: 11.2 us, 4.5 TB/s.
+// From 4000 to 158 000 tokens both are a fixed part (launch, dependent lookups) and a rate: append 2.9 us and 5.4 TB/s at heads of 64, 3.6 us and the
+// copy rate at 128; read 2.2 us and 6.1 TB/s, 2.9 us and 6.3 TB/s.
 #include <type_traits>
 
 #include "../../include/xsv.h"

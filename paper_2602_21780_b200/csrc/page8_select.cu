@@ -15,7 +15,7 @@
 // The first and the recent pages are looked up in the table at the start, beside the scores' loads, since one that is not there is not
 // listed and leaves its place to another.
 //
-// Measured.  32 query and 8 key/value heads of 128, 32 pages each: 16 tokens over 2000 to 60 000: 11.4 us, of which the launch and
+// Measured.  32 query and 8 key/value heads of 128, 32 pages each: 16 tokens over 2000 to 60 000: 11.5 us, of which the launch and
 // four loads that wait for one another (token, table, mean key; query) are about 6, the selection 3; 1021 tokens over 40 000: 41 us, half of it
 // the scores' and half of it the selections' instructions, at 32 warps a multiprocessor (at 16: 50).
 #include <algorithm>

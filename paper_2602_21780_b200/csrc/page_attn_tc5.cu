@@ -23,7 +23,7 @@
 // Measured.  1374 tokens on 21 984, 16 heads of 64, 4 bit: 217 us, 590 TFLOP/s (0.42 of the sustained bf16 peak; the kernel for few
 // rows took 788); 6 chunks of 300 to 2047 tokens on up to 9000, 32 / 8 heads of 128, in bursts: 4 bit 400 us, 872 TFLOP/s (0.61), 8 bit 380 us,
 // 917 TFLOP/s (0.65; 373 without the products that bring the values to their unit); call after call, under the power cap, 8 bit takes 395 to
-// 405 us (0.61 to 0.62).  At head_dim 64 the exponentials alone, 16 a clock and multiprocessor, take about 115 us of the frame.
+// 413 us (0.60 to 0.62).  At head_dim 64 the exponentials alone, 16 a clock and multiprocessor, take about 115 us of the frame.
 // The softmax warps are busy 90 % of the time, the producers wait 55 % of it for free stages.  Storing the tiles
 // through generic addresses cost 20 %; the second half of the logits arriving under the first half's exponentials and the
 // range of unmasked pages known per unit gave 5 %; a share of 1/8 of the exponentials as polynomials cost 10 %; quarters of the logits with
@@ -40,8 +40,10 @@ namespace {
 
 constexpr int BM = 128, NPROD = 6, NTHREADS = (8 + NPROD + 2) * 32;
 // Cost of a step with two query tiles, with one, and of entering a unit, in ticks: the steps' are the ratios of the attention over the
-// contiguous cache; a unit's is fitted (6 chunks, 8-bit pages: 72 430 us, 100 405, 144 377, 160 369, 200 373; 4-bit 448, 425, 398, 398, 401; a
-// frame on 21 984 does not tell them apart).
+// contiguous cache; a unit's is fitted, over eight mixes (6 chunks of 300 to 2047 tokens, 40 of 60 to 300, 3 of 400 to 700 on 8000, one of 300 on 60 000, 20
+// with a window of 500, a prompt of 2000, 100 prompts of 100 to 400, 8 chunks of 70 to 150 on up to 20 000), heads of 64 and 128, both kinds of pages:
+// 100 is 2 to 3 % slower than 144, 160 and 200 at heads of 128, 0.5 % at heads of 64, and these three are within 1.2 % of one another; single mixes differ
+// by up to 5 % either way.
 constexpr int COST_PAIR = 16, COST_SINGLE = 13, COST_UNIT = 160, MIN_SPAN = 320;
 // A row sum that reaches 2^8: look for the maximum again.  Over 8-bit pages weights and sums are 2^P_BIAS larger, still below fp16's largest
 // value, so that a weight keeps fp16's full significand down to 2^-21 of the maximum.
