@@ -220,7 +220,7 @@ cudaError_t launch(const NormRope& p, int norm, int rope, cudaStream_t st) {
         rounds1 += 2 * ((p.heads[part] + FLIGHT * groups - 1) / (FLIGHT * groups));
         rounds2 += (p.heads[part] + groups - 1) / groups;
     }
-    const int pairs = (p.n_tokens + 1) / 2, most2 = 7 * xsv_sm_count();
+    const int pairs = p.n_tokens / 2 + p.n_tokens % 2, most2 = 7 * xsv_sm_count();
     const long long turns = (pairs + most2 - 1) / most2;
     const bool two = 3 * rounds2 <= 2 * rounds1 ? 5LL * pairs >= 6LL * most2 : 4 * rounds2 <= 3 * rounds1 && turns > 1 && 9LL * pairs >= 8 * turns * most2;
     const dim3 grid2(std::min(pairs, most2));
